@@ -32,6 +32,9 @@ __all__ = [
     "qlayer_linear_bwd_workspace_size", "qlayer_linear_bwd",
     "qlayer_conv2d_bwd_relu_workspace_size", "qlayer_conv2d_bwd_relu",
     "qlayer_linear_bwd_relu_workspace_size", "qlayer_linear_bwd_relu",
+    "HEAD_ACTS", "HEAD_MAX_TOP", "HeadLinearDesc", "HeadRowsDesc",
+    "qhead_linear_fwd", "qhead_linear_bwd", "qhead_logprobs_fwd", "qhead_logprobs_bwd",
+    "qhead_distill_fwd", "qhead_distill_bwd", "qhead_distill_step",
 ]
 
 QL_F32 = 0
@@ -86,6 +89,19 @@ class Epilogue(ctypes.Structure):
     per-channel sum / sum of squares of the stored y' (every member optional)."""
     _fields_ = [("scale", ctypes.c_void_p), ("shift", ctypes.c_void_p), ("relu", ctypes.c_int),
                 ("sum", ctypes.c_void_p), ("sumsq", ctypes.c_void_p)]
+
+
+class HeadLinearDesc(ctypes.Structure):
+    """qhead_linear_desc: a first-order fully-connected layer (row strides in elements)."""
+    _fields_ = [("m", ctypes.c_int), ("k", ctypes.c_int), ("n", ctypes.c_int), ("ldx", ctypes.c_longlong),
+                ("ldw", ctypes.c_longlong), ("ldr", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int)]
+
+
+class HeadRowsDesc(ctypes.Structure):
+    """qhead_rows_desc: rows of logits, the places per row, temperature and the teacher's share."""
+    _fields_ = [("rows", ctypes.c_int), ("vocab", ctypes.c_int), ("ld", ctypes.c_longlong), ("top", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
 def epilogue(scale=None, shift=None, relu=False, stat_sum=None, stat_sumsq=None) -> Epilogue:
@@ -165,6 +181,19 @@ def lib():
     L.qnet_gap_bwd.argtypes = [sp, ctypes.c_int, _vp, _vp, _vp]
     for name in ("bn_act_fwd", "bn_act_bwd", "residual_bwd", "gap_fwd", "gap_bwd"):
         getattr(L, f"qnet_{name}").restype = ctypes.c_int
+    # the end of a network (include/qhead.h)
+    hl, hr = ctypes.POINTER(HeadLinearDesc), ctypes.POINTER(HeadRowsDesc)
+    for name, d, tensors, space in (("linear_fwd", hl, 6, True), ("linear_bwd", hl, 7, True),
+                                    ("logprobs_fwd", hr, 8, True), ("logprobs_bwd", hr, 7, False),
+                                    ("distill_fwd", hr, 6, True), ("distill_bwd", hr, 7, False),
+                                    ("distill_step", hr, 7, True)):
+        f = getattr(L, f"qhead_{name}")
+        f.argtypes = [d] + [_vp] * tensors + ([_vp, _sz] if space else []) + [_vp]
+        f.restype = ctypes.c_int
+    for name, d in (("linear_fwd", hl), ("linear_bwd", hl), ("logprobs_fwd", hr), ("distill", hr)):
+        f = getattr(L, f"qhead_{name}_workspace_size")
+        f.argtypes = [d]
+        f.restype = _sz
     _lib = L
     return L
 
@@ -581,3 +610,211 @@ def qnet_gap_bwd(dy, dx, stream=None):
     _expect("dy", dy, dx.shape[0] * dx.shape[3], dx.dtype, dev)
     _check("qnet_gap_bwd", lib().qnet_gap_bwd(ctypes.byref(net_shape(dx)), _net_dtype(dx), _ptr(dy), _ptr(dx),
                                               _stream(stream, dev)))
+
+
+# --- the end of a network (include/qhead.h) ------------------------------------
+# Matrices are 2-D tensors with contiguous rows, which may lie apart (a column
+# range of a wider tensor); their shapes and strides make the descriptor.
+
+HEAD_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+HEAD_MAX_TOP = 128  # QHEAD_MAX_TOP of qhead.h
+
+
+class _HeadOperands:
+    """Checks the tensors of one call and collects their pointers.
+
+    The first tensor sets the device; each one has to be on it, of its role's
+    dtype and shape, with contiguous rows."""
+
+    def __init__(self, t, dims=2):
+        import torch
+        self.torch = torch
+        self.index = t.get_device()
+        if self.index < 0:
+            raise ValueError(f"a CUDA device tensor is required, got one on {t.device}")
+        if t.dtype is torch.bfloat16:
+            self.code = QL_BF16
+        elif t.dtype is torch.float32:
+            self.code = QL_F32
+        else:
+            raise ValueError(f"dtype {t.dtype}: bfloat16 or float32 is required")
+        if t.dim() != dims:
+            raise ValueError(f"{t.dim()} dimensions, a matrix is required")
+        self.dtype = t.dtype
+        self.ptrs = []
+
+    def _take(self, name, t, shape, dtype):
+        if t.get_device() != self.index:
+            raise ValueError(f"{name}: on {t.device}, the other tensors on cuda:{self.index}")
+        if t.dtype is not dtype:
+            raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+        self.ptrs.append(t.data_ptr())
+
+    def rows(self, name, t, shape):
+        """A matrix of the first tensor's dtype; returns its row stride."""
+        if t is None:
+            self.ptrs.append(None)
+            return shape[1]
+        self._take(name, t, shape, self.dtype)
+        ld, step = t.stride()
+        if step != 1 and shape[1] > 1:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        if shape[0] <= 1 or shape[1] == 0:
+            return shape[1]
+        if ld < shape[1]:
+            raise ValueError(f"{name}: rows overlap (row stride {ld} of {shape[1]} elements)")
+        return ld
+
+    def dense(self, name, t, shape, dtype=None):
+        """A contiguous tensor, or None."""
+        if t is None:
+            self.ptrs.append(None)
+            return
+        self._take(name, t, shape, self.dtype if dtype is None else dtype)
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: must be contiguous")
+
+    def call(self, name, desc, query, workspace, stream):
+        L = lib()
+        if stream is None:
+            st = _current_stream(self.index)
+        else:
+            st = stream if isinstance(stream, int) else stream.cuda_stream
+        ref = ctypes.byref(desc)
+        if query is None:
+            _check(name, getattr(L, name)(ref, *self.ptrs, st))
+            return
+        if workspace is None:
+            need = getattr(L, query)(ref)
+            wp, wn = (None, 0) if need == 0 else _workspace(None, need, self.torch.device("cuda", self.index), stream)
+        else:
+            wp, wn = _workspace(workspace, 0, None)
+        _check(name, getattr(L, name)(ref, *self.ptrs, wp, wn, st))
+
+
+def _head_act(act):
+    try:
+        return HEAD_ACTS[act]
+    except (KeyError, TypeError):
+        raise ValueError(f"act {act!r}: one of {', '.join(HEAD_ACTS)} is required") from None
+
+
+def qhead_linear_fwd(x, w, b, res, y, z=None, act="none", workspace=None, stream=None):
+    """y = act(x w^T + b) + res; z, if given, receives x w^T + b.
+
+    x (m, k), w (n, k), y, res and z (m, n) of one dtype, b (n) float32; b and res may be None."""
+    o = _HeadOperands(x)
+    m, k = x.shape
+    n = w.shape[0]
+    ldx = o.rows("x", x, (m, k))
+    ldw = o.rows("w", w, (n, k))
+    o.dense("b", b, (n,), o.torch.float32)
+    ldr = o.rows("res", res, (m, n))
+    ldy = o.rows("y", y, (m, n))
+    o.dense("z", z, (m, n))
+    o.call("qhead_linear_fwd", HeadLinearDesc(m, k, n, ldx, ldw, ldr, ldy, o.code, _head_act(act)),
+           "qhead_linear_fwd_workspace_size", workspace, stream)
+
+
+def qhead_linear_bwd(x, w, dy, z=None, dx=None, dw=None, db=None, act="none", workspace=None, stream=None):
+    """The gradients of qhead_linear_fwd from dy = dl/dy and the z it stored (z may be None for act "none").
+
+    dx (m, k) and dw (n, k) of the dtype of x, db (n) float32; each may be None."""
+    o = _HeadOperands(x)
+    m, k = x.shape
+    n = w.shape[0]
+    ldx = o.rows("x", x, (m, k))
+    ldw = o.rows("w", w, (n, k))
+    ldy = o.rows("dy", dy, (m, n))
+    o.dense("z", z, (m, n))
+    o.dense("dx", dx, (m, k))
+    o.dense("dw", dw, (n, k))
+    o.dense("db", db, (n,), o.torch.float32)
+    o.call("qhead_linear_bwd", HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, o.code, _head_act(act)),
+           "qhead_linear_bwd_workspace_size", workspace, stream)
+
+
+def qhead_logprobs_fwd(logits, target, logp, entropy=None, lse=None, top_logp=None, top_ids=None, stats=None,
+                       temperature=1.0, workspace=None, stream=None):
+    """Log probabilities of `target` under softmax(logits / temperature), and more where a tensor for it is given.
+
+    logits (rows, vocab); target (rows) int64, negative where there is none; logp, entropy, lse
+    (rows) float32; top_logp float32 and top_ids int64 (rows, K): the K most likely tokens;
+    stats (rows, 2) float32: for qhead_logprobs_bwd."""
+    o = _HeadOperands(logits)
+    f32, i64 = o.torch.float32, o.torch.int64
+    rows, vocab = logits.shape
+    ld = o.rows("logits", logits, (rows, vocab))
+    if (top_logp is None) != (top_ids is None):
+        raise ValueError("top_logp and top_ids: both or neither")
+    top = 0 if top_logp is None else top_logp.shape[-1]
+    o.dense("target", target, (rows,), i64)
+    o.dense("logp", logp, (rows,), f32)
+    o.dense("entropy", entropy, (rows,), f32)
+    o.dense("lse", lse, (rows,), f32)
+    o.dense("top_logp", top_logp, (rows, top), f32)
+    o.dense("top_ids", top_ids, (rows, top), i64)
+    o.dense("stats", stats, (rows, 2), f32)
+    o.call("qhead_logprobs_fwd", HeadRowsDesc(rows, vocab, ld, top, o.code, temperature, 0.0),
+           "qhead_logprobs_fwd_workspace_size", workspace, stream)
+
+
+def qhead_logprobs_bwd(logits, target, stats, entropy, g, h, dlogits, temperature=1.0, stream=None):
+    """dlogits (rows, vocab) from g = dl/dlogp and h = dl/dentropy (rows, float32; h may be None)."""
+    o = _HeadOperands(logits)
+    f32 = o.torch.float32
+    rows, vocab = logits.shape
+    ld = o.rows("logits", logits, (rows, vocab))
+    o.dense("target", target, (rows,), o.torch.int64)
+    o.dense("stats", stats, (rows, 2), f32)
+    o.dense("entropy", entropy, (rows,), f32)
+    o.dense("g", g, (rows,), f32)
+    o.dense("h", h, (rows,), f32)
+    o.dense("dlogits", dlogits, (rows, vocab))
+    o.call("qhead_logprobs_bwd", HeadRowsDesc(rows, vocab, ld, 0, o.code, temperature, 0.0), None, None, stream)
+
+
+def _head_distill(logits, t_ids, t_logits, labels, temperature, alpha):
+    o = _HeadOperands(logits)
+    rows, vocab = logits.shape
+    ld = o.rows("logits", logits, (rows, vocab))
+    if (t_ids is None) != (t_logits is None):
+        raise ValueError("t_ids and t_logits: both or neither")
+    top = 0 if t_ids is None else t_ids.shape[-1]
+    o.dense("t_ids", t_ids, (rows, top), o.torch.int64)
+    o.dense("t_logits", t_logits, (rows, top))
+    o.dense("labels", labels, (rows,), o.torch.int64)
+    return o, rows, vocab, HeadRowsDesc(rows, vocab, ld, top, o.code, temperature, alpha)
+
+
+def qhead_distill_fwd(logits, t_ids, t_logits, labels, loss, stats=None, temperature=1.0, alpha=1.0, workspace=None,
+                      stream=None):
+    """loss (rows) = alpha T^2 KL(teacher's top places || softmax(logits / T)) + (1 - alpha) (cross entropy of the label).
+
+    logits (rows, vocab); t_ids int64 (negative: an empty place) and t_logits (rows, K), or both None; labels
+    (rows) int64 (negative: none), or None; loss float32; stats (rows, 4) float32: for qhead_distill_bwd."""
+    o, rows, _, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    o.dense("loss", loss, (rows,), o.torch.float32)
+    o.dense("stats", stats, (rows, 4), o.torch.float32)
+    o.call("qhead_distill_fwd", d, "qhead_distill_workspace_size", workspace, stream)
+
+
+def qhead_distill_bwd(logits, t_ids, t_logits, labels, stats, g, dlogits, temperature=1.0, alpha=1.0, stream=None):
+    """dlogits (rows, vocab) from g = dl/dloss (rows, float32) and the stats of the forward."""
+    o, rows, vocab, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    o.dense("stats", stats, (rows, 4), o.torch.float32)
+    o.dense("g", g, (rows,), o.torch.float32)
+    o.dense("dlogits", dlogits, (rows, vocab))
+    o.call("qhead_distill_bwd", d, None, None, stream)
+
+
+def qhead_distill_step(logits, t_ids, t_logits, labels, g, loss, dlogits, temperature=1.0, alpha=1.0, workspace=None,
+                       stream=None):
+    """The loss and its gradient in one call, for row weights g that are known beforehand."""
+    o, rows, vocab, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    o.dense("g", g, (rows,), o.torch.float32)
+    o.dense("loss", loss, (rows,), o.torch.float32)
+    o.dense("dlogits", dlogits, (rows, vocab))
+    o.call("qhead_distill_step", d, "qhead_distill_workspace_size", workspace, stream)

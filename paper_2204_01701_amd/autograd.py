@@ -31,6 +31,12 @@ weights), so channels_last inputs are not copied and the outputs come back
 channels_last.  X, the weights and Y share one dtype (bfloat16 or float32);
 biases are float32 or None (all three or none).  Weight gradients are
 returned in the weights' dtype, bias gradients in float32.
+
+The end of a network: ``linear_act`` is a first-order fully-connected layer with bias,
+activation and residual in one call, ``token_logprobs`` the log probabilities of
+given tokens (class labels) with the entropy and the most likely alternatives,
+``distill_loss`` the loss against a teacher's top logits, mixed with the label's
+cross entropy.  They take leading dimensions of any kind.
 """
 from __future__ import annotations
 
@@ -39,9 +45,12 @@ import torch
 from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL_NEURON_T24, conv_desc, epilogue,
                linear_desc, qlayer_conv2d_bwd_data, qlayer_conv2d_bwd_data_ex, qlayer_conv2d_bwd_relu,
                qlayer_conv2d_bwd_weight, qlayer_conv2d_fwd, qlayer_conv2d_fwd_ex,
-               qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex)
+               qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex,
+               qhead_distill_bwd, qhead_distill_fwd, qhead_linear_bwd, qhead_linear_fwd, qhead_logprobs_bwd,
+               qhead_logprobs_fwd)
 
-__all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction"]
+__all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction", "linear_act", "token_logprobs",
+           "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction"]
 
 
 def _qdtype(t: torch.Tensor) -> int:
@@ -244,3 +253,144 @@ def quad_linear(x, wa, wb=None, wc=None, ba=None, bb=None, bc=None, recompute=Fa
                 relu=False):
     """Quadratic fully-connected layer: x (B, I), weights (O, I)."""
     return QuadLinearFunction.apply(x, wa, wb, wc, ba, bb, bc, recompute, neuron, relu)
+
+
+# --- the end of a network -----------------------------------------------------------
+
+def _matrix(t):
+    """(..., c) as a matrix whose rows are contiguous and do not overlap (a view where there is one)."""
+    t = t.reshape(-1, t.shape[-1]) if t.numel() else t.new_empty((t.shape[:-1].numel(), t.shape[-1]))
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        t = t.contiguous()
+    return t
+
+
+class LinearActFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, b, res, act):
+        _same_device(x, w, b, res)
+        if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+            raise ValueError(f"x (..., in) and w (out, in) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
+        if b is not None and b.shape != w.shape[:1]:
+            raise ValueError(f"the bias must have {w.shape[0]} elements")
+        shape = x.shape[:-1] + w.shape[:1]
+        if res is not None and res.shape != shape:
+            raise ValueError(f"the residual must have the output's shape {tuple(shape)}, got {tuple(res.shape)}")
+        xm, wm = _matrix(x), _matrix(w.to(x.dtype))
+        y = torch.empty((xm.shape[0], w.shape[0]), device=x.device, dtype=x.dtype)
+        z = torch.empty_like(y) if act != "none" and any(ctx.needs_input_grad[:3]) else None
+        qhead_linear_fwd(xm, wm, b.contiguous().float() if b is not None else None,
+                         _matrix(res.to(x.dtype)) if res is not None else None, y, z, act=act)
+        ctx.save_for_backward(xm, wm, z)
+        ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
+        ctx.bdtype = b.dtype if b is not None else None
+        ctx.rdtype = res.dtype if res is not None else None
+        return y.view(shape)
+
+    @staticmethod
+    def backward(ctx, gy):
+        x, w, z = ctx.saved_tensors
+        gx, gw, gb, gr = ctx.needs_input_grad[:4]
+        dx = torch.empty(x.shape, device=x.device, dtype=x.dtype) if gx else None
+        dw = torch.empty(w.shape, device=x.device, dtype=x.dtype) if gw else None
+        db = torch.empty(w.shape[0], device=x.device) if gb else None
+        if gx or gw or gb:
+            qhead_linear_bwd(x, w, _matrix(gy), z, dx, dw, db, act=ctx.act)
+        return (dx.view(ctx.xshape) if gx else None, dw.to(ctx.wdtype) if gw else None,
+                db.to(ctx.bdtype) if gb else None, gy.to(ctx.rdtype) if gr else None, None)
+
+
+def linear_act(x, weight, bias=None, residual=None, act="none"):
+    """act(x weight^T + bias) + residual, with x (..., in), weight (out, in), bias (out), residual (..., out).
+
+    act: "none", "relu", "gelu" (error function), "gelu_tanh" or "silu".  The product, the
+    epilogue and the gradients run in the library's kernels in the dtype of x; the
+    pre-activation is kept for the backward in that dtype where there is an activation."""
+    return LinearActFunction.apply(x, weight, bias, residual, act)
+
+
+class TokenLogprobsFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, target, temperature, top):
+        ctx.set_materialize_grads(False)
+        _same_device(logits, target)
+        z = _matrix(logits)
+        rows, lead = z.shape[0], logits.shape[:-1]
+        if target.shape != lead or target.dtype != torch.int64:
+            raise ValueError(f"target must be int64 of shape {tuple(lead)}, got {target.dtype} {tuple(target.shape)}")
+        t = target.reshape(rows).contiguous()
+        logp, entropy = torch.empty((2, rows), device=z.device).unbind(0)
+        stats = torch.empty((rows, 2), device=z.device) if ctx.needs_input_grad[0] else None
+        top_logp = torch.empty((rows, top), device=z.device) if top else None
+        top_ids = torch.empty((rows, top), device=z.device, dtype=torch.int64) if top else None
+        qhead_logprobs_fwd(z, t, logp, entropy, None, top_logp, top_ids, stats, temperature=temperature)
+        ctx.temperature, ctx.shape = temperature, logits.shape
+        ctx.save_for_backward(z, t, stats, entropy)
+        out = logp.view(lead), entropy.view(lead)
+        if not top:
+            return out
+        more = top_logp.view(lead + (top,)), top_ids.view(lead + (top,))
+        ctx.mark_non_differentiable(*more)
+        return out + more
+
+    @staticmethod
+    def backward(ctx, g, h, *_):
+        z, t, stats, entropy = ctx.saved_tensors
+        if g is None and h is None:
+            return None, None, None, None
+        rows = z.shape[0]
+        g = g.reshape(rows).contiguous().float() if g is not None else torch.zeros(rows, device=z.device)
+        h = h.reshape(rows).contiguous().float() if h is not None else None
+        dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
+        qhead_logprobs_bwd(z, t, stats, entropy, g, h, dz, temperature=ctx.temperature)
+        return dz.view(ctx.shape), None, None, None
+
+
+def token_logprobs(logits, target, temperature=1.0, top=0):
+    """(log probability of `target`, entropy) under softmax(logits / temperature), float32.
+
+    logits (..., vocab); target (...) int64, negative where there is none (log probability 0, no
+    gradient from it).  top > 0 adds (top_logp, top_ids) of shape (..., top): the most likely
+    tokens, equal logits by rising id (no gradient passes through them)."""
+    return TokenLogprobsFunction.apply(logits, target, temperature, top)
+
+
+class DistillLossFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, t_ids, t_logits, labels, temperature, alpha):
+        _same_device(logits, t_ids, t_logits, labels)
+        z = _matrix(logits)
+        rows, lead = z.shape[0], logits.shape[:-1]
+        for name, t in (("teacher_ids", t_ids), ("teacher_logits", t_logits)):
+            if t is not None and t.shape[:-1] != lead:
+                raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit logits of shape {tuple(logits.shape)}")
+        if labels is not None and labels.shape != lead:
+            raise ValueError(f"labels: shape {tuple(labels.shape)}, expected {tuple(lead)}")
+        ids = t_ids.reshape(rows, t_ids.shape[-1]).contiguous() if t_ids is not None else None
+        tz = t_logits.reshape(rows, t_logits.shape[-1]).to(z.dtype).contiguous() if t_logits is not None else None
+        y = labels.reshape(rows).contiguous() if labels is not None else None
+        loss = torch.empty(rows, device=z.device)
+        stats = torch.empty((rows, 4), device=z.device) if ctx.needs_input_grad[0] else None
+        qhead_distill_fwd(z, ids, tz, y, loss, stats, temperature=temperature, alpha=alpha)
+        ctx.save_for_backward(z, ids, tz, y, stats)
+        ctx.how, ctx.shape = dict(temperature=temperature, alpha=alpha), logits.shape
+        return loss.view(lead)
+
+    @staticmethod
+    def backward(ctx, g):
+        z, ids, tz, y, stats = ctx.saved_tensors
+        dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
+        qhead_distill_bwd(z, ids, tz, y, stats, g.reshape(z.shape[0]).contiguous().float(), dz, **ctx.how)
+        return dz.view(ctx.shape), None, None, None, None, None
+
+
+def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1.0, alpha=1.0):
+    """Per-row loss of a student against a teacher's top logits, float32:
+
+        alpha T^2 KL(q || softmax(logits / T)) + (1 - alpha) cross_entropy(logits, label),
+
+    q the softmax of teacher_logits / T over the row's places.  logits (..., vocab); teacher_ids int64
+    (negative: an empty place) and teacher_logits (..., K), or both None; labels (...) int64, negative
+    where a row has none, or None.  The gradient goes to the logits."""
+    return DistillLossFunction.apply(logits, teacher_ids, teacher_logits, labels, temperature, alpha)

@@ -1,0 +1,776 @@
+// qhead_rows.h -- kernels over rows of logits (include/qhead.h): softmax
+// statistics with the entropy and the K largest values, and the distillation
+// loss; both with their gradients.
+//
+// Mathematics.  With c = log2(e) / T, m the largest logit of what was read and
+// d_j = (z_j - m) c, a row is reduced to
+//     S = sum 2^d_j,     D = sum 2^d_j d_j,
+// and two parts of a row are joined by shifting both to the common maximum:
+// S -> 2^s S, D -> 2^s (D + s S) for s = (m_old - m_new) c.  Then
+//     log p_j = ln2 d_j - ln S,   entropy = ln S - ln2 D / S.
+// d is formed as a difference, then a product: folding m c into one constant
+// would overflow for a row at the type's lowest value, whose softmax is uniform.
+// m starts at the lowest finite value, so that -inf logits alone leave S = 0 (the
+// mark of an empty row) and no difference of infinities is formed for them; NaN
+// and +inf make S NaN by themselves.
+//
+// A row is read as 16-byte vectors from its first element, whatever its
+// alignment (global loads need that of a dword at most; a row of an odd
+// vocabulary starts anywhere), and its last V mod (16 / size) elements one by one.
+#pragma once
+
+#include "qdevice.h"
+
+namespace ql {
+
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
+
+constexpr float kHeadLowest = -3.402823466e+38f;
+constexpr float kHeadFloor = -1e30f;  // stands for -inf in products with a 0 from the same exponent
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kHeadTopMax = 128;
+
+__device__ __forceinline__ float head_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// --- one row as 16-byte vectors ------------------------------------------------
+template <typename T> struct HeadRow {
+    static constexpr int VEC = Elem<T>::VEC;
+    const T *p;
+    int V, nfull, nvec;  // elements, whole vectors, vectors with the partial one
+    __device__ __forceinline__ HeadRow(const T *row, int v) : p(row), V(v), nfull(v / VEC), nvec((v + VEC - 1) / VEC) {}
+    __device__ __forceinline__ v4u load(int j) const { return *reinterpret_cast<const v4u_any *>(p + (size_t)j * VEC); }
+    // The vector behind the whole ones, -inf past the row's end.
+    __device__ __forceinline__ v4u partial() const {
+        float f[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const size_t i = (size_t)nfull * VEC + e;
+            f[e] = i < (size_t)V ? to_f32<T>(p[i]) : -__builtin_inff();
+        }
+        return vpack<T>(f);
+    }
+};
+
+template <typename T> __device__ __forceinline__ v4u head_neg_inf() {
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return v4u{w, w, w, w};
+}
+
+// r[u] = vector first + u * step + (this thread), -inf from `end` on.
+template <typename T, int U>
+__device__ __forceinline__ void head_load(const HeadRow<T> &row, int first, int step, int tid, int end, v4u (&r)[U]) {
+    const int whole = min(end, row.nfull);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int j = first + u * step + tid;
+        r[u] = head_neg_inf<T>();
+        if (j < whole) r[u] = row.load(j);
+    }
+    if (end > row.nfull && first + U * step > row.nfull) {
+        const v4u t = row.partial();
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u * step + tid == row.nfull) r[u] = t;
+    }
+}
+
+// z / T - m / T: halved around the difference, which would overflow between values at both
+// ends of the type (their quotient by T need not).
+__device__ __forceinline__ float head_scaled_diff(float z, float m, float inv_t) {
+    return (0.5f * z - 0.5f * m) * inv_t * 2.0f;
+}
+
+// --- running sums ----------------------------------------------------------------
+// s1 is the sum at T = 1 beside the one at T (distillation with labels), d the
+// entropy's; each kernel keeps those it needs.
+struct HeadSums {
+    float m, s, d, s1;
+};
+__device__ __forceinline__ HeadSums head_start() { return {kHeadLowest, 0.0f, 0.0f, 0.0f}; }
+
+// Shift `a` to the maximum m >= a.m.
+template <bool ENT, bool TWO>
+__device__ __forceinline__ void head_shift(HeadSums &a, float m, float c) {
+    const float x = fmaxf((a.m - m) * c, kHeadFloor), f = head_exp2(x);
+    if constexpr (ENT) a.d = f * (a.d + x * a.s);
+    a.s *= f;
+    if constexpr (TWO) a.s1 *= head_exp2((a.m - m) * kLog2e);
+    a.m = m;
+}
+
+template <bool ENT, bool TWO>
+__device__ __forceinline__ void head_join(HeadSums &a, HeadSums b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    head_shift<ENT, TWO>(a, m, c);
+    head_shift<ENT, TWO>(b, m, c);
+    a.s += b.s;
+    if constexpr (ENT) a.d += b.d;
+    if constexpr (TWO) a.s1 += b.s1;
+}
+
+// The sums of U vectors held in registers; returns their maximum.
+template <typename T, int U, bool ENT, bool TWO>
+__device__ __forceinline__ float head_accumulate(HeadSums &a, const v4u (&r)[U], float c) {
+    constexpr int VEC = Elem<T>::VEC;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) top = fmaxf(top, vget<T>(r[u], e));
+    if (top > a.m) head_shift<ENT, TWO>(a, top, c);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float x = vget<T>(r[u], e) - a.m, d = x * c, p = head_exp2(d);
+            a.s += p;
+            if constexpr (ENT) a.d += p * fmaxf(d, kHeadFloor);
+            if constexpr (TWO) a.s1 += head_exp2(x * kLog2e);
+        }
+    return top;
+}
+
+template <bool ENT, bool TWO> __device__ __forceinline__ HeadSums head_wave_join(HeadSums a, float c) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        HeadSums b = head_start();
+        b.m = __shfl_xor(a.m, o);
+        b.s = __shfl_xor(a.s, o);
+        if constexpr (ENT) b.d = __shfl_xor(a.d, o);
+        if constexpr (TWO) b.s1 = __shfl_xor(a.s1, o);
+        head_join<ENT, TWO>(a, b, c);
+    }
+    return a;
+}
+
+// Join of at most 64 parts of a row, in every wave.
+constexpr int kHeadMaxSplits = 64;
+template <bool ENT, bool TWO>
+__device__ __forceinline__ HeadSums head_join_parts(const HeadSums *part, int n, float c) {
+    HeadSums a = head_start();
+    const int lane = threadIdx.x & 63;
+    if (lane < n) a = part[lane];
+    return head_wave_join<ENT, TWO>(a, c);
+}
+
+// Join over the workgroup, in a fixed order; every thread gets the result.
+template <int TH, bool ENT, bool TWO>
+__device__ __forceinline__ HeadSums head_block_join(HeadSums a, float c, HeadSums *lds) {
+    a = head_wave_join<ENT, TWO>(a, c);
+    if constexpr (TH == 64) return a;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = lds[0];
+#pragma unroll
+    for (int w = 1; w < TH / 64; ++w) head_join<ENT, TWO>(a, lds[w], c);
+    return a;
+}
+
+template <int TH> __device__ __forceinline__ float head_block_max(float v, float *lds) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    if constexpr (TH == 64) return v;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < TH / 64; ++w) v = fmaxf(v, lds[w]);
+    return v;
+}
+
+template <int TH> __device__ __forceinline__ float head_block_sum(float v, float *lds) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    if constexpr (TH == 64) return v;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < TH / 64; ++w) v += lds[w];
+    return v;
+}
+
+// --- the K largest ------------------------------------------------------------------
+// An element's key: its value's bits in an order that unsigned integers share, over the
+// complement of its index, so that equal values rank by the lower index and no two
+// keys are equal.  -0 counts as 0.  NaN ranks behind every value; 0 is no element.
+constexpr uint32_t kKeyNaN = 1u, kKeyNegInf = 0x007fffffu;
+
+__device__ __forceinline__ uint32_t head_key(float z) {
+    if (!(z == z)) return kKeyNaN;
+    const uint32_t u = __float_as_uint(z + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float head_unkey(uint32_t k) {
+    if (k < kKeyNegInf) return __builtin_nanf("");
+    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ __forceinline__ uint64_t head_key64(uint32_t k, int i) { return (uint64_t)k << 32 | (uint32_t)~i; }
+
+constexpr int kHeadCap = 1024;  // candidates a workgroup can hold
+
+template <int TH> struct HeadTopLds {
+    uint64_t buf[kHeadCap];      // candidates; after head_rank the best ones in front, in order
+    uint64_t best[kHeadTopMax];
+    uint32_t keys[TH];
+    int wave[TH / 64];
+    int n;                       // candidates held
+    uint32_t pick;
+};
+
+// Ranks the n candidates by counting the larger ones: buf[0 .. min(n, K)) is then
+// the best in order.  n^2 / TH steps, without a barrier among them.
+template <int TH> __device__ __forceinline__ void head_rank(HeadTopLds<TH> &s, int K) {
+    __syncthreads();
+    const int n = s.n;
+    for (int i = threadIdx.x; i < n; i += TH) {
+        const uint64_t k = s.buf[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += s.buf[j] > k ? 1 : 0;
+        if (above < K) s.best[above] = k;
+    }
+    __syncthreads();
+    const int kept = min(n, K);
+    for (int i = threadIdx.x; i < kept; i += TH) s.buf[i] = s.best[i];
+    if (threadIdx.x == 0) s.n = kept;
+    __syncthreads();
+}
+
+// Exclusive prefix of v over the workgroup's threads, and the total.
+template <int TH> __device__ __forceinline__ int head_prefix(int v, int &total, int *lds) {
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if ((int)(threadIdx.x & 63) >= o) x += y;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < TH / 64; ++w) {
+        if (w < (int)(threadIdx.x >> 6)) before += lds[w];
+        total += lds[w];
+    }
+    return before + x - v;
+}
+
+// Elements of r whose key is at least kmin (`count` of them in the thread), as a bit
+// mask; only elements below `limit` count.
+template <typename T, int U>
+__device__ __forceinline__ uint64_t head_mask(const v4u (&r)[U], uint32_t kmin, int first, int step, int tid, int limit,
+                                              bool edge) {
+    constexpr int VEC = Elem<T>::VEC;
+    uint64_t mask = 0;
+    if (kmin < kKeyNegInf) {  // NaN may be needed: decide by the key itself
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                mask |= (uint64_t)(head_key(vget<T>(r[u], e)) >= kmin ? 1 : 0) << (u * VEC + e);
+    } else {
+        const float f = head_unkey(kmin);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            uint32_t part = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) part |= vget<T>(r[u], e) >= f ? 1u << e : 0u;
+            mask |= (uint64_t)part << (u * VEC);
+        }
+    }
+    if (edge) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long left = (long long)limit - (long long)(first + u * step + tid) * VEC;
+            if (left < VEC) {
+                const uint32_t keep = left > 0 ? (1u << (int)left) - 1 : 0u;
+                mask &= ~((uint64_t)(((1u << VEC) - 1) & ~keep) << (u * VEC));
+            }
+        }
+    }
+    return mask;
+}
+
+// The chunk of a row held in registers joins the candidates.
+// `least`: keys below it cannot be among the K largest (0: nothing is known yet);
+// returns the same for the chunks behind.  top: the thread's largest value.
+template <typename T, int TH, int U>
+__device__ __forceinline__ uint32_t head_top_chunk(HeadTopLds<TH> &s, const T *row, const v4u (&r)[U], float top, int K,
+                                                   int first, int end, int limit, uint32_t least) {
+    constexpr int VEC = Elem<T>::VEC;
+    const int tid = threadIdx.x;
+    const bool edge = first + U * TH > limit / VEC || first + U * TH > end;
+    const int stop = (int)min((long long)limit, (long long)end * VEC);  // elements of this call's vectors end here
+    if (least == 0 && K <= TH) {
+        // The K-th largest of the threads' own maxima bounds the K-th largest from below.
+        // (a maximum of -inf may stand for nothing but NaN: it vouches for no more than that)
+        const bool any = (long long)(first + tid) * VEC < stop;
+        const uint32_t k = !any ? 0u : top > -__builtin_inff() ? head_key(top) : kKeyNaN;
+        if (tid == 0) s.pick = 0;
+        s.keys[tid] = k;
+        __syncthreads();
+        int above = 0;
+        for (int j = 0; j < TH; ++j) {
+            const uint32_t o = s.keys[j];
+            above += o > k || (o == k && j < tid) ? 1 : 0;
+        }
+        if (above == K - 1) s.pick = k;
+        __syncthreads();
+        least = s.pick;
+    }
+    const uint64_t mask = head_mask<T, U>(r, least, first, TH, tid, stop, edge);
+    int total;
+    const int held = s.n;
+    int at = held + head_prefix<TH>(__popcll(mask), total, s.wave);  // (its barriers order the read of s.n before the write below)
+    if (held + total <= kHeadCap) {
+        for (uint64_t left = mask; left; left &= left - 1) {
+            const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
+            s.buf[at++] = head_key64(head_key(to_f32<T>(row[i])), i);
+        }
+        if (tid == 0) s.n = held + total;
+    } else {
+        // Too many (equal values, mostly): find the chunk's K-th largest key by bisection, take
+        // what lies above it, then the first ones equal to it in the order of their indices.
+        auto count = [&](uint32_t k) {
+            int t;
+            head_prefix<TH>(__popcll(head_mask<T, U>(r, k, first, TH, tid, stop, edge)), t, s.wave);
+            return t;
+        };
+        uint32_t lo = least, hi = 0xffffffffu;  // count(lo) >= K > count(hi)
+        if (count(lo + 1) < K) hi = lo + 1;     // rows of one value, and, in two more counts, masked ones
+        if (hi - lo > 1 && lo < kKeyNegInf && count(kKeyNegInf + 1) < K) hi = kKeyNegInf + 1;
+        if (hi - lo > 1 && hi == kKeyNegInf + 1 && count(kKeyNegInf) >= K) lo = kKeyNegInf;
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (count(mid) >= K) lo = mid;
+            else hi = mid;
+        }
+        const uint64_t over = head_mask<T, U>(r, hi, first, TH, tid, stop, edge);
+        const uint64_t equal = head_mask<T, U>(r, lo, first, TH, tid, stop, edge) & ~over;
+        at = held + head_prefix<TH>(__popcll(over), total, s.wave);
+        for (uint64_t left = over; left; left &= left - 1) {
+            const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
+            s.buf[at++] = head_key64(head_key(to_f32<T>(row[i])), i);
+        }
+        int have = held + total, want = K - total;
+        for (int u = 0; u < U && want > 0; ++u) {  // (vectors u of all threads precede vectors u + 1)
+            uint64_t mine = equal >> (u * VEC) & ((1u << VEC) - 1);
+            const int before = head_prefix<TH>(__popcll(mine), total, s.wave);
+            for (int q = before; mine && q < want; mine &= mine - 1, ++q) {
+                const int b = __builtin_ctzll(mine);
+                s.buf[have + q] = head_key64(lo, (first + u * TH + tid) * VEC + b);
+            }
+            have += min(total, want);
+            want -= min(total, want);
+        }
+        if (tid == 0) s.n = have;
+    }
+    head_rank<TH>(s, K);
+    // later elements have higher indices: only larger values can displace the K-th
+    return s.n == K ? (uint32_t)(s.buf[K - 1] >> 32) + 1 : 0u;
+}
+
+struct HeadLogprobArgs {
+    const void *z;
+    long long ld;
+    int V, K, splits, per;  // per: vectors of a split
+    float c, inv_t;
+    const int64_t *target;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+    float *stats;
+    HeadSums *part;      // rows x splits
+    uint64_t *part_top;  // rows x splits x K
+};
+
+// What a row's statistics say of it (whole workgroup; s: the best K in front of buf).
+template <typename T, int TH>
+__device__ __forceinline__ void head_logprobs_finish(const HeadLogprobArgs &a, long long row, const HeadSums &t,
+                                                     const uint64_t *best) {
+    const T *z = static_cast<const T *>(a.z) + row * a.ld;
+    const float ls = logf(t.s);  // -inf for an empty row
+    const bool empty = t.s == 0.0f;
+    if (threadIdx.x == 0) {
+        const int64_t g = a.target[row];
+        float lp = 0.0f;
+        if (g >= a.V) lp = __builtin_nanf("");
+        else if (g >= 0) lp = empty ? -__builtin_inff() : head_scaled_diff(to_f32<T>(z[g]), t.m, a.inv_t) - ls;
+        a.logp[row] = lp;
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - kLn2 * (t.d / t.s);
+        if (a.lse) a.lse[row] = empty ? -__builtin_inff() : t.m * a.inv_t + ls;
+        if (a.stats) {
+            a.stats[2 * row] = t.m;
+            a.stats[2 * row + 1] = t.s;
+        }
+    }
+    for (int k = threadIdx.x; k < a.K; k += TH) {
+        const uint64_t key = best[k];
+        a.top_logp[row * a.K + k] =
+            empty ? -__builtin_inff() : head_scaled_diff(head_unkey((uint32_t)(key >> 32)), t.m, a.inv_t) - ls;
+        a.top_ids[row * a.K + k] = (int64_t)(uint32_t)~(uint32_t)key;
+    }
+}
+
+template <typename T, int TH, int U, bool TOP>
+__global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
+    __shared__ HeadSums sums[TH / 64];
+    __shared__ HeadTopLds<TOP ? TH : 64> top;
+    const long long row = blockIdx.x / a.splits;
+    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
+    const int end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
+    HeadSums t = head_start();
+    uint32_t least = 0;
+    if constexpr (TOP) {
+        if (tid == 0) top.n = 0;
+        __syncthreads();
+    }
+    for (int first = sp * a.per; first < end; first += U * TH) {
+        v4u r[U];
+        head_load<T, U>(z, first, TH, tid, end, r);
+        const float most = head_accumulate<T, U, true, false>(t, r, a.c);
+        if constexpr (TOP) least = head_top_chunk<T, TH, U>(top, z.p, r, most, a.K, first, end, a.V, least);
+    }
+    t = head_block_join<TH, true, false>(t, a.c, sums);
+    const uint64_t *best = nullptr;
+    if constexpr (TOP) best = top.buf;
+    if (a.splits == 1) {
+        head_logprobs_finish<T, TH>(a, row, t, best);
+        return;
+    }
+    const long long at = row * a.splits + sp;
+    if (tid == 0) a.part[at] = t;
+    if constexpr (TOP)
+        for (int k = tid; k < a.K; k += TH) a.part_top[at * a.K + k] = k < top.n ? best[k] : 0;
+}
+
+// Joins the parts of a row: the K-th key of any part bounds the row's K-th from
+// below, so only what reaches the largest of those is ranked.
+template <typename T>
+__global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
+    extern __shared__ uint64_t cand[];  // splits x K
+    __shared__ uint64_t best[kHeadTopMax];
+    __shared__ int wave[4];
+    const long long row = blockIdx.x;
+    const int tid = threadIdx.x, K = a.K;
+    const HeadSums t = head_join_parts<true, false>(a.part + row * a.splits, a.splits, a.c);
+    if (K) {
+        const uint64_t *in = a.part_top + row * a.splits * K;
+        uint64_t least = 0;
+        for (int i = 0; i < a.splits; ++i) least = max(least, in[i * K + K - 1]);
+        int n = 0;
+        for (int i0 = 0; i0 < a.splits * K; i0 += 256) {
+            const uint64_t k = i0 + tid < a.splits * K ? in[i0 + tid] : 0;
+            int total;
+            const int at = head_prefix<256>(k != 0 && k >= least ? 1 : 0, total, wave);
+            if (k != 0 && k >= least) cand[n + at] = k;
+            n += total;
+        }
+        __syncthreads();
+        for (int i = tid; i < n; i += 256) {
+            const uint64_t k = cand[i];
+            int above = 0;
+            for (int j = 0; j < n; ++j) above += cand[j] > k ? 1 : 0;
+            if (above < K) best[above] = k;
+        }
+        __syncthreads();
+    }
+    head_logprobs_finish<T, 256>(a, row, t, best);
+}
+
+// --- gradients --------------------------------------------------------------------------
+// dz_j = A p_j + B p1_j + C p_j log p_j + (what the row's few ids add), with the
+// probabilities formed from the row's m, S, S1.
+struct HeadGrad {
+    float m, c, a, b, e, is, is1, ls;
+    bool zero;  // the row has no term: its gradient is 0 whatever the logits hold
+};
+
+template <bool ENT, bool TWO> __device__ __forceinline__ float head_grad_at(const HeadGrad &g, float z) {
+    const float x = z - g.m, d = x * g.c, p = head_exp2(d) * g.is;
+    float v = g.a;
+    if constexpr (ENT) v += g.e * fmaxf(kLn2 * d - g.ls, kHeadFloor);
+    v *= p;
+    if constexpr (TWO) v += g.b * (head_exp2(x * kLog2e) * g.is1);
+    return v;
+}
+
+template <typename T, int U, bool ENT, bool TWO>
+__device__ __forceinline__ void head_grad_store(const HeadGrad &g, const HeadRow<T> &z, T *dz, const v4u (&r)[U], int first,
+                                                int step, int tid, int end) {
+    constexpr int VEC = Elem<T>::VEC;
+    const int whole = min(end, z.nfull);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int j = first + u * step + tid;
+        if (j >= end) continue;
+        float f[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = g.zero ? 0.0f : head_grad_at<ENT, TWO>(g, vget<T>(r[u], e));
+        T *o = dz + (size_t)j * VEC;
+        if (j < whole) {
+            *reinterpret_cast<v4u_any *>(o) = vpack<T>(f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (j * (long long)VEC + e < z.V) o[e] = from_f32<T>(f[e]);
+        }
+    }
+}
+
+struct HeadLogprobGradArgs {
+    const void *z;
+    long long ld;
+    int V, splits, per;
+    float c, inv_t;
+    const int64_t *target;
+    const float *stats, *entropy, *g, *h;
+    void *dz;
+};
+
+template <typename T, int TH, int U, bool ENT>
+__global__ __launch_bounds__(TH) void qhead_logprobs_grad_kernel(HeadLogprobGradArgs a) {
+    const long long row = blockIdx.x / a.splits;
+    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
+    T *dz = static_cast<T *>(a.dz) + row * a.V;
+    const int begin = sp * a.per, end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
+    const int64_t t = a.target[row];
+    const bool given = t >= 0 && t < a.V;
+    const float up = given ? a.g[row] : 0.0f, h = ENT ? a.h[row] : 0.0f, s = a.stats[2 * row + 1];
+    HeadGrad g{};
+    g.m = a.stats[2 * row];
+    g.c = a.c;
+    g.is = s == 0.0f ? 0.0f : 1.0f / s;
+    g.ls = s == 0.0f ? 0.0f : logf(s);
+    g.e = -h * a.inv_t;
+    g.a = -up * a.inv_t + (ENT ? g.e * a.entropy[row] : 0.0f);
+    g.zero = (up == 0.0f && h == 0.0f) || s == 0.0f;
+    const long long lo = (long long)begin * HeadRow<T>::VEC, hi = min((long long)a.V, (long long)end * HeadRow<T>::VEC);
+    const bool mine = tid == 0 && given && t >= lo && t < hi;
+    float zt = 0.0f;
+    if (mine) zt = to_f32<T>(z.p[t]);  // (before the stores: the gradient may lie over the logits)
+    for (int first = begin; first < end; first += U * TH) {
+        v4u r[U];
+        head_load<T, U>(z, first, TH, tid, end, r);
+        head_grad_store<T, U, ENT, false>(g, z, dz, r, first, TH, tid, end);
+    }
+    __syncthreads();
+    if (mine && !g.zero) dz[t] = from_f32<T>(head_grad_at<ENT, false>(g, zt) + up * a.inv_t);
+}
+
+// --- distillation ------------------------------------------------------------------------
+struct HeadDistillArgs {
+    const void *z;
+    long long ld;
+    int V, K, splits, per;
+    float c, temp, inv_t, alpha;
+    const int64_t *ids;
+    const void *tz;
+    const int64_t *label;
+    const float *g;
+    float *loss, *stats;  // stats: rows x 4, (m, S, S1, 0)
+    HeadSums *part;
+    void *dz;
+};
+
+// The few places of a row whose gradient has more than the probabilities: the teacher's
+// (place k on thread k) and the label (on thread K).
+struct HeadPlaces {
+    float q, zt, logq;  // the place's probability, its student logit and log q
+    int id;             // -1: none
+    float has_q, has_l; // the row has a teacher's term, a label's (0 or 1)
+    bool wrong;         // an id or label past the vocabulary
+};
+
+template <int TH> struct HeadDistillLds {
+    HeadSums sums[TH / 64];
+    float red[TH / 64];
+    float q[kHeadTopMax + 1];
+    int id[kHeadTopMax + 1];
+};
+
+template <typename T, int TH>
+__device__ __forceinline__ HeadPlaces head_places(const HeadDistillArgs &a, long long row, const T *z, HeadDistillLds<TH> &s) {
+    const int tid = threadIdx.x;
+    HeadPlaces p{0.0f, 0.0f, 0.0f, -1, 0.0f, 0.0f, false};
+    float t = -__builtin_inff();
+    bool wrong = false, there = false;
+    if (tid < a.K && a.alpha != 0.0f) {
+        const int64_t id = a.ids[row * a.K + tid];
+        if (id >= 0) {
+            t = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + tid]);
+            there = true;
+            if (id < a.V) p.id = (int)id;
+            else wrong = true;
+        }
+    } else if (tid == a.K && a.label && a.alpha != 1.0f) {
+        const int64_t id = a.label[row];
+        if (id >= 0 && id < a.V) p.id = (int)id;
+        wrong = id >= a.V;
+    }
+    if (p.id >= 0) p.zt = to_f32<T>(z[p.id]);
+    const float most = head_block_max<TH>(t, s.red);
+    const float x = (t - most) * a.inv_t, e = there && t != -__builtin_inff() ? expf(x) : 0.0f;
+    const float sum = head_block_sum<TH>(e, s.red);
+    if (tid < a.K) {
+        p.q = sum != 0.0f ? e / sum : 0.0f;  // (no place, or all of probability 0: the row has no teacher's term)
+        p.logq = x - logf(sum);
+    }
+    p.has_q = sum != 0.0f ? 1.0f : 0.0f;
+    p.wrong = head_block_max<TH>(wrong ? 1.0f : 0.0f, s.red) != 0.0f;
+    if (tid <= a.K) {
+        s.q[tid] = p.q;
+        s.id[tid] = p.id;
+    }
+    __syncthreads();
+    p.has_l = s.id[a.K] >= 0 ? 1.0f : 0.0f;
+    return p;
+}
+
+// The row's loss, on every thread.
+template <int TH>
+__device__ __forceinline__ float head_distill_loss(const HeadDistillArgs &a, const HeadPlaces &p, const HeadSums &t,
+                                                   HeadDistillLds<TH> &s) {
+    const int tid = threadIdx.x;
+    float v = 0.0f;
+    if (tid < a.K) {
+        const float lp = t.s == 0.0f ? -__builtin_inff() : head_scaled_diff(p.zt, t.m, a.inv_t) - logf(t.s);
+        if (p.q != 0.0f && p.id >= 0) v = a.alpha * a.temp * a.temp * p.q * (p.logq - lp);
+    } else if (tid == a.K && p.id >= 0) {
+        v = t.s1 == 0.0f ? __builtin_inff() : (1.0f - a.alpha) * (logf(t.s1) - head_scaled_diff(p.zt, t.m, 1.0f));
+    }
+    v = head_block_sum<TH>(v, s.red);
+    return p.wrong ? __builtin_nanf("") : v;
+}
+
+__device__ __forceinline__ HeadGrad head_distill_coef(const HeadDistillArgs &a, const HeadPlaces &p, float m, float s,
+                                                      float s1, float up) {
+    HeadGrad g{};
+    g.m = m;
+    g.c = a.c;
+    g.is = s == 0.0f ? 0.0f : 1.0f / s;
+    g.is1 = s1 == 0.0f ? 0.0f : 1.0f / s1;
+    g.a = up * a.alpha * a.temp * p.has_q;
+    g.b = up * (1.0f - a.alpha) * p.has_l;
+    g.zero = up == 0.0f || (p.has_q == 0.0f && p.has_l == 0.0f);
+    return g;
+}
+
+// The places' own gradients, after the stream has written the row: each id is written by the first of the
+// places that have it, with the sum of their parts.
+template <typename T, int TH, bool TWO>
+__device__ __forceinline__ void head_place_grads(const HeadDistillArgs &a, const HeadGrad &g, const HeadPlaces &p, float up,
+                                                 T *dz, long long lo, long long hi, const HeadDistillLds<TH> &s) {
+    __syncthreads();
+    const int tid = threadIdx.x;
+    if (tid > a.K || p.id < lo || p.id >= hi || g.zero) return;
+    float q = 0.0f;
+    bool first = true;
+    for (int k = 0; k < a.K; ++k)
+        if (s.id[k] == p.id) {
+            first = first && k >= tid;
+            q += s.q[k];
+        }
+    if (!first) return;
+    float v = head_grad_at<false, TWO>(g, p.zt) - up * a.alpha * a.temp * q;
+    if (s.id[a.K] == p.id) v -= up * (1.0f - a.alpha);
+    dz[p.id] = from_f32<T>(v);
+}
+
+// One workgroup per row: the statistics, the loss and, for GRAD, the gradient from a second read
+// of the row, which the caches still hold.
+template <typename T, int TH, int U, bool TWO, bool GRAD>
+__global__ __launch_bounds__(TH) void qhead_distill_row_kernel(HeadDistillArgs a) {
+    __shared__ HeadDistillLds<TH> s;
+    const long long row = blockIdx.x;
+    const int tid = threadIdx.x;
+    const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
+    const HeadPlaces p = head_places<T, TH>(a, row, z.p, s);
+    HeadSums t = head_start();
+    for (int first = 0; first < z.nvec; first += U * TH) {
+        v4u r[U];
+        head_load<T, U>(z, first, TH, tid, z.nvec, r);
+        head_accumulate<T, U, false, TWO>(t, r, a.c);
+    }
+    t = head_block_join<TH, false, TWO>(t, a.c, s.sums);
+    if constexpr (!TWO) t.s1 = t.s;
+    const float loss = head_distill_loss<TH>(a, p, t, s);
+    if (tid == 0) {
+        a.loss[row] = loss;
+        if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
+    }
+    if constexpr (GRAD) {
+        const float up = a.g[row];
+        HeadGrad g = head_distill_coef(a, p, t.m, t.s, t.s1, up);
+        if constexpr (!TWO) g.a += g.b;  // (T = 1, or no label: one set of probabilities)
+        T *dz = static_cast<T *>(a.dz) + row * a.V;
+        for (int first = 0; first < z.nvec; first += U * TH) {
+            v4u r[U];
+            head_load<T, U>(z, first, TH, tid, z.nvec, r);
+            head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, z.nvec);
+        }
+        head_place_grads<T, TH, TWO>(a, g, p, up, dz, 0, a.V, s);
+    }
+}
+
+// Few rows: parts of rows on many workgroups, then a workgroup per row for the loss.
+template <typename T, int TH, int U, bool TWO>
+__global__ __launch_bounds__(TH) void qhead_distill_part_kernel(HeadDistillArgs a) {
+    __shared__ HeadSums sums[TH / 64];
+    const long long row = blockIdx.x / a.splits;
+    const int sp = blockIdx.x - (int)row * a.splits;
+    const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
+    const int end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
+    HeadSums t = head_start();
+    for (int first = sp * a.per; first < end; first += U * TH) {
+        v4u r[U];
+        head_load<T, U>(z, first, TH, threadIdx.x, end, r);
+        head_accumulate<T, U, false, TWO>(t, r, a.c);
+    }
+    t = head_block_join<TH, false, TWO>(t, a.c, sums);
+    if (threadIdx.x == 0) a.part[row * a.splits + sp] = t;
+}
+
+template <typename T, bool TWO>
+__global__ __launch_bounds__(256) void qhead_distill_join_kernel(HeadDistillArgs a) {
+    __shared__ HeadDistillLds<256> s;
+    const long long row = blockIdx.x;
+    const HeadPlaces p = head_places<T, 256>(a, row, static_cast<const T *>(a.z) + row * a.ld, s);
+    HeadSums t = head_join_parts<false, TWO>(a.part + row * a.splits, a.splits, a.c);
+    if constexpr (!TWO) t.s1 = t.s;
+    const float loss = head_distill_loss<256>(a, p, t, s);
+    if (threadIdx.x == 0) {
+        a.loss[row] = loss;
+        if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
+    }
+}
+
+template <typename T, int TH, int U, bool TWO>
+__global__ __launch_bounds__(TH) void qhead_distill_grad_kernel(HeadDistillArgs a) {
+    __shared__ HeadDistillLds<TH> s;
+    const long long row = blockIdx.x / a.splits;
+    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
+    const int begin = sp * a.per, end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
+    T *dz = static_cast<T *>(a.dz) + row * a.V;
+    const HeadPlaces p = head_places<T, TH>(a, row, z.p, s);
+    const float up = a.g[row];
+    const float *st = a.stats + 4 * row;
+    HeadGrad g = head_distill_coef(a, p, st[0], st[1], st[2], up);
+    if constexpr (!TWO) g.a += g.b;
+    for (int first = begin; first < end; first += U * TH) {
+        v4u r[U];
+        head_load<T, U>(z, first, TH, tid, end, r);
+        head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, end);
+    }
+    head_place_grads<T, TH, TWO>(a, g, p, up, dz, (long long)begin * HeadRow<T>::VEC,
+                                 min((long long)a.V, (long long)end * HeadRow<T>::VEC), s);
+}
+
+}  // namespace ql
