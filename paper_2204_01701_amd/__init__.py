@@ -95,7 +95,7 @@ class HeadLinearDesc(ctypes.Structure):
     """qhead_linear_desc: a first-order fully-connected layer (row strides in elements)."""
     _fields_ = [("m", ctypes.c_int), ("k", ctypes.c_int), ("n", ctypes.c_int), ("ldx", ctypes.c_longlong),
                 ("ldw", ctypes.c_longlong), ("ldr", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
-                ("dtype", ctypes.c_int), ("act", ctypes.c_int)]
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("unaligned", ctypes.c_int)]
 
 
 class HeadRowsDesc(ctypes.Structure):
@@ -676,6 +676,10 @@ class _HeadOperands:
         if not t.is_contiguous():
             raise ValueError(f"{name}: must be contiguous")
 
+    def unaligned(self, *which):
+        """Whether one of these tensors (by their order) is off 16-byte alignment."""
+        return int(any(self.ptrs[i] & 15 for i in which))
+
     def call(self, name, desc, query, workspace, stream):
         L = lib()
         if stream is None:
@@ -714,7 +718,7 @@ def qhead_linear_fwd(x, w, b, res, y, z=None, act="none", workspace=None, stream
     ldr = o.rows("res", res, (m, n))
     ldy = o.rows("y", y, (m, n))
     o.dense("z", z, (m, n))
-    o.call("qhead_linear_fwd", HeadLinearDesc(m, k, n, ldx, ldw, ldr, ldy, o.code, _head_act(act)),
+    o.call("qhead_linear_fwd", HeadLinearDesc(m, k, n, ldx, ldw, ldr, ldy, o.code, _head_act(act), o.unaligned(0, 1)),
            "qhead_linear_fwd_workspace_size", workspace, stream)
 
 
@@ -732,7 +736,7 @@ def qhead_linear_bwd(x, w, dy, z=None, dx=None, dw=None, db=None, act="none", wo
     o.dense("dx", dx, (m, k))
     o.dense("dw", dw, (n, k))
     o.dense("db", db, (n,), o.torch.float32)
-    o.call("qhead_linear_bwd", HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, o.code, _head_act(act)),
+    o.call("qhead_linear_bwd", HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, o.code, _head_act(act), o.unaligned(0, 1, 2)),
            "qhead_linear_bwd_workspace_size", workspace, stream)
 
 

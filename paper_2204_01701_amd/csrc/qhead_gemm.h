@@ -9,37 +9,90 @@
 // contiguous ("NAT": w in the second, both in the third).
 #pragma once
 
-#include "qdevice.h"
+#include "qpipe.h"
 
 namespace ql {
 
 enum HeadAct { HEAD_NONE = 0, HEAD_RELU = 1, HEAD_GELU = 2, HEAD_GELU_TANH = 3, HEAD_SILU = 4 };
 
-__device__ __forceinline__ float head_act(int act, float z) {
-    switch (act) {
-        case HEAD_RELU: return z > 0.0f ? z : z == z ? 0.0f : z;  // (NaN stays NaN)
-        case HEAD_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-        case HEAD_GELU_TANH: return 0.5f * z * (1.0f + tanhf(0.79788456f * (z + 0.044715f * z * z * z)));
-        case HEAD_SILU: return z / (1.0f + expf(-z));
-        default: return z;
+// The activations from exp2 and a reciprocal (each within an ulp or so): absolute errors of a few
+// 1e-7 (1 + |z|), where the library functions' branches would cost a GEMM epilogue several times the
+// instructions.  erf by the rational approximation 7.1.26 of Abramowitz and Stegun, Handbook of
+// Mathematical Functions (absolute error 1.5e-7).
+__device__ __forceinline__ float head_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.4426950408889634f); }
+__device__ __forceinline__ float head_rcp(float x) { return __builtin_amdgcn_rcpf(x); }
+
+// Phi(z), and e = exp(-z^2 / 2) for the slope.
+__device__ __forceinline__ float head_phi(float z, float &e) {
+    const float x = fabsf(z) * 0.70710678118f;
+    const float t = head_rcp(1.0f + 0.3275911f * x);
+    e = head_exp(-0.5f * z * z);
+    const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float tail = 0.5f * p * e;  // Phi(-|z|)
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+__device__ __forceinline__ float head_sigmoid(float z) { return head_rcp(1.0f + head_exp(-z)); }
+
+template <int ACT> __device__ __forceinline__ float head_act(float z) {
+    if constexpr (ACT == HEAD_RELU) return z > 0.0f ? z : z == z ? 0.0f : z;  // (NaN stays NaN)
+    if constexpr (ACT == HEAD_GELU) {
+        float e;
+        return z * head_phi(z, e);
     }
+    // 0.5 (1 + tanh u) = sigmoid(2 u)
+    if constexpr (ACT == HEAD_GELU_TANH) return z * head_sigmoid(z * (1.5957691216f + 0.0713548163f * z * z));
+    if constexpr (ACT == HEAD_SILU) return z * head_sigmoid(z);
+    return z;
 }
 
-__device__ __forceinline__ float head_act_slope(int act, float z) {
-    switch (act) {
-        case HEAD_RELU: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-        case HEAD_GELU: return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
-        case HEAD_GELU_TANH: {
-            const float t = tanhf(0.79788456f * (z + 0.044715f * z * z * z)), u = 1.0f - t * t;
-            // (u is 0 where the polynomial behind it may have overflowed)
-            return 0.5f * (1.0f + t) + (u == 0.0f ? 0.0f : 0.5f * z * u * 0.79788456f * (1.0f + 0.134145f * z * z));
-        }
-        case HEAD_SILU: {
-            const float s = 1.0f / (1.0f + expf(-z));
-            return s * (1.0f + z * (1.0f - s));
-        }
-        default: return 1.0f;
+template <int ACT> __device__ __forceinline__ float head_act_slope(float z) {
+    if constexpr (ACT == HEAD_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
+    if constexpr (ACT == HEAD_GELU) {
+        float e;
+        const float p = head_phi(z, e);
+        return p + (e == 0.0f ? 0.0f : z * e * 0.39894228040f);
     }
+    if constexpr (ACT == HEAD_GELU_TANH) {
+        const float s = head_sigmoid(z * (1.5957691216f + 0.0713548163f * z * z)), u = s * (1.0f - s);
+        // (u is 0 where the polynomial behind it may have overflowed)
+        return s + (u == 0.0f ? 0.0f : z * u * (1.5957691216f + 0.2140644488f * z * z));
+    }
+    if constexpr (ACT == HEAD_SILU) {
+        const float s = head_sigmoid(z);
+        return s * (1.0f + z * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// N values at once: the choice among the activations is uniform and made once for them.
+template <int N> __device__ __forceinline__ void head_acts(int act, float *v) {
+#define HEAD_ALL(A)                                           \
+    case A:                                                   \
+        _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] = head_act<A>(v[e]); \
+        break
+    switch (act) {
+        HEAD_ALL(HEAD_RELU);
+        HEAD_ALL(HEAD_GELU);
+        HEAD_ALL(HEAD_GELU_TANH);
+        HEAD_ALL(HEAD_SILU);
+        default: break;
+    }
+#undef HEAD_ALL
+}
+// v *= act'(z)
+template <int N> __device__ __forceinline__ void head_slopes(int act, const float *z, float *v) {
+#define HEAD_ALL(A)                                           \
+    case A:                                                   \
+        _Pragma("unroll") for (int e = 0; e < N; ++e) v[e] *= head_act_slope<A>(z[e]); \
+        break
+    switch (act) {
+        HEAD_ALL(HEAD_RELU);
+        HEAD_ALL(HEAD_GELU);
+        HEAD_ALL(HEAD_GELU_TANH);
+        HEAD_ALL(HEAD_SILU);
+        default: break;
+    }
+#undef HEAD_ALL
 }
 
 // Output side of a product: C (ldc), and for the forward the epilogue's operands.
@@ -64,7 +117,8 @@ template <typename T>
 __device__ __forceinline__ void head_store(const HeadOut &o, int J, int i, int j, float acc) {
     if (o.b) acc += o.b[j];
     if (o.z) static_cast<T *>(o.z)[(size_t)i * J + j] = from_f32<T>(acc);
-    float y = head_act(o.act, acc);
+    float y = acc;
+    head_acts<1>(o.act, &y);
     if (o.r) y += to_f32<T>(static_cast<const T *>(o.r)[(size_t)i * o.ldr + j]);
     static_cast<T *>(o.c)[(size_t)i * o.ldc + j] = from_f32<T>(y);
 }
@@ -76,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void qhead_gemm_any_kernel(HeadGemmArgs g
     constexpr int KT = 64 / (int)sizeof(T), ROW = 80;
     __shared__ __attribute__((aligned(16))) char la[64 * ROW], lb[64 * ROW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;
+    const int i0 = blockIdx.x * 64, j0 = blockIdx.y * 64;
     const T *A = static_cast<const T *>(g.a), *B = static_cast<const T *>(g.b);
     f32x16_t acc = {};
     auto stage = [&](const T *p, long long ld, bool nat, int r0, int rows, int t0, char *l) {
@@ -109,35 +163,316 @@ __global__ __launch_bounds__(kThreads) void qhead_gemm_any_kernel(HeadGemmArgs g
     }
 }
 
-// The backward's start: dz = dy o act'(z) (dense, where asked for) and the column sums of the
-// unrounded dz over `rpp` rows as partial sums [part][n], joined below in the order of parts.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void qhead_dz_kernel(const T *dy, long long ldy, const T *z, int act, int m, int n,
-                                                            int rpp, T *dz, float *part) {
-    __shared__ float sum[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int j = blockIdx.x * 64 + lane;
-    const int begin = blockIdx.y * rpp, end = min(m, begin + rpp);
-    float s = 0.0f;
-    if (j < n)
-        for (int i = begin + wave; i < end; i += 4) {
-            float v = to_f32<T>(dy[(size_t)i * ldy + j]);
-            if (act != HEAD_NONE) v *= head_act_slope(act, to_f32<T>(z[(size_t)i * n + j]));
-            if (dz) dz[(size_t)i * n + j] = from_f32<T>(v);
-            s += v;
+// --- large products ----------------------------------------------------------------------
+// A workgroup computes a BI x BJ tile of C from a ring of NS stages in LDS (qpipe.h), each 64 bytes
+// of t deep: 32 bf16 or 16 fp32.  A stage's operand tiles are copied straight into LDS through
+// buffer resources; a lane with nothing to load (a row past the matrix, t past its end) passes an
+// offset past the buffer and gets zeros.  KM tiles are read as 16-byte fragments, NAT tiles
+// transposed on the read (bf16) or element by element (fp32, whose MFMAs take four times as
+// long as the reads).  The MFMA's rows are j and its columns i, so a lane holds four neighbours of a row of C.
+constexpr uint32_t kPastBuffer = 0x80000000u;  // (resources claim 2^31 - 1 bytes; the host keeps a tile's offsets below)
+
+template <typename T> struct HeadStep {
+    static constexpr int BK = 64 / (int)sizeof(T);
+};
+
+// One operand's part in the copies of a stage: BX rows of C's side, W waves.
+template <typename T, bool NAT, int BX, int W> struct HeadSrc {
+    static constexpr int NI = BX / (16 * W);               // instructions a wave issues per stage
+    static constexpr int S16 = BX * (int)sizeof(T) / 16;   // 16-byte slots in a NAT row
+    static_assert(BX % (16 * W) == 0, "whole instructions");
+    const char *base;
+    size_t step_bytes;
+    uint32_t off[NI];
+    int at[NI];  // KM: the byte of t within the stage (the same for all); NAT: its row
+
+    __device__ __forceinline__ static int swz(int row) { return sizeof(T) == 2 ? nat_swz<S16>(row) : 0; }
+
+    __device__ __forceinline__ HeadSrc(const void *p, long long ld, int x0, int X, int wave, int lane) {
+        const size_t ldb = (size_t)ld * sizeof(T);
+        if constexpr (NAT) {
+            base = static_cast<const char *>(p) + (size_t)x0 * sizeof(T);
+            step_bytes = HeadStep<T>::BK * ldb;
+        } else {
+            base = static_cast<const char *>(p) + (size_t)x0 * ldb;
+            step_bytes = 64;
         }
-    sum[wave][lane] = s;
-    __syncthreads();
-    if (part && wave == 0 && j < n)
-        part[(size_t)blockIdx.y * n + j] = sum[0][lane] + sum[1][lane] + sum[2][lane] + sum[3][lane];
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+            const int q = wave * NI + n;
+            if constexpr (NAT) {
+                constexpr int RPI = 64 / S16;
+                const int row = q * RPI + lane / S16, slot = (lane % S16) ^ swz(row);
+                const bool ok = x0 + slot * Elem<T>::VEC < X;
+                off[n] = ok ? (uint32_t)(row * ldb) + slot * 16 : kPastBuffer;
+                at[n] = row;
+            } else {
+                const int row = q * 16 + (lane >> 2), col = km_fill_col(lane);
+                off[n] = x0 + row < X ? (uint32_t)(row * ldb) + col * 16 : kPastBuffer;
+                at[n] = col * 16;
+            }
+        }
+    }
+    // Copies the stage of K step s (left: what remains of t from there, in `at`'s units; 0 or less: nothing).
+    __device__ __forceinline__ void issue(int s, int left, char *tile, int wave, DmaPart &part) const {
+        const __amdgpu_buffer_rsrc_t rs = raw_rsrc(base + (size_t)s * step_bytes, 0x7fffffffu);
+#pragma unroll
+        for (int n = 0; n < NI; ++n)
+            if (part.take()) dma16_buf(rs, at[n] < left ? off[n] : kPastBuffer, 0, tile + (wave * NI + n) * 1024);
+    }
+    __device__ __forceinline__ static int left_at(int R, int s) {
+        return NAT ? R - s * HeadStep<T>::BK : (R - s * HeadStep<T>::BK) * (int)sizeof(T);
+    }
+    // The 32 x (32-byte chunk c) MFMA fragment at row x of the tile.
+    __device__ __forceinline__ static v4u frag(const char *tile, int x, int c, int lane) {
+        if constexpr (!NAT) return lds_read16(tile + km_off(x + (lane & 31), 2 * c + (lane >> 5)));
+        else if constexpr (sizeof(T) == 2) return nat_frag_bf16<S16>(tile, 16 * c, x, lane);
+        else {
+            const char *p = tile + (8 * c + 4 * (lane >> 5)) * (BX * 4) + (x + (lane & 31)) * 4;
+            v4u v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t *>(p + i * BX * 4);
+            return v;
+        }
+    }
+};
+
+typedef uint32_t v4u_row __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes at any element
+
+// Eight neighbours of a row of C: epilogue and stores (`n` of them are inside the row).
+template <typename T> __device__ __forceinline__ void head_store8(T *p, const float *v, int n) {
+    if (n >= 8) {
+#pragma unroll
+        for (int h = 0; h < 8; h += Elem<T>::VEC) *reinterpret_cast<v4u_row *>(p + h) = vpack<T>(v + h);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = from_f32<T>(v[e]);
+    }
+}
+template <typename T> __device__ __forceinline__ void head_load8(const T *p, float *v, int n) {
+    if (n >= 8) {
+#pragma unroll
+        for (int h = 0; h < 8; h += Elem<T>::VEC) {
+            const v4u x = *reinterpret_cast<const v4u_row *>(p + h);
+#pragma unroll
+            for (int e = 0; e < Elem<T>::VEC; ++e) v[h + e] = vget<T>(x, e);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32<T>(p[e]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void head_epilogue8(const HeadOut &o, int J, int i, int j, float *v, const float *b) {
+    const int n = J - j;
+    if (o.b) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += b[e];
+    }
+    if (o.z) head_store8<T>(static_cast<T *>(o.z) + (size_t)i * J + j, v, n);
+    head_acts<8>(o.act, v);
+    if (o.r) {
+        float r[8];
+        head_load8<T>(static_cast<const T *>(o.r) + (size_t)i * o.ldr + j, r, n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
+    }
+    head_store8<T>(static_cast<T *>(o.c) + (size_t)i * o.ldc + j, v, n);
 }
 
+struct HeadTileArgs {
+    HeadGemmArgs g;
+    int ti, tj, splits, per;  // tiles; K steps of a split
+    float *part;              // splits x I x J, for splits > 1
+};
+
+// Logical tile of a workgroup: the workgroups of an XCD take neighbouring tiles, in bands of
+// eight rows of tiles, so that they share operands in its L2.
+__device__ __forceinline__ void head_tile(int bid, int ti, int tj, int &i, int &j) {
+    const int band = bid / (8 * tj), rows = min(8, ti - band * 8), in = bid - band * 8 * tj;
+    i = band * 8 + in % rows;
+    j = in / rows;
+}
+
+template <int BI, int BJ, int WVI, int NS> constexpr int head_tile_lds() {
+    const int ring = NS * (BI + BJ) * 64, stage = BI / WVI * (BJ * 4 + 16);
+    return ring > stage ? ring : stage;
+}
+
+template <typename T, bool ANAT, bool BNAT, int BI, int BJ, int WVI, int WVJ, int NS, int WGS>
+__global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_kernel(HeadTileArgs a) {
+    constexpr int W = WVI * WVJ, TH = 64 * W, WI = BI / WVI, WJ = BJ / WVJ, MI = WI / 32, MJ = WJ / 32;
+    constexpr int STAGE = (BI + BJ) * 64, BK = HeadStep<T>::BK;
+    typedef HeadSrc<T, ANAT, BI, W> SA;
+    typedef HeadSrc<T, BNAT, BJ, W> SB;
+    __shared__ __attribute__((aligned(16))) char lds[head_tile_lds<BI, BJ, WVI, NS>()];
+    const int lane = threadIdx.x & 63, wave = wave_id(), wi = wave / WVJ, wj = wave - wi * WVJ;
+    const HeadGemmArgs &g = a.g;
+    int bid = xcd_remap(blockIdx.x, a.ti * a.tj * a.splits);
+    const int split = bid / (a.ti * a.tj);
+    int ti, tj;
+    head_tile(bid - split * a.ti * a.tj, a.ti, a.tj, ti, tj);
+    const int i0 = ti * BI, j0 = tj * BJ;
+    const int steps = (g.R + BK - 1) / BK, begin = split * a.per, nst = min(a.per, steps - begin);
+    const SA sa(g.a, g.lda, i0, g.I, wave, lane);
+    const SB sb(g.b, g.ldb, j0, g.J, wave, lane);
+    f32x16_t acc[MI][MJ];
+#pragma unroll
+    for (int x = 0; x < MI; ++x)
+#pragma unroll
+        for (int y = 0; y < MJ; ++y) acc[x][y] = f32x16_t{};
+    v4u fa[2][MI], fb[2][MJ];
+    run_ring<NS, SA::NI + SB::NI>(
+        nst, begin,
+        [&](int s, int slot, bool live, int lo, int hi) {
+            char *st = lds + slot * STAGE;
+            DmaPart part(lo, hi);
+            sa.issue(s, live ? SA::left_at(g.R, s) : 0, st, wave, part);
+            sb.issue(s, live ? SB::left_at(g.R, s) : 0, st + BI * 64, wave, part);
+        },
+        [&](int slot, int c, int buf) {
+            const char *st = lds + slot * STAGE;
+#pragma unroll
+            for (int x = 0; x < MI; ++x) fa[buf][x] = SA::frag(st, wi * WI + 32 * x, c, lane);
+#pragma unroll
+            for (int y = 0; y < MJ; ++y) fb[buf][y] = SB::frag(st + BI * 64, wj * WJ + 32 * y, c, lane);
+        },
+        [&](int buf) {
+#pragma unroll
+            for (int x = 0; x < MI; ++x)
+#pragma unroll
+                for (int y = 0; y < MJ; ++y) mfma_chunk<T>(fb[buf][y], fa[buf][x], acc[x][y]);
+        });
+    // Epilogue, one row of waves at a time: the accumulators go to LDS as rows of C, and come back as
+    // eight neighbours a thread, whose global accesses are whole lines.
+    constexpr int ROW = BJ * 4 + 16, CG = BJ / 8, SWEEP = TH / CG;
+    const int j = j0 + (threadIdx.x % CG) * 8;
+    float b[8] = {};
+    if (g.o.b && a.splits == 1) head_load8<float>(g.o.b + j, b, g.J - j);
+#pragma unroll
+    for (int p = 0; p < WVI; ++p) {
+        lds_barrier();
+        if (wi == p) {
+#pragma unroll
+            for (int x = 0; x < MI; ++x)
+#pragma unroll
+                for (int y = 0; y < MJ; ++y)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        *reinterpret_cast<v4f *>(lds + (32 * x + (lane & 31)) * ROW + (wj * WJ + 32 * y + 8 * v + 4 * (lane >> 5)) * 4) =
+                            v4f{acc[x][y][4 * v], acc[x][y][4 * v + 1], acc[x][y][4 * v + 2], acc[x][y][4 * v + 3]};
+        }
+        lds_barrier();
+        if (j >= g.J) continue;
+        for (int r = threadIdx.x / CG; r < WI; r += SWEEP) {
+            const int i = i0 + p * WI + r;
+            if (i >= g.I) break;
+            float v[8];
+            const char *q = lds + r * ROW + (threadIdx.x % CG) * 32;
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const v4f t = *reinterpret_cast<const v4f *>(q + h * 4);
+                v[h] = t[0], v[h + 1] = t[1], v[h + 2] = t[2], v[h + 3] = t[3];
+            }
+            if (a.splits > 1) head_store8<float>(a.part + ((size_t)split * g.I + i) * g.J + j, v, g.J - j);
+            else head_epilogue8<T>(g.o, g.J, i, j, v, b);
+        }
+    }
+}
+
+// The splits' partial products, in their order, and the epilogue.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void qhead_join_kernel(HeadTileArgs a) {
+    const HeadGemmArgs &g = a.g;
+    const int groups = (g.J + 7) / 8;
+    const long long total = (long long)g.I * groups;
+    for (long long q = (long long)blockIdx.x * kThreads + threadIdx.x; q < total; q += (long long)gridDim.x * kThreads) {
+        const int i = (int)(q / groups), j = (int)(q - (long long)i * groups) * 8;
+        float v[8], b[8] = {};
+        head_load8<float>(a.part + (size_t)i * g.J + j, v, g.J - j);
+        for (int s = 1; s < a.splits; ++s) {
+            float u[8];
+            head_load8<float>(a.part + ((size_t)s * g.I + i) * g.J + j, u, g.J - j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += u[e];
+        }
+        if (g.o.b) head_load8<float>(g.o.b + j, b, g.J - j);
+        head_epilogue8<T>(g.o, g.J, i, j, v, b);
+    }
+}
+
+// rows x cols at any stride and alignment -> rows of `out_cols` (whole 16-byte vectors), zeros behind.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void qhead_pad_kernel(const T *p, long long ld, long long rows, int cols, int out_cols, T *out) {
+    constexpr int VEC = Elem<T>::VEC;
+    const int vecs = out_cols / VEC;
+    for (long long q = (long long)blockIdx.x * kThreads + threadIdx.x; q < rows * vecs; q += (long long)gridDim.x * kThreads) {
+        const long long i = q / vecs;
+        const int j = (int)(q - i * vecs) * VEC;
+        const T *src = p + (size_t)i * ld + j;
+        v4u v;
+        if (j + VEC <= cols) {
+            v = *reinterpret_cast<const v4u_row *>(src);
+        } else {
+            float f[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = j + e < cols ? to_f32<T>(src[e]) : 0.0f;
+            v = vpack<T>(f);
+        }
+        *reinterpret_cast<v4u *>(out + (size_t)i * out_cols + j) = v;
+    }
+}
+
+// The backward's start: dz = dy o act'(z) (rows of ldd, where asked for) and the column sums of the
+// unrounded dz over `rpp` rows as partial sums [part][n], joined below in the order of parts.
+// A workgroup takes 256 columns, eight a thread, eight rows at a time.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void qhead_dz_kernel(const T *dy, long long ldy, const T *z, int act, int m, int n,
+                                                            int rpp, T *dz, long long ldd, float *part) {
+    __shared__ float sum[8][256 + 8];
+    const int cg = threadIdx.x & 31, rg = threadIdx.x >> 5;
+    const int j = blockIdx.x * 256 + cg * 8;
+    const int begin = blockIdx.y * rpp, end = min(m, begin + rpp);
+    float s[8] = {};
+    if (j < n)
+        for (int i = begin + rg; i < end; i += 8) {
+            float v[8], u[8];
+            head_load8<T>(dy + (size_t)i * ldy + j, v, n - j);
+            if (act != HEAD_NONE) {
+                head_load8<T>(z + (size_t)i * n + j, u, n - j);
+                head_slopes<8>(act, u, v);
+            }
+            // (elements behind the row's end loaded as 0 stay 0: a padded dz has zeros there)
+            if (dz) head_store8<T>(dz + (size_t)i * ldd + j, v, (int)min(ldd - j, 8LL));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += v[e];
+        }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[rg][cg * 8 + e] = s[e];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= n) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) t += sum[r][threadIdx.x];
+    part[(size_t)blockIdx.y * n + c] = t;
+}
+
+// db: 32 columns a workgroup, eight threads each.
 template <int = 0>
 __global__ __launch_bounds__(kThreads) void qhead_colsum_kernel(const float *part, int parts, int n, float *db) {
-    const int j = blockIdx.x * kThreads + threadIdx.x;
-    if (j >= n) return;
+    __shared__ float sum[8][32];
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
     float s = 0.0f;
-    for (int p = 0; p < parts; ++p) s += part[(size_t)p * n + j];
+    if (j < n)
+        for (int p = r; p < parts; p += 8) s += part[(size_t)p * n + j];
+    sum[r][c] = s;
+    __syncthreads();
+    if (r || j >= n) return;
+#pragma unroll
+    for (int q = 1; q < 8; ++q) s += sum[q][c];
     db[j] = s;
 }
 

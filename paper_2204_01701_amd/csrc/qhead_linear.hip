@@ -16,29 +16,152 @@ bool linear_ok(const qhead_linear_desc *d) {
            (int)d->act >= QL_ACT_NONE && (int)d->act <= QL_ACT_SILU && d->ldx >= d->k && d->ldw >= d->k;
 }
 
-template <bool ANAT, bool BNAT> ql_status run_gemm(const HeadGemmArgs &g, ql_dtype dt, hipStream_t st) {
-    if (g.I == 0 || g.J == 0) return QL_OK;
-    const dim3 grid(cdiv(g.J, 64), cdiv(g.I, 64));
-    if (grid.y > 65535) return QL_EUNSUPPORTED;
-    if (dt == QL_BF16)
-        hipLaunchKernelGGL((qhead_gemm_any_kernel<uint16_t, ANAT, BNAT>), grid, dim3(kThreads), 0, st, g);
-    else
-        hipLaunchKernelGGL((qhead_gemm_any_kernel<float, ANAT, BNAT>), grid, dim3(kThreads), 0, st, g);
+// --- one product ------------------------------------------------------------------------
+// An operand as the caller has it: `rows` rows of `cols` elements.  NAT: t is the row index.
+struct Operand {
+    const void *p;
+    long long rows, cols, ld;
+    bool padded;  // (one of our own copies: whole vectors, zeros behind each row)
+};
+
+int vec(ql_dtype t) { return t == QL_BF16 ? 8 : 4; }
+long long padded_cols(const Operand &o, ql_dtype t) { return (o.cols + vec(t) - 1) / vec(t) * vec(t); }
+
+// Rows of whole 16-byte vectors, whose offsets within a tile fit a buffer resource.
+bool direct(const Operand &o, ql_dtype t, bool ptr_aligned) {
+    return (o.padded || (o.cols % vec(t) == 0 && o.ld % vec(t) == 0 && ptr_aligned)) &&
+           (double)o.ld * (double)esize(t) * 256 < 2147483648.0;
+}
+bool pad_fits(const Operand &o, ql_dtype t) { return (double)padded_cols(o, t) * (double)esize(t) * 256 < 2147483648.0; }
+
+struct Product {
+    int I, J, R;
+    Operand a, b;
+};
+
+enum Tile { TILE_ANY, TILE_128, TILE_256 };
+struct ProductPlan {
+    Tile tile;
+    bool pad_a, pad_b;
+    int ti, tj, splits, per;
+    size_t a_bytes, b_bytes, part_bytes;
+    size_t bytes() const { return a_bytes + b_bytes + part_bytes; }
+};
+
+// al_a, al_b: whether the operands' pointers are (taken to be) 16-byte aligned.
+ProductPlan plan_product(const Product &q, ql_dtype t, bool al_a, bool al_b) {
+    ProductPlan p{};
+    p.splits = 1;
+    p.pad_a = !direct(q.a, t, al_a);
+    p.pad_b = !direct(q.b, t, al_b);
+    const double flops = 2.0 * q.I * q.J * std::max(1, q.R);
+    const bool fits = (!p.pad_a || pad_fits(q.a, t)) && (!p.pad_b || pad_fits(q.b, t));
+    if (!fits || ((p.pad_a || p.pad_b) && flops < 2e7) || q.R == 0) {
+        p.pad_a = p.pad_b = false;
+        return p;
+    }
+    p.tile = cdiv(q.I, 256) * (long long)cdiv(q.J, 256) >= 3 * kNumCUs / 4 ? TILE_256 : TILE_128;
+    const int forced = env_override("QHEAD_TILE", 0);
+    if (forced) p.tile = forced == 256 ? TILE_256 : forced == 128 ? TILE_128 : TILE_ANY;
+    if (p.tile == TILE_ANY) {
+        p.pad_a = p.pad_b = false;
+        return p;
+    }
+    const int B = p.tile == TILE_256 ? 256 : 128, steps = cdiv(q.R, 64 / (int)esize(t));
+    p.ti = cdiv(q.I, B);
+    p.tj = cdiv(q.J, B);
+    const long long tiles = (long long)p.ti * p.tj;
+    int want = 1;
+    if (p.tile == TILE_128 && tiles < kNumCUs) {
+        // split t until two workgroups a CU are busy, 8 steps each at least, the partial sums within their cap
+        want = (int)std::min<long long>(2 * kNumCUs / tiles, steps / 8);
+        want = (int)std::min<double>(want, (double)kMaxSplitBytes / (4.0 * q.I * q.J));
+    }
+    want = std::max(1, env_override("QHEAD_SPLITS", want));
+    p.per = cdiv(steps, std::min(want, steps));
+    p.splits = cdiv(steps, p.per);
+    if (p.pad_a) p.a_bytes = align_up((size_t)q.a.rows * padded_cols(q.a, t) * esize(t));
+    if (p.pad_b) p.b_bytes = align_up((size_t)q.b.rows * padded_cols(q.b, t) * esize(t));
+    if (p.splits > 1) p.part_bytes = align_up((size_t)p.splits * q.I * q.J * sizeof(float));
+    return p;
+}
+
+// A zero-padded copy of an operand at `to`; o becomes the copy.
+template <typename T> ql_status pad_operand(Operand &o, void *to, ql_dtype t, hipStream_t st) {
+    const long long cols = padded_cols(o, t);
+    hipLaunchKernelGGL((qhead_pad_kernel<T>), dim3(grid_1d(o.rows * cols / vec(t))), dim3(kThreads), 0, st,
+                       static_cast<const T *>(o.p), o.ld, o.rows, (int)o.cols, (int)cols, static_cast<T *>(to));
+    o.p = to;
+    o.ld = cols;
+    o.padded = true;
     return hip_status();
 }
 
-// The pass over dy and z: rows of a part, parts, and the workspace's pieces.
+template <typename T, bool ANAT, bool BNAT>
+ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_t st) {
+    const HeadGemmArgs &g = a.g;
+    if (p.tile == TILE_ANY) {
+        const dim3 grid(cdiv(g.I, 64), cdiv(g.J, 64));
+        if (grid.y > 65535) return QL_EUNSUPPORTED;
+        hipLaunchKernelGGL((qhead_gemm_any_kernel<T, ANAT, BNAT>), grid, dim3(kThreads), 0, st, g);
+        return hip_status();
+    }
+    const dim3 grid((unsigned)(a.ti * a.tj * a.splits));
+    if (p.tile == TILE_256)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 2, 4, 1>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 128, 2, 2, 4, 2>), grid, dim3(256), 0, st, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((qhead_join_kernel<T>), dim3(grid_1d((long long)g.I * cdiv(g.J, 8))), dim3(kThreads), 0, st, a);
+    return hip_status();
+}
+
+template <bool ANAT, bool BNAT>
+ql_status run_product(Product q, const HeadOut &o, ql_dtype t, char *ws, size_t ws_bytes, hipStream_t st) {
+    if (q.I == 0 || q.J == 0) return QL_OK;
+    ProductPlan p = plan_product(q, t, aligned16(q.a.p), aligned16(q.b.p));
+    if (p.bytes() > ws_bytes) {
+        // (a misaligned pointer that the descriptor does not announce)
+        p = ProductPlan{};
+        p.splits = 1;
+    }
+    ql_status s = QL_OK;
+    if (p.pad_a) s = t == QL_BF16 ? pad_operand<uint16_t>(q.a, ws, t, st) : pad_operand<float>(q.a, ws, t, st);
+    if (s == QL_OK && p.pad_b)
+        s = t == QL_BF16 ? pad_operand<uint16_t>(q.b, ws + p.a_bytes, t, st) : pad_operand<float>(q.b, ws + p.a_bytes, t, st);
+    if (s != QL_OK) return s;
+    const HeadTileArgs a{HeadGemmArgs{q.a.p, q.b.p, q.a.ld, q.b.ld, q.I, q.J, q.R, o}, p.ti, p.tj, p.splits, p.per,
+                         reinterpret_cast<float *>(ws + p.a_bytes + p.b_bytes)};
+    return t == QL_BF16 ? launch_product<uint16_t, ANAT, BNAT>(p, a, st) : launch_product<float, ANAT, BNAT>(p, a, st);
+}
+
+Product fwd_product(const qhead_linear_desc *d, const void *x, const void *w) {
+    return {d->m, d->n, d->k, {x, d->m, d->k, d->ldx, false}, {w, d->n, d->k, d->ldw, false}};
+}
+Product dx_product(const qhead_linear_desc *d, const Operand &dz, const void *w) {
+    return {d->m, d->k, d->n, dz, {w, d->n, d->k, d->ldw, false}};
+}
+Product dw_product(const qhead_linear_desc *d, const Operand &dz, const void *x) {
+    return {d->n, d->k, d->m, dz, {x, d->m, d->k, d->ldx, false}};
+}
+
+// --- the pass over dy and z ----------------------------------------------------------------
+// dz is stored where there is an activation, and as a copy of dy where the products would copy it
+// both; rows of whole vectors.
 struct DzPlan {
     bool store;
+    long long ld;
     int rpp, parts;
     size_t dz_bytes, part_bytes;
 };
-DzPlan plan_dz(const qhead_linear_desc *d) {
+DzPlan plan_dz(const qhead_linear_desc *d, bool al) {
     DzPlan p;
-    p.store = d->act != QL_ACT_NONE;
+    const Operand dy{nullptr, d->m, d->n, d->ldy, false};
+    p.store = d->act != QL_ACT_NONE || !direct(dy, d->dtype, al);
+    p.ld = padded_cols(dy, d->dtype);
     p.rpp = std::max(32, cdiv(d->m, 256));
     p.parts = std::max(1, cdiv(d->m, p.rpp));
-    p.dz_bytes = p.store ? align_up((size_t)d->m * d->n * esize(d->dtype)) : 0;
+    p.dz_bytes = p.store ? align_up((size_t)d->m * p.ld * esize(d->dtype)) : 0;
     p.part_bytes = align_up((size_t)p.parts * d->n * sizeof(float));
     return p;
 }
@@ -46,9 +169,14 @@ DzPlan plan_dz(const qhead_linear_desc *d) {
 template <typename T>
 void launch_dz(const qhead_linear_desc *d, const DzPlan &p, const void *dy, const void *z, void *dz, float *part,
                hipStream_t st) {
-    hipLaunchKernelGGL((qhead_dz_kernel<T>), dim3(cdiv(d->n, 64), p.parts), dim3(kThreads), 0, st,
+    hipLaunchKernelGGL((qhead_dz_kernel<T>), dim3(cdiv(d->n, 256), p.parts), dim3(kThreads), 0, st,
                        static_cast<const T *>(dy), d->ldy, static_cast<const T *>(z), (int)d->act, d->m, d->n, p.rpp,
-                       static_cast<T *>(dz), part);
+                       static_cast<T *>(dz), p.ld, part);
+}
+
+Operand dz_operand(const qhead_linear_desc *d, const DzPlan &p, const void *dy, void *dz) {
+    if (p.store) return {dz, d->m, d->n, p.ld, true};
+    return {dy, d->m, d->n, d->ldy, false};
 }
 
 }  // namespace
@@ -56,8 +184,8 @@ void launch_dz(const qhead_linear_desc *d, const DzPlan &p, const void *dy, cons
 extern "C" {
 
 size_t qhead_linear_fwd_workspace_size(const qhead_linear_desc *d) {
-    (void)d;
-    return 0;
+    if (!linear_ok(d) || d->m == 0) return 0;
+    return plan_product(fwd_product(d, nullptr, nullptr), d->dtype, !d->unaligned, !d->unaligned).bytes();
 }
 
 ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void *w, const float *b, const void *r,
@@ -72,14 +200,18 @@ ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void
     const size_t need = qhead_linear_fwd_workspace_size(d);
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
-    HeadGemmArgs g{x, w, d->ldx, d->ldw, d->m, d->n, d->k, HeadOut{y, d->ldy, b, r, d->ldr, z, (int)d->act}};
-    return run_gemm<false, false>(g, d->dtype, static_cast<hipStream_t>(stream));
+    return run_product<false, false>(fwd_product(d, x, w), HeadOut{y, d->ldy, b, r, d->ldr, z, (int)d->act}, d->dtype,
+                                     static_cast<char *>(workspace), workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
 size_t qhead_linear_bwd_workspace_size(const qhead_linear_desc *d) {
     if (!linear_ok(d) || d->ldy < d->n) return 0;
-    const DzPlan p = plan_dz(d);
-    return p.dz_bytes + p.part_bytes;
+    const bool al = !d->unaligned;
+    const DzPlan p = plan_dz(d, al);
+    const Operand dz = dz_operand(d, p, nullptr, nullptr);
+    // the two products run one after the other on the same piece
+    return p.dz_bytes + p.part_bytes + std::max(plan_product(dx_product(d, dz, nullptr), d->dtype, al, al).bytes(),
+                                                plan_product(dw_product(d, dz, nullptr), d->dtype, al, al).bytes());
 }
 
 ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void *w, const void *dy, const void *z,
@@ -95,28 +227,28 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const DzPlan p = plan_dz(d);
+    const DzPlan p = plan_dz(d, !d->unaligned);
     char *ws = static_cast<char *>(workspace);
     void *dz = p.store && (dx || dw) ? ws : nullptr;
     float *part = db ? reinterpret_cast<float *>(ws + p.dz_bytes) : nullptr;
     if (dz || part) {
         if (d->dtype == QL_BF16) launch_dz<uint16_t>(d, p, dy, z, dz, part, st);
         else launch_dz<float>(d, p, dy, z, dz, part, st);
-        if (db) hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(cdiv(d->n, kThreads)), dim3(kThreads), 0, st, part, p.parts, d->n, db);
+        if (db) hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(cdiv(d->n, 32)), dim3(kThreads), 0, st, part, p.parts, d->n, db);
         const ql_status s = hip_status();
         if (s != QL_OK) return s;
     }
-    const void *src = p.store ? dz : dy;
-    const long long ld = p.store ? d->n : d->ldy;
+    const Operand src = dz_operand(d, p, dy, dz);
+    ws += p.dz_bytes + p.part_bytes;
+    const size_t left = workspace_bytes - p.dz_bytes - p.part_bytes;
     if (dx) {
-        HeadGemmArgs g{src, w, ld, d->ldw, d->m, d->k, d->n, HeadOut{dx, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE}};
-        const ql_status s = run_gemm<false, true>(g, d->dtype, st);
+        const ql_status s = run_product<false, true>(dx_product(d, src, w), HeadOut{dx, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE},
+                                                     d->dtype, ws, left, st);
         if (s != QL_OK) return s;
     }
-    if (dw) {
-        HeadGemmArgs g{src, x, ld, d->ldx, d->n, d->k, d->m, HeadOut{dw, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE}};
-        return run_gemm<true, true>(g, d->dtype, st);
-    }
+    if (dw)
+        return run_product<true, true>(dw_product(d, src, x), HeadOut{dw, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE},
+                                       d->dtype, ws, left, st);
     return QL_OK;
 }
 

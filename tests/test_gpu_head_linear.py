@@ -116,6 +116,17 @@ def test_larger(m, k, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("tile,splits", [(128, 1), (128, 3), (256, 1), (256, 2), (1, 1)])
+@pytest.mark.parametrize("m,k,n", [(300, 200, 264), (520, 1040, 128), (70, 96, 1031)])
+def test_every_tile(m, k, n, tile, splits, dtype, monkeypatch):
+    """Each tile on the same product, whatever the size would choose."""
+    monkeypatch.setenv("QHEAD_TILE", str(tile))
+    monkeypatch.setenv("QHEAD_SPLITS", str(splits))
+    _fwd(m, k, n, dtype, "silu", offset=8, pad=8)
+    _bwd(m, k, n, dtype, "gelu", offset=1, pad=4)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
 def test_no_rows(dtype):
     _fwd(0, 9, 5, dtype, "gelu")
     _bwd(0, 9, 5, dtype, "gelu")
