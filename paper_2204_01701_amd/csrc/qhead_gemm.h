@@ -263,8 +263,18 @@ template <typename T> __device__ __forceinline__ void head_load8(const T *p, flo
         for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32<T>(p[e]) : 0.0f;
     }
 }
+// r: the residual's raw bits, loaded beforehand, where eight of its elements are inside the row.
+template <typename T> struct HeadRaw8 {
+    v4u v[8 / Elem<T>::VEC];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int h = 0; h < 8 / Elem<T>::VEC; ++h) v[h] = *reinterpret_cast<const v4u_row *>(p + h * Elem<T>::VEC);
+    }
+    __device__ __forceinline__ float get(int e) const { return vget<T>(v[e / Elem<T>::VEC], e % Elem<T>::VEC); }
+};
 template <typename T>
-__device__ __forceinline__ void head_epilogue8(const HeadOut &o, int J, int i, int j, float *v, const float *b) {
+__device__ __forceinline__ void head_epilogue8(const HeadOut &o, int J, int i, int j, float *v, const float *b,
+                                               const HeadRaw8<T> &raw) {
     const int n = J - j;
     if (o.b) {
 #pragma unroll
@@ -273,10 +283,15 @@ __device__ __forceinline__ void head_epilogue8(const HeadOut &o, int J, int i, i
     if (o.z) head_store8<T>(static_cast<T *>(o.z) + (size_t)i * J + j, v, n);
     head_acts<8>(o.act, v);
     if (o.r) {
-        float r[8];
-        head_load8<T>(static_cast<const T *>(o.r) + (size_t)i * o.ldr + j, r, n);
+        if (n >= 8) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += r[e];
+            for (int e = 0; e < 8; ++e) v[e] += raw.get(e);
+        } else {
+            const T *r = static_cast<const T *>(o.r) + (size_t)i * o.ldr + j;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < n) v[e] += to_f32<T>(r[e]);
+        }
     }
     head_store8<T>(static_cast<T *>(o.c) + (size_t)i * o.ldc + j, v, n);
 }
@@ -300,7 +315,7 @@ template <int BI, int BJ, int WVI, int NS> constexpr int head_tile_lds() {
     return ring > stage ? ring : stage;
 }
 
-template <typename T, bool ANAT, bool BNAT, int BI, int BJ, int WVI, int WVJ, int NS, int WGS>
+template <typename T, bool ANAT, bool BNAT, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int RING = 0, int NI1 = HeadSrc<T, ANAT, BI, WVI * WVJ>::NI + HeadSrc<T, BNAT, BJ, WVI * WVJ>::NI>
 __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_kernel(HeadTileArgs a) {
     constexpr int W = WVI * WVJ, TH = 64 * W, WI = BI / WVI, WJ = BJ / WVJ, MI = WI / 32, MJ = WJ / 32;
     constexpr int STAGE = (BI + BJ) * 64, BK = HeadStep<T>::BK;
@@ -323,35 +338,44 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_k
 #pragma unroll
         for (int y = 0; y < MJ; ++y) acc[x][y] = f32x16_t{};
     v4u fa[2][MI], fb[2][MJ];
-    run_ring<NS, SA::NI + SB::NI>(
-        nst, begin,
-        [&](int s, int slot, bool live, int lo, int hi) {
-            char *st = lds + slot * STAGE;
-            DmaPart part(lo, hi);
-            sa.issue(s, live ? SA::left_at(g.R, s) : 0, st, wave, part);
-            sb.issue(s, live ? SB::left_at(g.R, s) : 0, st + BI * 64, wave, part);
-        },
-        [&](int slot, int c, int buf) {
-            const char *st = lds + slot * STAGE;
+    auto issue = [&](int s, int slot, bool live, int lo, int hi) {
+        char *st = lds + slot * STAGE;
+        DmaPart part(lo, hi);
+        sa.issue(s, live ? SA::left_at(g.R, s) : 0, st, wave, part);
+        sb.issue(s, live ? SB::left_at(g.R, s) : 0, st + BI * 64, wave, part);
+    };
+    auto read = [&](int slot, int c, int buf) {
+        const char *st = lds + slot * STAGE;
 #pragma unroll
-            for (int x = 0; x < MI; ++x) fa[buf][x] = SA::frag(st, wi * WI + 32 * x, c, lane);
+        for (int x = 0; x < MI; ++x) fa[buf][x] = SA::frag(st, wi * WI + 32 * x, c, lane);
 #pragma unroll
-            for (int y = 0; y < MJ; ++y) fb[buf][y] = SB::frag(st + BI * 64, wj * WJ + 32 * y, c, lane);
-        },
-        [&](int buf) {
+        for (int y = 0; y < MJ; ++y) fb[buf][y] = SB::frag(st + BI * 64, wj * WJ + 32 * y, c, lane);
+    };
+    auto mma = [&](int buf) {
 #pragma unroll
-            for (int x = 0; x < MI; ++x)
+        for (int x = 0; x < MI; ++x)
 #pragma unroll
-                for (int y = 0; y < MJ; ++y) mfma_chunk<T>(fb[buf][y], fa[buf][x], acc[x][y]);
-        });
+            for (int y = 0; y < MJ; ++y) mfma_chunk<T>(fb[buf][y], fa[buf][x], acc[x][y]);
+    };
+    if constexpr (RING == 1) run_ring_single<NS, SA::NI + SB::NI, 2, NI1>(nst, begin, issue, read, mma);
+    else run_ring<NS, SA::NI + SB::NI, NI1>(nst, begin, issue, read, mma);
     // Epilogue, one row of waves at a time: the accumulators go to LDS as rows of C, and come back as
-    // eight neighbours a thread, whose global accesses are whole lines.
-    constexpr int ROW = BJ * 4 + 16, CG = BJ / 8, SWEEP = TH / CG;
-    const int j = j0 + (threadIdx.x % CG) * 8;
+    // eight neighbours a thread, whose global accesses are whole lines.  A pass's residuals are
+    // all requested before its hand-over through LDS: one at a time their latency was 21 us a tile.
+    constexpr int ROW = BJ * 4 + 16, CG = BJ / 8, SWEEP = TH / CG, IT = WI / SWEEP;
+    const int jc = (threadIdx.x % CG) * 8, j = j0 + jc, r0 = threadIdx.x / CG;
+    const bool whole = a.splits == 1 && g.o.r && j + 8 <= g.J;
     float b[8] = {};
     if (g.o.b && a.splits == 1) head_load8<float>(g.o.b + j, b, g.J - j);
 #pragma unroll
     for (int p = 0; p < WVI; ++p) {
+        const int ip = i0 + p * WI + r0;
+        HeadRaw8<T> raw[IT] = {};
+        if (whole) {
+#pragma unroll
+            for (int q = 0; q < IT; ++q)
+                if (ip + q * SWEEP < g.I) raw[q].load(static_cast<const T *>(g.o.r) + (size_t)(ip + q * SWEEP) * g.o.ldr + j);
+        }
         lds_barrier();
         if (wi == p) {
 #pragma unroll
@@ -365,18 +389,19 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_k
         }
         lds_barrier();
         if (j >= g.J) continue;
-        for (int r = threadIdx.x / CG; r < WI; r += SWEEP) {
-            const int i = i0 + p * WI + r;
-            if (i >= g.I) break;
+#pragma unroll
+        for (int q = 0; q < IT; ++q) {
+            const int i = ip + q * SWEEP;
+            if (i >= g.I) continue;
             float v[8];
-            const char *q = lds + r * ROW + (threadIdx.x % CG) * 32;
+            const char *l = lds + (r0 + q * SWEEP) * ROW + jc * 4;
 #pragma unroll
             for (int h = 0; h < 8; h += 4) {
-                const v4f t = *reinterpret_cast<const v4f *>(q + h * 4);
+                const v4f t = *reinterpret_cast<const v4f *>(l + h * 4);
                 v[h] = t[0], v[h + 1] = t[1], v[h + 2] = t[2], v[h + 3] = t[3];
             }
             if (a.splits > 1) head_store8<float>(a.part + ((size_t)split * g.I + i) * g.J + j, v, g.J - j);
-            else head_epilogue8<T>(g.o, g.J, i, j, v, b);
+            else head_epilogue8<T>(g.o, g.J, i, j, v, b, raw[q]);
         }
     }
 }
@@ -398,7 +423,9 @@ __global__ __launch_bounds__(kThreads) void qhead_join_kernel(HeadTileArgs a) {
             for (int e = 0; e < 8; ++e) v[e] += u[e];
         }
         if (g.o.b) head_load8<float>(g.o.b + j, b, g.J - j);
-        head_epilogue8<T>(g.o, g.J, i, j, v, b);
+        HeadRaw8<T> raw = {};
+        if (g.o.r && j + 8 <= g.J) raw.load(static_cast<const T *>(g.o.r) + (size_t)i * g.o.ldr + j);
+        head_epilogue8<T>(g.o, g.J, i, j, v, b, raw);
     }
 }
 

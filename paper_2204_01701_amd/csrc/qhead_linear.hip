@@ -69,7 +69,7 @@ ProductPlan plan_product(const Product &q, ql_dtype t, bool al_a, bool al_b) {
     }
     const int B = p.tile == TILE_256 ? 256 : 128, steps = cdiv(q.R, 64 / (int)esize(t));
     p.ti = cdiv(q.I, B);
-    p.tj = cdiv(q.J, B);
+    p.tj = cdiv(q.J, p.tile == TILE_256 && env_override("QHEAD_VAR", 0) ? 128 : B);
     const long long tiles = (long long)p.ti * p.tj;
     int want = 1;
     if (p.tile == TILE_128 && tiles < kNumCUs) {
@@ -107,8 +107,17 @@ ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_
         return hip_status();
     }
     const dim3 grid((unsigned)(a.ti * a.tj * a.splits));
-    if (p.tile == TILE_256)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 2, 4, 1>), grid, dim3(256), 0, st, a);
+    const int var = env_override("QHEAD_VAR", 0);
+    if (p.tile == TILE_256 && var == 1)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 4, 1, 0, 2>), grid, dim3(512), 0, st, a);
+    else if (p.tile == TILE_256 && var == 2)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 6, 1, 0, 2>), grid, dim3(512), 0, st, a);
+    else if (p.tile == TILE_256 && var == 3)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 2, 2, 3, 2, 0, 4>), grid, dim3(256), 0, st, a);
+    else if (p.tile == TILE_256 && var == 4)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 3, 2, 1>), grid, dim3(512), 0, st, a);
+    else if (p.tile == TILE_256)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 4, 4, 1, 0, 2>), grid, dim3(512), 0, st, a);
     else
         hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 128, 2, 2, 4, 2>), grid, dim3(256), 0, st, a);
     if (a.splits > 1)

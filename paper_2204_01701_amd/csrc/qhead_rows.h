@@ -119,6 +119,11 @@ __device__ __forceinline__ float head_accumulate(HeadSums &a, const v4u (&r)[U],
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = fmaxf(top, vget<T>(r[u], e));
     if (top > a.m) head_shift<ENT, TWO>(a, top, c);
+    if constexpr (sizeof(T) == 2 && U > 4) {
+        // (unpacked anew below: the values of a long chunk would fill the registers)
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(const_cast<v4u &>(r[u])));
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -215,27 +220,62 @@ constexpr int kHeadCap = 1024;  // candidates a workgroup can hold
 template <int TH> struct HeadTopLds {
     uint64_t buf[kHeadCap];      // candidates; after head_rank the best ones in front, in order
     uint64_t best[kHeadTopMax];
-    uint32_t keys[TH];
+    uint32_t kth[2][TH / 64];
     int wave[TH / 64];
-    int n;                       // candidates held
-    uint32_t pick;
+    int n;                       // candidates found (those past kHeadCap were not kept)
 };
 
-// Ranks the n candidates by counting the larger ones: buf[0 .. min(n, K)) is then
-// the best in order.  n^2 / TH steps, without a barrier among them.
-template <int TH> __device__ __forceinline__ void head_rank(HeadTopLds<TH> &s, int K) {
+// A key that at least j lanes of the wave reach, and no smaller one of 16 bits would miss: bits
+// are set from the top while j lanes stay at or above.  (The lower 16 bits stay 0: bf16 values have
+// none, and for fp32 a bound slightly too low only costs candidates.)
+__device__ __forceinline__ uint32_t head_wave_kth(uint32_t key, int j) {
+    uint32_t t = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t up = t | 1u << bit;
+        if (__popcll(__ballot(key >= up)) >= j) t = up;
+    }
+    return t;
+}
+
+// Ranks the candidates at or above `least` by counting the larger ones: buf[0 .. min(n, K)) is
+// then the best in order.
+template <int TH> __device__ __forceinline__ void head_rank(HeadTopLds<TH> &s, int K, uint32_t least) {
     __syncthreads();
     const int n = s.n;
-    for (int i = threadIdx.x; i < n; i += TH) {
+    constexpr int PER = (kHeadCap + TH - 1) / TH;
+    // drop what later bounds ruled out, so that the counting below is about few
+    uint64_t mine[PER];
+    int kept = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        const int i = q * TH + threadIdx.x;
+        mine[q] = i < n ? s.buf[i] : 0;
+        if ((uint32_t)(mine[q] >> 32) < least) mine[q] = 0;
+        kept += mine[q] != 0 ? 1 : 0;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    if (kept) {
+        int at = atomicAdd(&s.n, kept);
+#pragma unroll
+        for (int q = 0; q < PER; ++q)
+            if (mine[q]) s.buf[at++] = mine[q];
+    }
+    __syncthreads();
+    const int m = s.n;
+    for (int i = threadIdx.x; i < m; i += TH) {
         const uint64_t k = s.buf[i];
         int above = 0;
-        for (int j = 0; j < n; ++j) above += s.buf[j] > k ? 1 : 0;
+#pragma unroll 8
+        for (int j = 0; j < m; ++j) above += s.buf[j] > k ? 1 : 0;
         if (above < K) s.best[above] = k;
     }
     __syncthreads();
-    const int kept = min(n, K);
-    for (int i = threadIdx.x; i < kept; i += TH) s.buf[i] = s.best[i];
-    if (threadIdx.x == 0) s.n = kept;
+    const int best = min(m, K);
+    for (int i = threadIdx.x; i < best; i += TH) s.buf[i] = s.best[i];
+    if (threadIdx.x == 0) s.n = best;
     __syncthreads();
 }
 
@@ -260,119 +300,133 @@ template <int TH> __device__ __forceinline__ int head_prefix(int v, int &total, 
     return before + x - v;
 }
 
-// Elements of r whose key is at least kmin (`count` of them in the thread), as a bit
-// mask; only elements below `limit` count.
-template <typename T, int U>
-__device__ __forceinline__ uint64_t head_mask(const v4u (&r)[U], uint32_t kmin, int first, int step, int tid, int limit,
-                                              bool edge) {
+// The elements of a vector whose key is at least kmin, as a bit mask, of the first `left` ones.
+template <typename T> __device__ __forceinline__ uint32_t head_mask(const v4u &r, uint32_t kmin, long long left) {
     constexpr int VEC = Elem<T>::VEC;
-    uint64_t mask = 0;
-    if (kmin < kKeyNegInf) {  // NaN may be needed: decide by the key itself
+    uint32_t mask = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                mask |= (uint64_t)(head_key(vget<T>(r[u], e)) >= kmin ? 1 : 0) << (u * VEC + e);
-    } else {
-        const float f = head_unkey(kmin);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            uint32_t part = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) part |= vget<T>(r[u], e) >= f ? 1u << e : 0u;
-            mask |= (uint64_t)part << (u * VEC);
-        }
-    }
-    if (edge) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long left = (long long)limit - (long long)(first + u * step + tid) * VEC;
-            if (left < VEC) {
-                const uint32_t keep = left > 0 ? (1u << (int)left) - 1 : 0u;
-                mask &= ~((uint64_t)(((1u << VEC) - 1) & ~keep) << (u * VEC));
-            }
-        }
-    }
+    for (int e = 0; e < VEC; ++e) mask |= head_key(vget<T>(r, e)) >= kmin ? 1u << e : 0u;
+    if (left < VEC) mask &= left > 0 ? (1u << (int)left) - 1 : 0u;
     return mask;
 }
 
-// The chunk of a row held in registers joins the candidates.
-// `least`: keys below it cannot be among the K largest (0: nothing is known yet);
-// returns the same for the chunks behind.  top: the thread's largest value.
+// Too many candidates at once (equal values, mostly: a masked or constant row): the chunk's K-th
+// largest key by bisection over re-reads of the chunk, then what lies above it and the first ones
+// equal to it in the order of their indices.
 template <typename T, int TH, int U>
-__device__ __forceinline__ uint32_t head_top_chunk(HeadTopLds<TH> &s, const T *row, const v4u (&r)[U], float top, int K,
-                                                   int first, int end, int limit, uint32_t least) {
+__device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<T> &z, int K, int first, int end, int stop,
+                                                         uint32_t least, int held) {
     constexpr int VEC = Elem<T>::VEC;
     const int tid = threadIdx.x;
-    const bool edge = first + U * TH > limit / VEC || first + U * TH > end;
-    const int stop = (int)min((long long)limit, (long long)end * VEC);  // elements of this call's vectors end here
-    if (least == 0 && K <= TH) {
-        // The K-th largest of the threads' own maxima bounds the K-th largest from below.
-        // (a maximum of -inf may stand for nothing but NaN: it vouches for no more than that)
-        const bool any = (long long)(first + tid) * VEC < stop;
-        const uint32_t k = !any ? 0u : top > -__builtin_inff() ? head_key(top) : kKeyNaN;
-        if (tid == 0) s.pick = 0;
-        s.keys[tid] = k;
-        __syncthreads();
-        int above = 0;
-        for (int j = 0; j < TH; ++j) {
-            const uint32_t o = s.keys[j];
-            above += o > k || (o == k && j < tid) ? 1 : 0;
-        }
-        if (above == K - 1) s.pick = k;
-        __syncthreads();
-        least = s.pick;
+    auto mask = [&](int u, uint32_t k) {
+        v4u r[1];
+        head_load<T, 1>(z, first + u * TH, TH, tid, end, r);
+        return head_mask<T>(r[0], k, (long long)stop - (long long)(first + u * TH + tid) * VEC);
+    };
+    auto count = [&](uint32_t k) {
+        int n = 0, total;
+#pragma unroll 1
+        for (int u = 0; u < U; ++u) n += __popc(mask(u, k));
+        head_prefix<TH>(n, total, s.wave);
+        return total;
+    };
+    uint32_t lo = least, hi = 0xffffffffu;  // count(lo) >= K > count(hi)
+    if (count(lo + 1) < K) hi = lo + 1;     // rows of one value, and, in two more counts, masked ones
+    if (hi - lo > 1 && lo < kKeyNegInf && count(kKeyNegInf + 1) < K) hi = kKeyNegInf + 1;
+    if (hi - lo > 1 && hi == kKeyNegInf + 1 && count(kKeyNegInf) >= K) lo = kKeyNegInf;
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (count(mid) >= K) lo = mid;
+        else hi = mid;
     }
-    const uint64_t mask = head_mask<T, U>(r, least, first, TH, tid, stop, edge);
-    int total;
-    const int held = s.n;
-    int at = held + head_prefix<TH>(__popcll(mask), total, s.wave);  // (its barriers order the read of s.n before the write below)
-    if (held + total <= kHeadCap) {
-        for (uint64_t left = mask; left; left &= left - 1) {
-            const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
-            s.buf[at++] = head_key64(head_key(to_f32<T>(row[i])), i);
-        }
-        if (tid == 0) s.n = held + total;
-    } else {
-        // Too many (equal values, mostly): find the chunk's K-th largest key by bisection, take
-        // what lies above it, then the first ones equal to it in the order of their indices.
-        auto count = [&](uint32_t k) {
-            int t;
-            head_prefix<TH>(__popcll(head_mask<T, U>(r, k, first, TH, tid, stop, edge)), t, s.wave);
-            return t;
-        };
-        uint32_t lo = least, hi = 0xffffffffu;  // count(lo) >= K > count(hi)
-        if (count(lo + 1) < K) hi = lo + 1;     // rows of one value, and, in two more counts, masked ones
-        if (hi - lo > 1 && lo < kKeyNegInf && count(kKeyNegInf + 1) < K) hi = kKeyNegInf + 1;
-        if (hi - lo > 1 && hi == kKeyNegInf + 1 && count(kKeyNegInf) >= K) lo = kKeyNegInf;
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (count(mid) >= K) lo = mid;
-            else hi = mid;
-        }
-        const uint64_t over = head_mask<T, U>(r, hi, first, TH, tid, stop, edge);
-        const uint64_t equal = head_mask<T, U>(r, lo, first, TH, tid, stop, edge) & ~over;
-        at = held + head_prefix<TH>(__popcll(over), total, s.wave);
-        for (uint64_t left = over; left; left &= left - 1) {
-            const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
-            s.buf[at++] = head_key64(head_key(to_f32<T>(row[i])), i);
-        }
-        int have = held + total, want = K - total;
-        for (int u = 0; u < U && want > 0; ++u) {  // (vectors u of all threads precede vectors u + 1)
-            uint64_t mine = equal >> (u * VEC) & ((1u << VEC) - 1);
-            const int before = head_prefix<TH>(__popcll(mine), total, s.wave);
-            for (int q = before; mine && q < want; mine &= mine - 1, ++q) {
-                const int b = __builtin_ctzll(mine);
-                s.buf[have + q] = head_key64(lo, (first + u * TH + tid) * VEC + b);
+    int have = held, want = K;
+    // above first, then the equal ones (vectors u of all threads precede vectors u + 1)
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass)
+#pragma unroll 1
+        for (int u = 0; u < U && want > 0; ++u) {
+            uint32_t mine = mask(u, pass ? lo : hi);
+            if (pass) mine &= ~mask(u, hi);
+            int total;
+            int q = head_prefix<TH>(__popc(mine), total, s.wave);
+            for (; mine && q < want; mine &= mine - 1, ++q) {
+                const int i = (first + u * TH + tid) * VEC + __builtin_ctz(mine);
+                s.buf[have + q] = head_key64(head_key(to_f32<T>(z.p[i])), i);
             }
             have += min(total, want);
             want -= min(total, want);
         }
-        if (tid == 0) s.n = have;
+    __syncthreads();
+    if (tid == 0) s.n = have;
+    __syncthreads();
+}
+
+// The chunk of a row held in registers joins the candidates.  top: the thread's largest value of the row
+// so far.  bound: at least K elements of the row reach it (0: nothing is known); least: smaller keys of
+// what comes cannot be among the K largest (the bound, or more where K equal values came before).  Distinct threads hold distinct elements, so a value that K of
+// their maxima reach bounds the K-th largest from below; each wave contributes its share of K.
+template <typename T, int TH, int U>
+__device__ __forceinline__ void head_top_chunk(HeadTopLds<TH> &s, const HeadRow<T> &z, v4u (&r)[U], float top, int K, int first,
+                                               int start, int end, uint32_t &bound, uint32_t &least, int phase) {
+    constexpr int VEC = Elem<T>::VEC, W = TH / 64;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int stop = (int)min((long long)z.V, (long long)end * VEC);  // this call's elements end here
+    if (K <= TH) {
+        // (a maximum of -inf may stand for nothing but NaN: it vouches for no more than that)
+        const bool any = (long long)(start + tid) * VEC < stop;
+        uint32_t k = head_wave_kth(!any ? 0u : top > -__builtin_inff() ? head_key(top) : kKeyNaN, (K + W - 1) / W);
+        if constexpr (W > 1) {
+            if (lane == 0) s.kth[phase & 1][tid >> 6] = k;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < W; ++w) k = min(k, s.kth[phase & 1][w]);
+        }
+        bound = max(bound, k);
+        least = max(least, k);
     }
-    head_rank<TH>(s, K);
-    // later elements have higher indices: only larger values can displace the K-th
-    return s.n == K ? (uint32_t)(s.buf[K - 1] >> 32) + 1 : 0u;
+    // this thread's candidates, as a mask over the chunk
+    uint64_t mask = 0;
+    if (least > kKeyNegInf) {
+        const float f = head_unkey(least);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (unpacked anew: kept from the sums, a chunk's values would fill the registers)
+            asm volatile("" : "+v"(r[u]));
+            uint32_t part = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) part |= vget<T>(r[u], e) >= f ? 1u << e : 0u;
+            mask |= (uint64_t)part << (u * VEC);  // (what fills a chunk behind its end is -inf)
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            mask |= (uint64_t)head_mask<T>(r[u], least, (long long)stop - (long long)(first + u * TH + tid) * VEC) << (u * VEC);
+    }
+    const int held = s.n;
+    const int n = __popcll(mask);
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();  // (every thread has read s.n)
+    int at = 0;
+    if (lane == 63 && x) at = atomicAdd(&s.n, x);
+    at = __shfl(at, 63) + x - n;
+    for (uint64_t left = mask; left; left &= left - 1, ++at) {
+        const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
+        if (at < kHeadCap) s.buf[at] = head_key64(head_key(to_f32<T>(z.p[i])), i);
+    }
+    __syncthreads();
+    if (s.n > kHeadCap) head_top_crowd<T, TH, U>(s, z, K, first, end, stop, least, held);
+    if (s.n > kHeadCap / 2) {  // make room; what comes later has to be larger than the K-th
+        head_rank<TH>(s, K, bound);
+        if (s.n == K) {
+            bound = max(bound, (uint32_t)(s.buf[K - 1] >> 32));
+            least = max(least, bound + 1);
+        }
+    }
 }
 
 struct HeadLogprobArgs {
@@ -417,7 +471,7 @@ __device__ __forceinline__ void head_logprobs_finish(const HeadLogprobArgs &a, l
 }
 
 template <typename T, int TH, int U, bool TOP>
-__global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
+__global__ __launch_bounds__(TH, 4) void qhead_logprobs_kernel(HeadLogprobArgs a) {
     __shared__ HeadSums sums[TH / 64];
     __shared__ HeadTopLds<TOP ? TH : 64> top;
     const long long row = blockIdx.x / a.splits;
@@ -425,17 +479,20 @@ __global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     const int end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
     HeadSums t = head_start();
-    uint32_t least = 0;
+    uint32_t bound = 0, least = 0;
+    const int start = sp * a.per;
     if constexpr (TOP) {
         if (tid == 0) top.n = 0;
         __syncthreads();
     }
-    for (int first = sp * a.per; first < end; first += U * TH) {
+    float most = -__builtin_inff();
+    for (int first = start, phase = 0; first < end; first += U * TH, ++phase) {
         v4u r[U];
         head_load<T, U>(z, first, TH, tid, end, r);
-        const float most = head_accumulate<T, U, true, false>(t, r, a.c);
-        if constexpr (TOP) least = head_top_chunk<T, TH, U>(top, z.p, r, most, a.K, first, end, a.V, least);
+        most = fmaxf(most, head_accumulate<T, U, true, false>(t, r, a.c));
+        if constexpr (TOP) head_top_chunk<T, TH, U>(top, z, r, most, a.K, first, start, end, bound, least, phase);
     }
+    if constexpr (TOP) head_rank<TH>(top, a.K, bound);
     t = head_block_join<TH, true, false>(t, a.c, sums);
     const uint64_t *best = nullptr;
     if constexpr (TOP) best = top.buf;
@@ -455,26 +512,26 @@ template <typename T>
 __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
     extern __shared__ uint64_t cand[];  // splits x K
     __shared__ uint64_t best[kHeadTopMax];
-    __shared__ int wave[4];
+    __shared__ int n;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x, K = a.K;
     const HeadSums t = head_join_parts<true, false>(a.part + row * a.splits, a.splits, a.c);
     if (K) {
         const uint64_t *in = a.part_top + row * a.splits * K;
-        uint64_t least = 0;
-        for (int i = 0; i < a.splits; ++i) least = max(least, in[i * K + K - 1]);
-        int n = 0;
-        for (int i0 = 0; i0 < a.splits * K; i0 += 256) {
-            const uint64_t k = i0 + tid < a.splits * K ? in[i0 + tid] : 0;
-            int total;
-            const int at = head_prefix<256>(k != 0 && k >= least ? 1 : 0, total, wave);
-            if (k != 0 && k >= least) cand[n + at] = k;
-            n += total;
+        uint64_t least = (tid & 63) < a.splits ? in[(tid & 63) * K + K - 1] : 0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) least = max(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
+        if (tid == 0) n = 0;
+        __syncthreads();
+        for (int i = tid; i < a.splits * K; i += 256) {
+            const uint64_t k = in[i];
+            if (k != 0 && k >= least) cand[atomicAdd(&n, 1)] = k;
         }
         __syncthreads();
         for (int i = tid; i < n; i += 256) {
             const uint64_t k = cand[i];
             int above = 0;
+#pragma unroll 8
             for (int j = 0; j < n; ++j) above += cand[j] > k ? 1 : 0;
             if (above < K) best[above] = k;
         }
