@@ -30,6 +30,7 @@ constexpr float kHeadFloor = -1e30f;  // stands for -inf in products with a 0 fr
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kHeadTopMax = 128;
+constexpr int kHeadJoinKeys = 2048;  // alternatives of a row's parts together
 
 __device__ __forceinline__ float head_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -119,11 +120,6 @@ __device__ __forceinline__ float head_accumulate(HeadSums &a, const v4u (&r)[U],
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = fmaxf(top, vget<T>(r[u], e));
     if (top > a.m) head_shift<ENT, TWO>(a, top, c);
-    if constexpr (sizeof(T) == 2 && U > 4) {
-        // (unpacked anew below: the values of a long chunk would fill the registers)
-#pragma unroll
-        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(const_cast<v4u &>(r[u])));
-    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -215,67 +211,60 @@ __device__ __forceinline__ float head_unkey(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t head_key64(uint32_t k, int i) { return (uint64_t)k << 32 | (uint32_t)~i; }
 
-constexpr int kHeadCap = 1024;  // candidates a workgroup can hold
+constexpr int kHeadCap = 1024;    // candidates (and blocks that may hold some) a workgroup can list
+constexpr int kHeadGroups = 16;   // blocks a thread's share of a row is divided into at most
 
 template <int TH> struct HeadTopLds {
-    uint64_t buf[kHeadCap];      // candidates; after head_rank the best ones in front, in order
-    uint64_t best[kHeadTopMax];
-    uint32_t kth[2][TH / 64];
+    union {
+        uint16_t top[kHeadGroups * TH];  // the upper halves of the blocks' largest keys, while the row is read
+        uint64_t buf[kHeadCap];          // candidates
+    };
+    uint64_t best[kHeadTopMax];          // the K best in order
+    uint16_t block[kHeadCap];
+    uint32_t kth[TH / 64];
     int wave[TH / 64];
-    int n;                       // candidates found (those past kHeadCap were not kept)
+    int n, blocks;                       // candidates and blocks found (those past kHeadCap were not kept)
 };
 
-// A key that at least j lanes of the wave reach, and no smaller one of 16 bits would miss: bits
-// are set from the top while j lanes stay at or above.  (The lower 16 bits stay 0: bf16 values have
-// none, and for fp32 a bound slightly too low only costs candidates.)
-__device__ __forceinline__ uint32_t head_wave_kth(uint32_t key, int j) {
+// The largest key of 16 bits that at least j of the wave's 64 x N keys reach: bits are set from the top
+// while j stay at or above.  (The lower 16 bits stay 0: bf16 values have none, and for fp32 a bound
+// slightly too low only costs candidates.)
+template <int N> __device__ __forceinline__ uint32_t head_wave_kth(const uint32_t (&key)[N], int j) {
     uint32_t t = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t up = t | 1u << bit;
-        if (__popcll(__ballot(key >= up)) >= j) t = up;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= up));
+        if (n >= j) t = up;
     }
     return t;
 }
 
-// Ranks the candidates at or above `least` by counting the larger ones: buf[0 .. min(n, K)) is
-// then the best in order.
-template <int TH> __device__ __forceinline__ void head_rank(HeadTopLds<TH> &s, int K, uint32_t least) {
-    __syncthreads();
-    const int n = s.n;
-    constexpr int PER = (kHeadCap + TH - 1) / TH;
-    // drop what later bounds ruled out, so that the counting below is about few
-    uint64_t mine[PER];
-    int kept = 0;
+// Where this thread's `v` items go in a list of *n: the wave's sum is added once.
+__device__ __forceinline__ int head_append(int v, int *n) {
+    const int lane = threadIdx.x & 63;
+    int x = v;
 #pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        const int i = q * TH + threadIdx.x;
-        mine[q] = i < n ? s.buf[i] : 0;
-        if ((uint32_t)(mine[q] >> 32) < least) mine[q] = 0;
-        kept += mine[q] != 0 ? 1 : 0;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) s.n = 0;
-    __syncthreads();
-    if (kept) {
-        int at = atomicAdd(&s.n, kept);
-#pragma unroll
-        for (int q = 0; q < PER; ++q)
-            if (mine[q]) s.buf[at++] = mine[q];
-    }
-    __syncthreads();
-    const int m = s.n;
+    int at = 0;
+    if (lane == 63 && x) at = atomicAdd(n, x);
+    return __shfl(at, 63) + x - v;
+}
+
+// best: the K largest of the m keys, in order, by counting the larger ones of each.
+template <int TH> __device__ __forceinline__ void head_rank(const uint64_t *keys, int m, uint64_t *best, int K) {
     for (int i = threadIdx.x; i < m; i += TH) {
-        const uint64_t k = s.buf[i];
+        const uint64_t k = keys[i];
         int above = 0;
 #pragma unroll 8
-        for (int j = 0; j < m; ++j) above += s.buf[j] > k ? 1 : 0;
-        if (above < K) s.best[above] = k;
+        for (int j = 0; j < m; ++j) above += keys[j] > k ? 1 : 0;
+        if (above < K) best[above] = k;
     }
-    __syncthreads();
-    const int best = min(m, K);
-    for (int i = threadIdx.x; i < best; i += TH) s.buf[i] = s.best[i];
-    if (threadIdx.x == 0) s.n = best;
     __syncthreads();
 }
 
@@ -300,33 +289,32 @@ template <int TH> __device__ __forceinline__ int head_prefix(int v, int &total, 
     return before + x - v;
 }
 
-// The elements of a vector whose key is at least kmin, as a bit mask, of the first `left` ones.
-template <typename T> __device__ __forceinline__ uint32_t head_mask(const v4u &r, uint32_t kmin, long long left) {
+// The elements of vector j of a row whose key is at least kmin, as a bit mask; none from vector `end` on.
+template <typename T> __device__ __forceinline__ uint32_t head_mask(const HeadRow<T> &z, int j, int end, uint32_t kmin) {
     constexpr int VEC = Elem<T>::VEC;
+    if (j >= end) return 0;
+    const v4u r = j < z.nfull ? z.load(j) : z.partial();
     uint32_t mask = 0;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) mask |= head_key(vget<T>(r, e)) >= kmin ? 1u << e : 0u;
-    if (left < VEC) mask &= left > 0 ? (1u << (int)left) - 1 : 0u;
-    return mask;
+    return j < z.nfull ? mask : mask & ((1u << (z.V - z.nfull * VEC)) - 1);
 }
 
-// Too many candidates at once (equal values, mostly: a masked or constant row): the chunk's K-th
-// largest key by bisection over re-reads of the chunk, then what lies above it and the first ones
-// equal to it in the order of their indices.
-template <typename T, int TH, int U>
-__device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<T> &z, int K, int first, int end, int stop,
-                                                         uint32_t least, int held) {
+template <typename T> __device__ __forceinline__ uint64_t head_key_at(const HeadRow<T> &z, int i) {
+    return head_key64(head_key(to_f32<T>(z.p[i])), i);
+}
+
+// Too many candidates (equal values, mostly: a masked or constant row): the K-th largest key of the
+// vectors [start, end) by bisection over re-reads, then what lies above it and the first ones equal
+// to it in the order of their indices.  Leaves K candidates.
+template <typename T, int TH>
+__device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<T> &z, int K, int start, int end, uint32_t least) {
     constexpr int VEC = Elem<T>::VEC;
     const int tid = threadIdx.x;
-    auto mask = [&](int u, uint32_t k) {
-        v4u r[1];
-        head_load<T, 1>(z, first + u * TH, TH, tid, end, r);
-        return head_mask<T>(r[0], k, (long long)stop - (long long)(first + u * TH + tid) * VEC);
-    };
     auto count = [&](uint32_t k) {
         int n = 0, total;
 #pragma unroll 1
-        for (int u = 0; u < U; ++u) n += __popc(mask(u, k));
+        for (int j = start + tid; j < end; j += TH) n += __popc(head_mask<T>(z, j, end, k));
         head_prefix<TH>(n, total, s.wave);
         return total;
     };
@@ -339,94 +327,63 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
         if (count(mid) >= K) lo = mid;
         else hi = mid;
     }
-    int have = held, want = K;
-    // above first, then the equal ones (vectors u of all threads precede vectors u + 1)
+    int have = 0, total;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass)
 #pragma unroll 1
-        for (int u = 0; u < U && want > 0; ++u) {
-            uint32_t mine = mask(u, pass ? lo : hi);
-            if (pass) mine &= ~mask(u, hi);
-            int total;
-            int q = head_prefix<TH>(__popc(mine), total, s.wave);
-            for (; mine && q < want; mine &= mine - 1, ++q) {
-                const int i = (first + u * TH + tid) * VEC + __builtin_ctz(mine);
-                s.buf[have + q] = head_key64(head_key(to_f32<T>(z.p[i])), i);
-            }
-            have += min(total, want);
-            want -= min(total, want);
+        for (int first = start; first < end && have < K; first += TH) {  // (whole passes of TH vectors keep the order)
+            const int j = first + tid;
+            uint32_t mine = head_mask<T>(z, j, end, pass ? lo : hi);
+            if (pass) mine &= ~head_mask<T>(z, j, end, hi);
+            int q = have + head_prefix<TH>(__popc(mine), total, s.wave);
+            for (; mine && q < K; mine &= mine - 1, ++q) s.buf[q] = head_key_at<T>(z, j * VEC + __builtin_ctz(mine));
+            have += total;
         }
     __syncthreads();
-    if (tid == 0) s.n = have;
+    if (tid == 0) s.n = min(have, K);
     __syncthreads();
 }
 
-// The chunk of a row held in registers joins the candidates.  top: the thread's largest value of the row
-// so far.  bound: at least K elements of the row reach it (0: nothing is known); least: smaller keys of
-// what comes cannot be among the K largest (the bound, or more where K equal values came before).  Distinct threads hold distinct elements, so a value that K of
-// their maxima reach bounds the K-th largest from below; each wave contributes its share of K.
-template <typename T, int TH, int U>
-__device__ __forceinline__ void head_top_chunk(HeadTopLds<TH> &s, const HeadRow<T> &z, v4u (&r)[U], float top, int K, int first,
-                                               int start, int end, uint32_t &bound, uint32_t &least, int phase) {
+// The K largest of vectors [start, end) of a row, into s.best.  While they were read, s.top got the upper
+// halves of the largest keys of blocks of `rows` x one vector a thread; quarter[i]: the thread's largest
+// value in blocks i mod 4.  These maxima belong to distinct elements, so a value that K of them reach
+// (each wave contributing its share of K) bounds the K-th largest from below; only blocks that reach
+// it are read again: a little more than K of them, whatever the row's length.
+template <typename T, int TH>
+__device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z, const float (&quarter)[4], int K, int start,
+                                         int end, int rows) {
     constexpr int VEC = Elem<T>::VEC, W = TH / 64;
     const int tid = threadIdx.x, lane = tid & 63;
-    const int stop = (int)min((long long)z.V, (long long)end * VEC);  // this call's elements end here
-    if (K <= TH) {
-        // (a maximum of -inf may stand for nothing but NaN: it vouches for no more than that)
-        const bool any = (long long)(start + tid) * VEC < stop;
-        uint32_t k = head_wave_kth(!any ? 0u : top > -__builtin_inff() ? head_key(top) : kKeyNaN, (K + W - 1) / W);
-        if constexpr (W > 1) {
-            if (lane == 0) s.kth[phase & 1][tid >> 6] = k;
-            __syncthreads();
+    uint32_t key[4];
 #pragma unroll
-            for (int w = 0; w < W; ++w) k = min(k, s.kth[phase & 1][w]);
-        }
-        bound = max(bound, k);
-        least = max(least, k);
-    }
-    // this thread's candidates, as a mask over the chunk
-    uint64_t mask = 0;
-    if (least > kKeyNegInf) {
-        const float f = head_unkey(least);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            // (unpacked anew: kept from the sums, a chunk's values would fill the registers)
-            asm volatile("" : "+v"(r[u]));
-            uint32_t part = 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) part |= vget<T>(r[u], e) >= f ? 1u << e : 0u;
-            mask |= (uint64_t)part << (u * VEC);  // (what fills a chunk behind its end is -inf)
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            mask |= (uint64_t)head_mask<T>(r[u], least, (long long)stop - (long long)(first + u * TH + tid) * VEC) << (u * VEC);
-    }
-    const int held = s.n;
-    const int n = __popcll(mask);
-    int x = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();  // (every thread has read s.n)
-    int at = 0;
-    if (lane == 63 && x) at = atomicAdd(&s.n, x);
-    at = __shfl(at, 63) + x - n;
-    for (uint64_t left = mask; left; left &= left - 1, ++at) {
-        const int b = __builtin_ctzll(left), i = (first + (b / VEC) * TH + tid) * VEC + b % VEC;
-        if (at < kHeadCap) s.buf[at] = head_key64(head_key(to_f32<T>(z.p[i])), i);
-    }
+    for (int i = 0; i < 4; ++i)  // (a maximum of -inf may stand for nothing, or for NaN: it vouches for neither)
+        key[i] = quarter[i] > -__builtin_inff() ? head_key(quarter[i]) : 0u;
+    uint32_t least = head_wave_kth(key, (K + W - 1) / W);
+    if (lane == 0) s.kth[tid >> 6] = least;
+    if (tid == 0) s.n = s.blocks = 0;
     __syncthreads();
-    if (s.n > kHeadCap) head_top_crowd<T, TH, U>(s, z, K, first, end, stop, least, held);
-    if (s.n > kHeadCap / 2) {  // make room; what comes later has to be larger than the K-th
-        head_rank<TH>(s, K, bound);
-        if (s.n == K) {
-            bound = max(bound, (uint32_t)(s.buf[K - 1] >> 32));
-            least = max(least, bound + 1);
+#pragma unroll
+    for (int w = 0; w < W; ++w) least = min(least, s.kth[w]);
+    uint32_t mask = 0;
+    for (int g = 0; start + g * rows * TH + tid < end; ++g) mask |= s.top[g * TH + tid] >= least >> 16 ? 1u << g : 0u;
+    int at = head_append(__popc(mask), &s.blocks);
+    for (; mask; mask &= mask - 1, ++at)
+        if (at < kHeadCap) s.block[at] = (uint16_t)(__builtin_ctz(mask) * TH + tid);
+    __syncthreads();
+    const int blocks = s.blocks;
+    if (blocks <= kHeadCap) {
+        for (int q = tid; q < blocks * rows; q += TH) {
+            const int b = s.block[q / rows], j = start + (b / TH * rows + q % rows) * TH + b % TH;
+            uint32_t mine = head_mask<T>(z, j, end, least);
+            if (!mine) continue;
+            int to = atomicAdd(&s.n, __popc(mine));
+            for (; mine; mine &= mine - 1, ++to)
+                if (to < kHeadCap) s.buf[to] = head_key_at<T>(z, j * VEC + __builtin_ctz(mine));
         }
+        __syncthreads();
     }
+    if (blocks > kHeadCap || s.n > kHeadCap) head_top_crowd<T, TH>(s, z, K, start, end, least);
+    head_rank<TH>(s.buf, s.n, s.best, K);
 }
 
 struct HeadLogprobArgs {
@@ -442,18 +399,26 @@ struct HeadLogprobArgs {
     uint64_t *part_top;  // rows x splits x K
 };
 
-// What a row's statistics say of it (whole workgroup; s: the best K in front of buf).
+// A row's target and its logit (0: none, or past the vocabulary), requested early.
+struct HeadTarget {
+    int64_t id;
+    float z;
+};
+template <typename T> __device__ __forceinline__ HeadTarget head_target(const HeadLogprobArgs &a, long long row) {
+    const int64_t id = a.target[row];
+    return {id, id >= 0 && id < a.V ? to_f32<T>((static_cast<const T *>(a.z) + row * a.ld)[id]) : 0.0f};
+}
+
+// What a row's statistics say of it (whole workgroup; best: its K largest keys in order).
 template <typename T, int TH>
 __device__ __forceinline__ void head_logprobs_finish(const HeadLogprobArgs &a, long long row, const HeadSums &t,
-                                                     const uint64_t *best) {
-    const T *z = static_cast<const T *>(a.z) + row * a.ld;
+                                                     const uint64_t *best, const HeadTarget &g) {
     const float ls = logf(t.s);  // -inf for an empty row
     const bool empty = t.s == 0.0f;
     if (threadIdx.x == 0) {
-        const int64_t g = a.target[row];
         float lp = 0.0f;
-        if (g >= a.V) lp = __builtin_nanf("");
-        else if (g >= 0) lp = empty ? -__builtin_inff() : head_scaled_diff(to_f32<T>(z[g]), t.m, a.inv_t) - ls;
+        if (g.id >= a.V) lp = __builtin_nanf("");
+        else if (g.id >= 0) lp = empty ? -__builtin_inff() : head_scaled_diff(g.z, t.m, a.inv_t) - ls;
         a.logp[row] = lp;
         if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - kLn2 * (t.d / t.s);
         if (a.lse) a.lse[row] = empty ? -__builtin_inff() : t.m * a.inv_t + ls;
@@ -471,33 +436,45 @@ __device__ __forceinline__ void head_logprobs_finish(const HeadLogprobArgs &a, l
 }
 
 template <typename T, int TH, int U, bool TOP>
-__global__ __launch_bounds__(TH, 4) void qhead_logprobs_kernel(HeadLogprobArgs a) {
+__global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
     __shared__ HeadSums sums[TH / 64];
     __shared__ HeadTopLds<TOP ? TH : 64> top;
     const long long row = blockIdx.x / a.splits;
     const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     const int end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
+    const HeadTarget g = head_target<T>(a, row);
     HeadSums t = head_start();
-    uint32_t bound = 0, least = 0;
     const int start = sp * a.per;
     if constexpr (TOP) {
-        if (tid == 0) top.n = 0;
-        __syncthreads();
+        const int steps = (end - start + U * TH - 1) / (U * TH), group = (steps + kHeadGroups - 1) / kHeadGroups;
+        float quarter[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+        for (int step = 0, b = 0; step < steps; step += group, ++b) {
+            float here = -__builtin_inff();
+            for (int i = step; i < min(step + group, steps); ++i) {
+                v4u r[U];
+                head_load<T, U>(z, start + i * U * TH, TH, tid, end, r);
+                here = fmaxf(here, head_accumulate<T, U, true, false>(t, r, a.c));
+            }
+            // (NaN apart, which ranks behind everything and is found where all of a block counts)
+            top.top[b * TH + tid] = (uint16_t)((here > -__builtin_inff() ? head_key(here) : kKeyNegInf) >> 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((b & 3) == i) quarter[i] = fmaxf(quarter[i], here);
+        }
+        head_top<T, TH>(top, z, quarter, a.K, start, end, group * U);
+    } else {
+        for (int first = start; first < end; first += U * TH) {
+            v4u r[U];
+            head_load<T, U>(z, first, TH, tid, end, r);
+            head_accumulate<T, U, true, false>(t, r, a.c);
+        }
     }
-    float most = -__builtin_inff();
-    for (int first = start, phase = 0; first < end; first += U * TH, ++phase) {
-        v4u r[U];
-        head_load<T, U>(z, first, TH, tid, end, r);
-        most = fmaxf(most, head_accumulate<T, U, true, false>(t, r, a.c));
-        if constexpr (TOP) head_top_chunk<T, TH, U>(top, z, r, most, a.K, first, start, end, bound, least, phase);
-    }
-    if constexpr (TOP) head_rank<TH>(top, a.K, bound);
     t = head_block_join<TH, true, false>(t, a.c, sums);
     const uint64_t *best = nullptr;
-    if constexpr (TOP) best = top.buf;
+    if constexpr (TOP) best = top.best;
     if (a.splits == 1) {
-        head_logprobs_finish<T, TH>(a, row, t, best);
+        head_logprobs_finish<T, TH>(a, row, t, best, g);
         return;
     }
     const long long at = row * a.splits + sp;
@@ -507,37 +484,40 @@ __global__ __launch_bounds__(TH, 4) void qhead_logprobs_kernel(HeadLogprobArgs a
 }
 
 // Joins the parts of a row: the K-th key of any part bounds the row's K-th from
-// below, so only what reaches the largest of those is ranked.
+// below, so only what reaches the largest of those is ranked.  Everything is requested from
+// memory at once (one after the other, the latencies made up most of 15 us).
 template <typename T>
 __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
     extern __shared__ uint64_t cand[];  // splits x K
-    __shared__ uint64_t best[kHeadTopMax];
+    __shared__ uint64_t best[kHeadTopMax], wave[4];
     __shared__ int n;
     const long long row = blockIdx.x;
-    const int tid = threadIdx.x, K = a.K;
+    const int tid = threadIdx.x, K = a.K, keys = a.splits * K;
+    constexpr int PER = kHeadJoinKeys / 256;
+    uint64_t mine[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) mine[q] = tid + q * 256 < keys ? a.part_top[row * keys + tid + q * 256] : 0;
+    const HeadTarget g = head_target<T>(a, row);
     const HeadSums t = head_join_parts<true, false>(a.part + row * a.splits, a.splits, a.c);
     if (K) {
-        const uint64_t *in = a.part_top + row * a.splits * K;
-        uint64_t least = (tid & 63) < a.splits ? in[(tid & 63) * K + K - 1] : 0;
+        uint64_t least = 0;
+#pragma unroll
+        for (int q = 0; q < PER; ++q)
+            if ((tid + q * 256) % K == K - 1) least = max(least, mine[q]);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) least = max(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
         if (tid == 0) n = 0;
+        if ((tid & 63) == 0) wave[tid >> 6] = least;
         __syncthreads();
-        for (int i = tid; i < a.splits * K; i += 256) {
-            const uint64_t k = in[i];
-            if (k != 0 && k >= least) cand[atomicAdd(&n, 1)] = k;
-        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) least = max(least, wave[w]);
+#pragma unroll
+        for (int q = 0; q < PER; ++q)
+            if (mine[q] != 0 && mine[q] >= least) cand[atomicAdd(&n, 1)] = mine[q];
         __syncthreads();
-        for (int i = tid; i < n; i += 256) {
-            const uint64_t k = cand[i];
-            int above = 0;
-#pragma unroll 8
-            for (int j = 0; j < n; ++j) above += cand[j] > k ? 1 : 0;
-            if (above < K) best[above] = k;
-        }
-        __syncthreads();
+        head_rank<256>(cand, n, best, K);
     }
-    head_logprobs_finish<T, 256>(a, row, t, best);
+    head_logprobs_finish<T, 256>(a, row, t, best, g);
 }
 
 // --- gradients --------------------------------------------------------------------------

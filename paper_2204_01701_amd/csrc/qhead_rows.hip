@@ -39,7 +39,7 @@ Split split_rows(int rows, int nvec, int blocks, int most, int least_per) {
 // A part of a row has two vectors a thread at least.  (Parts of the alternatives' lists
 // together fit the join's 16 KiB.)
 Split logprobs_split(const qhead_rows_desc *d) {
-    const int most = std::min(kHeadMaxSplits, 2048 / std::max(1, d->top));
+    const int most = std::min(kHeadMaxSplits, kHeadJoinKeys / std::max(1, d->top));
     return split_rows(d->rows, vectors(d), 2 * kNumCUs, most, 2 * kRowThreads);
 }
 Split sums_split(const qhead_rows_desc *d) {
@@ -51,12 +51,10 @@ Split grad_split(const qhead_rows_desc *d) { return split_rows(d->rows, vectors(
 template <typename T> void launch_logprobs(const HeadLogprobArgs &a, int rows, hipStream_t st) {
     const dim3 grid((unsigned)((long long)rows * a.splits));
     const int nvec = cdiv(a.V, Elem<T>::VEC);
-    // one wave where a row is at most one vector a lane; else chunks of 2 or 8 vectors a thread
+    // one wave where a row is at most one vector a lane
     if (a.K) {
         if (nvec <= 64) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, true>), grid, dim3(64), 0, st, a);
-        else if (a.per <= 2 * kRowThreads)
-            hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 2, true>), grid, dim3(kRowThreads), 0, st, a);
-        else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 8, true>), grid, dim3(kRowThreads), 0, st, a);
+        else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, true>), grid, dim3(kRowThreads), 0, st, a);
     } else {
         if (nvec <= 64) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, false>), grid, dim3(64), 0, st, a);
         else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, false>), grid, dim3(kRowThreads), 0, st, a);
