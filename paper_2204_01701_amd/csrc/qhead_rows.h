@@ -290,18 +290,25 @@ template <int TH> __device__ __forceinline__ int head_prefix(int v, int &total, 
 }
 
 // The elements of vector j of a row whose key is at least kmin, as a bit mask; none from vector `end` on.
-template <typename T> __device__ __forceinline__ uint32_t head_mask(const HeadRow<T> &z, int j, int end, uint32_t kmin) {
+template <typename T> __device__ __forceinline__ uint32_t head_mask(const HeadRow<T> &z, int j, int end, uint32_t kmin, v4u &r) {
     constexpr int VEC = Elem<T>::VEC;
     if (j >= end) return 0;
-    const v4u r = j < z.nfull ? z.load(j) : z.partial();
+    r = j < z.nfull ? z.load(j) : z.partial();
     uint32_t mask = 0;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) mask |= head_key(vget<T>(r, e)) >= kmin ? 1u << e : 0u;
     return j < z.nfull ? mask : mask & ((1u << (z.V - z.nfull * VEC)) - 1);
 }
+template <typename T> __device__ __forceinline__ uint32_t head_mask(const HeadRow<T> &z, int j, int end, uint32_t kmin) {
+    v4u r;
+    return head_mask<T>(z, j, end, kmin, r);
+}
 
-template <typename T> __device__ __forceinline__ uint64_t head_key_at(const HeadRow<T> &z, int i) {
-    return head_key64(head_key(to_f32<T>(z.p[i])), i);
+// The key of element e of a vector, e known at run time only.
+template <typename T> __device__ __forceinline__ uint64_t head_key_of(const v4u &r, int e, int i) {
+    const int d = sizeof(T) == 2 ? e >> 1 : e;
+    const uint32_t w = d & 2 ? (d & 1 ? r.w : r.z) : (d & 1 ? r.y : r.x);
+    return head_key64(head_key(sizeof(T) == 2 ? __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16) : __uint_as_float(w)), i);
 }
 
 // Too many candidates (equal values, mostly: a masked or constant row): the K-th largest key of the
@@ -333,10 +340,11 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
 #pragma unroll 1
         for (int first = start; first < end && have < K; first += TH) {  // (whole passes of TH vectors keep the order)
             const int j = first + tid;
-            uint32_t mine = head_mask<T>(z, j, end, pass ? lo : hi);
+            v4u r;
+            uint32_t mine = head_mask<T>(z, j, end, pass ? lo : hi, r);
             if (pass) mine &= ~head_mask<T>(z, j, end, hi);
             int q = have + head_prefix<TH>(__popc(mine), total, s.wave);
-            for (; mine && q < K; mine &= mine - 1, ++q) s.buf[q] = head_key_at<T>(z, j * VEC + __builtin_ctz(mine));
+            for (; mine && q < K; mine &= mine - 1, ++q) s.buf[q] = head_key_of<T>(r, __builtin_ctz(mine), j * VEC + __builtin_ctz(mine));
             have += total;
         }
     __syncthreads();
@@ -374,11 +382,12 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
     if (blocks <= kHeadCap) {
         for (int q = tid; q < blocks * rows; q += TH) {
             const int b = s.block[q / rows], j = start + (b / TH * rows + q % rows) * TH + b % TH;
-            uint32_t mine = head_mask<T>(z, j, end, least);
+            v4u r;
+            uint32_t mine = head_mask<T>(z, j, end, least, r);
             if (!mine) continue;
             int to = atomicAdd(&s.n, __popc(mine));
             for (; mine; mine &= mine - 1, ++to)
-                if (to < kHeadCap) s.buf[to] = head_key_at<T>(z, j * VEC + __builtin_ctz(mine));
+                if (to < kHeadCap) s.buf[to] = head_key_of<T>(r, __builtin_ctz(mine), j * VEC + __builtin_ctz(mine));
         }
         __syncthreads();
     }
@@ -483,13 +492,14 @@ __global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
         for (int k = tid; k < a.K; k += TH) a.part_top[at * a.K + k] = k < top.n ? best[k] : 0;
 }
 
-// Joins the parts of a row: the K-th key of any part bounds the row's K-th from
-// below, so only what reaches the largest of those is ranked.  Everything is requested from
+// Joins the parts of a row: what K of the parts' alternatives reach bounds the row's K-th from
+// below, and only the alternatives that reach it are ranked.  Everything is requested from
 // memory at once (one after the other, the latencies made up most of 15 us).
 template <typename T>
 __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
     extern __shared__ uint64_t cand[];  // splits x K
-    __shared__ uint64_t best[kHeadTopMax], wave[4];
+    __shared__ uint64_t best[kHeadTopMax];
+    __shared__ uint32_t wave[4];
     __shared__ int n;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x, K = a.K, keys = a.splits * K;
@@ -500,20 +510,22 @@ __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArg
     const HeadTarget g = head_target<T>(a, row);
     const HeadSums t = head_join_parts<true, false>(a.part + row * a.splits, a.splits, a.c);
     if (K) {
-        uint64_t least = 0;
+        uint32_t key[PER];
 #pragma unroll
-        for (int q = 0; q < PER; ++q)
-            if ((tid + q * 256) % K == K - 1) least = max(least, mine[q]);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) least = max(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
+        for (int q = 0; q < PER; ++q) key[q] = (uint32_t)(mine[q] >> 32);
+        uint32_t least = head_wave_kth(key, (K + 3) / 4);
         if (tid == 0) n = 0;
         if ((tid & 63) == 0) wave[tid >> 6] = least;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) least = max(least, wave[w]);
+        for (int w = 0; w < 4; ++w) least = min(least, wave[w]);
+        int kept = 0;
+#pragma unroll
+        for (int q = 0; q < PER; ++q) kept += mine[q] != 0 && key[q] >= least ? 1 : 0;
+        int at = head_append(kept, &n);
 #pragma unroll
         for (int q = 0; q < PER; ++q)
-            if (mine[q] != 0 && mine[q] >= least) cand[atomicAdd(&n, 1)] = mine[q];
+            if (mine[q] != 0 && key[q] >= least) cand[at++] = mine[q];
         __syncthreads();
         head_rank<256>(cand, n, best, K);
     }
