@@ -112,7 +112,7 @@ __device__ __forceinline__ void head_join(HeadSums &a, HeadSums b, float c) {
 
 // The sums of U vectors held in registers; returns their maximum.
 template <typename T, int U, bool ENT, bool TWO>
-__device__ __forceinline__ float head_accumulate(HeadSums &a, const v4u (&r)[U], float c) {
+__device__ __forceinline__ float head_accumulate(HeadSums &a, v4u (&r)[U], float c) {
     constexpr int VEC = Elem<T>::VEC;
     float top = -__builtin_inff();
 #pragma unroll
@@ -120,6 +120,11 @@ __device__ __forceinline__ float head_accumulate(HeadSums &a, const v4u (&r)[U],
 #pragma unroll
         for (int e = 0; e < VEC; ++e) top = fmaxf(top, vget<T>(r[u], e));
     if (top > a.m) head_shift<ENT, TWO>(a, top, c);
+    if constexpr (U >= 8) {
+        // (unpacked anew: kept from above, the values of so many vectors would fill the registers)
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(r[u]));
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -168,32 +173,6 @@ __device__ __forceinline__ HeadSums head_block_join(HeadSums a, float c, HeadSum
     return a;
 }
 
-template <int TH> __device__ __forceinline__ float head_block_max(float v, float *lds) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    if constexpr (TH == 64) return v;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int w = 1; w < TH / 64; ++w) v = fmaxf(v, lds[w]);
-    return v;
-}
-
-template <int TH> __device__ __forceinline__ float head_block_sum(float v, float *lds) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    if constexpr (TH == 64) return v;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int w = 1; w < TH / 64; ++w) v += lds[w];
-    return v;
-}
-
 // --- the K largest ------------------------------------------------------------------
 // An element's key: its value's bits in an order that unsigned integers share, over the
 // complement of its index, so that equal values rank by the lower index and no two
@@ -211,19 +190,21 @@ __device__ __forceinline__ float head_unkey(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t head_key64(uint32_t k, int i) { return (uint64_t)k << 32 | (uint32_t)~i; }
 
-constexpr int kHeadCap = 1024;    // candidates (and blocks that may hold some) a workgroup can list
+// Candidates (and blocks that may hold some) a workgroup can list.
+constexpr int head_cap(int threads) { return threads == 64 ? 512 : 1024; }
 constexpr int kHeadGroups = 16;   // blocks a thread's share of a row is divided into at most
 
 template <int TH> struct HeadTopLds {
+    static constexpr int CAP = head_cap(TH);
     union {
         uint16_t top[kHeadGroups * TH];  // the upper halves of the blocks' largest keys, while the row is read
-        uint64_t buf[kHeadCap];          // candidates
+        uint64_t buf[CAP];               // candidates
     };
     uint64_t best[kHeadTopMax];          // the K best in order
-    uint16_t block[kHeadCap];
+    uint16_t block[CAP];
     uint32_t kth[TH / 64];
     int wave[TH / 64];
-    int n, blocks;                       // candidates and blocks found (those past kHeadCap were not kept)
+    int n, blocks;                       // candidates and blocks found (those past CAP were not kept)
 };
 
 // The largest key of 16 bits that at least j of the wave's 64 x N keys reach: bits are set from the top
@@ -360,7 +341,7 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
 template <typename T, int TH>
 __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z, const float (&quarter)[4], int K, int start,
                                          int end, int rows) {
-    constexpr int VEC = Elem<T>::VEC, W = TH / 64;
+    constexpr int VEC = Elem<T>::VEC, W = TH / 64, CAP = head_cap(TH);
     const int tid = threadIdx.x, lane = tid & 63;
     uint32_t key[4];
 #pragma unroll
@@ -376,10 +357,10 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
     for (int g = 0; start + g * rows * TH + tid < end; ++g) mask |= s.top[g * TH + tid] >= least >> 16 ? 1u << g : 0u;
     int at = head_append(__popc(mask), &s.blocks);
     for (; mask; mask &= mask - 1, ++at)
-        if (at < kHeadCap) s.block[at] = (uint16_t)(__builtin_ctz(mask) * TH + tid);
+        if (at < CAP) s.block[at] = (uint16_t)(__builtin_ctz(mask) * TH + tid);
     __syncthreads();
     const int blocks = s.blocks;
-    if (blocks <= kHeadCap) {
+    if (blocks <= CAP) {
         for (int q = tid; q < blocks * rows; q += TH) {
             const int b = s.block[q / rows], j = start + (b / TH * rows + q % rows) * TH + b % TH;
             v4u r;
@@ -387,11 +368,11 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
             if (!mine) continue;
             int to = atomicAdd(&s.n, __popc(mine));
             for (; mine; mine &= mine - 1, ++to)
-                if (to < kHeadCap) s.buf[to] = head_key_of<T>(r, __builtin_ctz(mine), j * VEC + __builtin_ctz(mine));
+                if (to < CAP) s.buf[to] = head_key_of<T>(r, __builtin_ctz(mine), j * VEC + __builtin_ctz(mine));
         }
         __syncthreads();
     }
-    if (blocks > kHeadCap || s.n > kHeadCap) head_top_crowd<T, TH>(s, z, K, start, end, least);
+    if (blocks > CAP || s.n > CAP) head_top_crowd<T, TH>(s, z, K, start, end, least);
     head_rank<TH>(s.buf, s.n, s.best, K);
 }
 
@@ -628,141 +609,203 @@ struct HeadDistillArgs {
     void *dz;
 };
 
-// The few places of a row whose gradient has more than the probabilities: the teacher's
-// (place k on thread k) and the label (on thread K).
+// The few places of a row whose gradient has more than the probabilities: the teacher's K and, as
+// place K, the label.  The first wave holds them, place lane + 64 i on a lane, so that they need no
+// barriers of their own; what the other waves need of them goes through LDS with the row's sums.
+constexpr int kHeadPlaces = (kHeadTopMax + 64) / 64;
 struct HeadPlaces {
-    float q, zt, logq;  // the place's probability, its student logit and log q
-    int id;             // -1: none
-    float has_q, has_l; // the row has a teacher's term, a label's (0 or 1)
-    bool wrong;         // an id or label past the vocabulary
+    float q[kHeadPlaces], zt[kHeadPlaces], logq[kHeadPlaces];  // probability, student logit, log q
+    int id[kHeadPlaces];                                       // -1: none
+    float has_q, has_l;  // the row has a teacher's term, a label's (0 or 1)
+    bool wrong;          // an id or label past the vocabulary
 };
 
 template <int TH> struct HeadDistillLds {
     HeadSums sums[TH / 64];
-    float red[TH / 64];
     float q[kHeadTopMax + 1];
     int id[kHeadTopMax + 1];
+    float has_q, has_l;
 };
 
+// (first wave)
 template <typename T, int TH>
 __device__ __forceinline__ HeadPlaces head_places(const HeadDistillArgs &a, long long row, const T *z, HeadDistillLds<TH> &s) {
-    const int tid = threadIdx.x;
-    HeadPlaces p{0.0f, 0.0f, 0.0f, -1, 0.0f, 0.0f, false};
-    float t = -__builtin_inff();
-    bool wrong = false, there = false;
-    if (tid < a.K && a.alpha != 0.0f) {
-        const int64_t id = a.ids[row * a.K + tid];
-        if (id >= 0) {
-            t = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + tid]);
-            there = true;
-            if (id < a.V) p.id = (int)id;
-            else wrong = true;
+    const int lane = threadIdx.x;
+    HeadPlaces p;
+    float t[kHeadPlaces], most = -__builtin_inff();
+    bool wrong = false, label = false;
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        const int k = lane + 64 * i;
+        p.q[i] = p.zt[i] = p.logq[i] = 0.0f;
+        p.id[i] = -1;
+        t[i] = -__builtin_inff();
+        if (64 * i > a.K) continue;
+        int64_t id = -1;
+        if (k < a.K) {
+            id = a.ids[row * a.K + k];
+            if (id >= 0) t[i] = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + k]);
+        } else if (k == a.K && a.label) {
+            id = a.label[row];
+            label = id >= 0 && id < a.V;
         }
-    } else if (tid == a.K && a.label && a.alpha != 1.0f) {
-        const int64_t id = a.label[row];
-        if (id >= 0 && id < a.V) p.id = (int)id;
-        wrong = id >= a.V;
+        wrong = wrong || id >= a.V;
+        if (id >= 0 && id < a.V) {
+            p.id[i] = (int)id;
+            p.zt[i] = to_f32<T>(z[id]);
+        }
+        most = fmaxf(most, t[i]);
     }
-    if (p.id >= 0) p.zt = to_f32<T>(z[p.id]);
-    const float most = head_block_max<TH>(t, s.red);
-    const float x = (t - most) * a.inv_t, e = there && t != -__builtin_inff() ? expf(x) : 0.0f;
-    const float sum = head_block_sum<TH>(e, s.red);
-    if (tid < a.K) {
-        p.q = sum != 0.0f ? e / sum : 0.0f;  // (no place, or all of probability 0: the row has no teacher's term)
-        p.logq = x - logf(sum);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        p.logq[i] = (t[i] - most) * a.inv_t;
+        p.q[i] = t[i] != -__builtin_inff() ? expf(p.logq[i]) : 0.0f;  // (-inf: an empty place, or one of probability 0)
+        sum += p.q[i];
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    const float ls = logf(sum);
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        p.q[i] = sum != 0.0f ? p.q[i] / sum : 0.0f;
+        p.logq[i] -= ls;
+        const int k = lane + 64 * i;
+        if (k <= a.K) {
+            s.q[k] = p.q[i];
+            s.id[k] = p.id[i];
+        }
     }
     p.has_q = sum != 0.0f ? 1.0f : 0.0f;
-    p.wrong = head_block_max<TH>(wrong ? 1.0f : 0.0f, s.red) != 0.0f;
-    if (tid <= a.K) {
-        s.q[tid] = p.q;
-        s.id[tid] = p.id;
+    p.has_l = __ballot(label) != 0 ? 1.0f : 0.0f;
+    p.wrong = __ballot(wrong) != 0;
+    if (lane == 0) {
+        s.has_q = p.has_q;
+        s.has_l = p.has_l;
     }
-    __syncthreads();
-    p.has_l = s.id[a.K] >= 0 ? 1.0f : 0.0f;
     return p;
 }
 
-// The row's loss, on every thread.
-template <int TH>
-__device__ __forceinline__ float head_distill_loss(const HeadDistillArgs &a, const HeadPlaces &p, const HeadSums &t,
-                                                   HeadDistillLds<TH> &s) {
-    const int tid = threadIdx.x;
+// The row's loss (first wave).
+__device__ __forceinline__ float head_distill_loss(const HeadDistillArgs &a, const HeadPlaces &p, const HeadSums &t) {
     float v = 0.0f;
-    if (tid < a.K) {
-        const float lp = t.s == 0.0f ? -__builtin_inff() : head_scaled_diff(p.zt, t.m, a.inv_t) - logf(t.s);
-        if (p.q != 0.0f && p.id >= 0) v = a.alpha * a.temp * a.temp * p.q * (p.logq - lp);
-    } else if (tid == a.K && p.id >= 0) {
-        v = t.s1 == 0.0f ? __builtin_inff() : (1.0f - a.alpha) * (logf(t.s1) - head_scaled_diff(p.zt, t.m, 1.0f));
+    const float ls = logf(t.s);
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        const int k = threadIdx.x + 64 * i;
+        if (p.id[i] < 0) continue;
+        if (k < a.K) {
+            const float lp = t.s == 0.0f ? -__builtin_inff() : head_scaled_diff(p.zt[i], t.m, a.inv_t) - ls;
+            if (p.q[i] != 0.0f) v += a.alpha * a.temp * a.temp * p.q[i] * (p.logq[i] - lp);
+        } else if (k == a.K) {
+            v += t.s1 == 0.0f ? __builtin_inff() : (1.0f - a.alpha) * (logf(t.s1) - head_scaled_diff(p.zt[i], t.m, 1.0f));
+        }
     }
-    v = head_block_sum<TH>(v, s.red);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
     return p.wrong ? __builtin_nanf("") : v;
 }
 
-__device__ __forceinline__ HeadGrad head_distill_coef(const HeadDistillArgs &a, const HeadPlaces &p, float m, float s,
+__device__ __forceinline__ HeadGrad head_distill_coef(const HeadDistillArgs &a, float has_q, float has_l, float m, float s,
                                                       float s1, float up) {
     HeadGrad g{};
     g.m = m;
     g.c = a.c;
     g.is = s == 0.0f ? 0.0f : 1.0f / s;
     g.is1 = s1 == 0.0f ? 0.0f : 1.0f / s1;
-    g.a = up * a.alpha * a.temp * p.has_q;
-    g.b = up * (1.0f - a.alpha) * p.has_l;
-    g.zero = up == 0.0f || (p.has_q == 0.0f && p.has_l == 0.0f);
+    g.a = up * a.alpha * a.temp * has_q;
+    g.b = up * (1.0f - a.alpha) * has_l;
+    g.zero = up == 0.0f || (has_q == 0.0f && has_l == 0.0f);
     return g;
 }
 
-// The places' own gradients, after the stream has written the row: each id is written by the first of the
-// places that have it, with the sum of their parts.
+// The places' own gradients, after the stream has written the row (first wave): each id is written by
+// the first of the places that have it, with the sum of their parts.
 template <typename T, int TH, bool TWO>
 __device__ __forceinline__ void head_place_grads(const HeadDistillArgs &a, const HeadGrad &g, const HeadPlaces &p, float up,
                                                  T *dz, long long lo, long long hi, const HeadDistillLds<TH> &s) {
-    __syncthreads();
-    const int tid = threadIdx.x;
-    if (tid > a.K || p.id < lo || p.id >= hi || g.zero) return;
-    float q = 0.0f;
-    bool first = true;
-    for (int k = 0; k < a.K; ++k)
-        if (s.id[k] == p.id) {
-            first = first && k >= tid;
-            q += s.q[k];
+    float v[kHeadPlaces];
+    bool mine[kHeadPlaces];
+    if (threadIdx.x < 64) {
+        float q[kHeadPlaces] = {};
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i)
+            mine[i] = (int)threadIdx.x + 64 * i <= a.K && p.id[i] >= lo && p.id[i] < hi && !g.zero;
+        for (int k = 0; k < a.K; ++k) {
+            const int id = s.id[k];
+            const float add = s.q[k];
+#pragma unroll
+            for (int i = 0; i < kHeadPlaces; ++i)
+                if (id == p.id[i]) {
+                    mine[i] = mine[i] && k >= (int)threadIdx.x + 64 * i;
+                    q[i] += add;
+                }
         }
-    if (!first) return;
-    float v = head_grad_at<false, TWO>(g, p.zt) - up * a.alpha * a.temp * q;
-    if (s.id[a.K] == p.id) v -= up * (1.0f - a.alpha);
-    dz[p.id] = from_f32<T>(v);
+        const int label = s.id[a.K];
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i) {
+            v[i] = head_grad_at<false, TWO>(g, p.zt[i]) - up * a.alpha * a.temp * q[i];
+            if (label == p.id[i]) v[i] -= up * (1.0f - a.alpha);
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i)
+            if (mine[i]) dz[p.id[i]] = from_f32<T>(v[i]);
+    }
 }
 
-// One workgroup per row: the statistics, the loss and, for GRAD, the gradient from a second read
-// of the row, which the caches still hold.
-template <typename T, int TH, int U, bool TWO, bool GRAD>
-__global__ __launch_bounds__(TH) void qhead_distill_row_kernel(HeadDistillArgs a) {
+__device__ __forceinline__ void head_distill_write(const HeadDistillArgs &a, long long row, const HeadSums &t, float loss) {
+    a.loss[row] = loss;
+    if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
+}
+
+// One workgroup per row: the statistics, the loss and, for GRAD, the gradient.  HELD: the row fits the
+// workgroup's registers, U vectors a thread, and is read once; else the gradient reads it again, from
+// what the caches still hold of it.
+template <typename T, int TH, int U, bool TWO, bool GRAD, bool HELD>
+__global__ __launch_bounds__(TH, HELD &&U == 8 ? 4 : 1) void qhead_distill_row_kernel(HeadDistillArgs a) {
     __shared__ HeadDistillLds<TH> s;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
-    const HeadPlaces p = head_places<T, TH>(a, row, z.p, s);
     HeadSums t = head_start();
-    for (int first = 0; first < z.nvec; first += U * TH) {
-        v4u r[U];
-        head_load<T, U>(z, first, TH, tid, z.nvec, r);
+    v4u r[U];
+    HeadPlaces p;
+    const float up = GRAD ? a.g[row] : 0.0f;
+    if constexpr (HELD) {
+        head_load<T, U>(z, 0, TH, tid, z.nvec, r);
+        if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
         head_accumulate<T, U, false, TWO>(t, r, a.c);
+    } else {
+        if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
+        for (int first = 0; first < z.nvec; first += U * TH) {
+            head_load<T, U>(z, first, TH, tid, z.nvec, r);
+            head_accumulate<T, U, false, TWO>(t, r, a.c);
+        }
     }
     t = head_block_join<TH, false, TWO>(t, a.c, s.sums);
     if constexpr (!TWO) t.s1 = t.s;
-    const float loss = head_distill_loss<TH>(a, p, t, s);
-    if (tid == 0) {
-        a.loss[row] = loss;
-        if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
+    if (tid < 64) {
+        const float loss = head_distill_loss(a, p, t);
+        if (tid == 0) head_distill_write(a, row, t, loss);
     }
     if constexpr (GRAD) {
-        const float up = a.g[row];
-        HeadGrad g = head_distill_coef(a, p, t.m, t.s, t.s1, up);
+        HeadGrad g = head_distill_coef(a, s.has_q, s.has_l, t.m, t.s, t.s1, up);
         if constexpr (!TWO) g.a += g.b;  // (T = 1, or no label: one set of probabilities)
         T *dz = static_cast<T *>(a.dz) + row * a.V;
-        for (int first = 0; first < z.nvec; first += U * TH) {
-            v4u r[U];
-            head_load<T, U>(z, first, TH, tid, z.nvec, r);
-            head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, z.nvec);
+        if constexpr (HELD) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) asm volatile("" : "+v"(r[u]));  // (unpacked anew: kept, the values fill the registers)
+            head_grad_store<T, U, false, TWO>(g, z, dz, r, 0, TH, tid, z.nvec);
+        } else {
+            for (int first = 0; first < z.nvec; first += U * TH) {
+                head_load<T, U>(z, first, TH, tid, z.nvec, r);
+                head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, z.nvec);
+            }
         }
         head_place_grads<T, TH, TWO>(a, g, p, up, dz, 0, a.V, s);
     }
@@ -786,18 +829,16 @@ __global__ __launch_bounds__(TH) void qhead_distill_part_kernel(HeadDistillArgs 
     if (threadIdx.x == 0) a.part[row * a.splits + sp] = t;
 }
 
+// One wave a row.
 template <typename T, bool TWO>
-__global__ __launch_bounds__(256) void qhead_distill_join_kernel(HeadDistillArgs a) {
-    __shared__ HeadDistillLds<256> s;
+__global__ __launch_bounds__(64) void qhead_distill_join_kernel(HeadDistillArgs a) {
+    __shared__ HeadDistillLds<64> s;
     const long long row = blockIdx.x;
-    const HeadPlaces p = head_places<T, 256>(a, row, static_cast<const T *>(a.z) + row * a.ld, s);
+    const HeadPlaces p = head_places<T, 64>(a, row, static_cast<const T *>(a.z) + row * a.ld, s);
     HeadSums t = head_join_parts<false, TWO>(a.part + row * a.splits, a.splits, a.c);
     if constexpr (!TWO) t.s1 = t.s;
-    const float loss = head_distill_loss<256>(a, p, t, s);
-    if (threadIdx.x == 0) {
-        a.loss[row] = loss;
-        if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
-    }
+    const float loss = head_distill_loss(a, p, t);
+    if (threadIdx.x == 0) head_distill_write(a, row, t, loss);
 }
 
 template <typename T, int TH, int U, bool TWO>
@@ -808,14 +849,17 @@ __global__ __launch_bounds__(TH) void qhead_distill_grad_kernel(HeadDistillArgs 
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     const int begin = sp * a.per, end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
     T *dz = static_cast<T *>(a.dz) + row * a.V;
-    const HeadPlaces p = head_places<T, TH>(a, row, z.p, s);
     const float up = a.g[row];
     const float *st = a.stats + 4 * row;
-    HeadGrad g = head_distill_coef(a, p, st[0], st[1], st[2], up);
+    v4u r[U];
+    head_load<T, U>(z, begin, TH, tid, end, r);  // (in flight while the places are read)
+    HeadPlaces p;
+    if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
+    __syncthreads();
+    HeadGrad g = head_distill_coef(a, s.has_q, s.has_l, st[0], st[1], st[2], up);
     if constexpr (!TWO) g.a += g.b;
     for (int first = begin; first < end; first += U * TH) {
-        v4u r[U];
-        head_load<T, U>(z, first, TH, tid, end, r);
+        if (first != begin) head_load<T, U>(z, first, TH, tid, end, r);
         head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, end);
     }
     head_place_grads<T, TH, TWO>(a, g, p, up, dz, (long long)begin * HeadRow<T>::VEC,

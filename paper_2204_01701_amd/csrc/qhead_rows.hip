@@ -13,6 +13,9 @@ namespace {
 
 constexpr int kRowThreads = 256;
 
+// Rows enough to fill the GPU with one wave each (eight a CU at least).
+bool many_rows(int rows) { return rows >= 8 * kNumCUs; }
+
 bool rows_ok(const qhead_rows_desc *d) {
     return d && d->rows >= 0 && d->vocab > 0 && d->ld >= d->vocab && (d->dtype == QL_F32 || d->dtype == QL_BF16) &&
            std::isfinite(d->temperature) && d->temperature > 0.0f;
@@ -39,6 +42,7 @@ Split split_rows(int rows, int nvec, int blocks, int most, int least_per) {
 // A part of a row has two vectors a thread at least.  (Parts of the alternatives' lists
 // together fit the join's 16 KiB.)
 Split logprobs_split(const qhead_rows_desc *d) {
+    if (d->rows >= kNumCUs) return {1, vectors(d)};
     const int most = std::min(kHeadMaxSplits, kHeadJoinKeys / std::max(1, d->top));
     return split_rows(d->rows, vectors(d), 2 * kNumCUs, most, 2 * kRowThreads);
 }
@@ -51,12 +55,15 @@ Split grad_split(const qhead_rows_desc *d) { return split_rows(d->rows, vectors(
 template <typename T> void launch_logprobs(const HeadLogprobArgs &a, int rows, hipStream_t st) {
     const dim3 grid((unsigned)((long long)rows * a.splits));
     const int nvec = cdiv(a.V, Elem<T>::VEC);
-    // one wave where a row is at most one vector a lane
+    // one wave where a row is at most one vector a lane, or short and one of many
+    const bool one = nvec <= 64, wave = nvec <= 1024 && many_rows(rows);
     if (a.K) {
-        if (nvec <= 64) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, true>), grid, dim3(64), 0, st, a);
+        if (one) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, true>), grid, dim3(64), 0, st, a);
+        else if (wave) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 4, true>), grid, dim3(64), 0, st, a);
         else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, true>), grid, dim3(kRowThreads), 0, st, a);
     } else {
-        if (nvec <= 64) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, false>), grid, dim3(64), 0, st, a);
+        if (one) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, false>), grid, dim3(64), 0, st, a);
+        else if (wave) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 4, false>), grid, dim3(64), 0, st, a);
         else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, false>), grid, dim3(kRowThreads), 0, st, a);
     }
     if (a.splits > 1)
@@ -103,12 +110,35 @@ ql_status distill_args(const qhead_rows_desc *d, const void *logits, const int64
     return QL_OK;
 }
 
+template <typename T, int TH, int U, bool TWO, bool GRAD, bool HELD>
+void launch_row_as(const HeadDistillArgs &a, int rows, hipStream_t st) {
+    hipLaunchKernelGGL((qhead_distill_row_kernel<T, TH, U, TWO, GRAD, HELD>), dim3(rows), dim3(TH), 0, st, a);
+}
+// The kernel of a workgroup per row by the row's length in vectors.  One wave where a row is short and rows
+// are many (8192 rows of 1000, bf16, step: 24 us against 57 with 256 threads; 4096 of 8000: 45 and 49), else
+// rows held in registers up to 8 vectors a thread (2048 rows of 32768, fp32: 134 us held by 1024 threads, 145
+// to 175 read twice), and beyond that 1024 threads, so that few rows are under way and the second read
+// finds them in the caches (4096 rows of 131072, bf16: 520 us against 650 with 256 threads).
 template <typename T, bool TWO, bool GRAD> void launch_row(const HeadDistillArgs &a, int rows, hipStream_t st) {
-    hipLaunchKernelGGL((qhead_distill_row_kernel<T, kRowThreads, 4, TWO, GRAD>), dim3(rows), dim3(kRowThreads), 0, st, a);
+    const int nvec = cdiv(a.V, Elem<T>::VEC);
+    const bool many = many_rows(rows);
+    if (nvec <= 64) return launch_row_as<T, 64, 1, TWO, GRAD, GRAD>(a, rows, st);
+    if (nvec <= 256 && many) return launch_row_as<T, 64, 4, TWO, GRAD, GRAD>(a, rows, st);
+    if (nvec <= 1024) {
+        if (many) return launch_row_as<T, 64, 4, TWO, GRAD, false>(a, rows, st);
+        return launch_row_as<T, kRowThreads, 4, TWO, GRAD, GRAD>(a, rows, st);
+    }
+    if constexpr (GRAD) {
+        if (nvec <= 2048) return launch_row_as<T, 256, 8, TWO, GRAD, true>(a, rows, st);
+        if (nvec <= 4096) return launch_row_as<T, 512, 8, TWO, GRAD, true>(a, rows, st);
+        if (nvec <= 8192) return launch_row_as<T, 1024, 8, TWO, GRAD, true>(a, rows, st);
+        return launch_row_as<T, 1024, 2, TWO, GRAD, false>(a, rows, st);
+    }
+    launch_row_as<T, kRowThreads, 4, TWO, GRAD, false>(a, rows, st);
 }
 template <typename T, bool TWO> void launch_parts(const HeadDistillArgs &a, int rows, hipStream_t st) {
     hipLaunchKernelGGL((qhead_distill_part_kernel<T, kRowThreads, 4, TWO>), dim3(rows * a.splits), dim3(kRowThreads), 0, st, a);
-    hipLaunchKernelGGL((qhead_distill_join_kernel<T, TWO>), dim3(rows), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((qhead_distill_join_kernel<T, TWO>), dim3(rows), dim3(64), 0, st, a);
 }
 template <typename T, bool TWO> void launch_distill_grad(const HeadDistillArgs &a, int rows, hipStream_t st) {
     hipLaunchKernelGGL((qhead_distill_grad_kernel<T, kRowThreads, 4, TWO>), dim3((unsigned)((long long)rows * a.splits)),
