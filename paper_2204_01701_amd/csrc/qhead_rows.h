@@ -133,6 +133,8 @@ __device__ __forceinline__ float head_accumulate(HeadSums &a, v4u (&r)[U], float
             a.s += p;
             if constexpr (ENT) a.d += p * fmaxf(d, kHeadFloor);
             if constexpr (TWO) a.s1 += head_exp2(x * kLog2e);
+            if constexpr (U >= 8)
+                if (e == VEC - 1) __builtin_amdgcn_sched_barrier(0);  // (one vector's values at a time)
         }
     return top;
 }
@@ -538,6 +540,7 @@ __device__ __forceinline__ void head_grad_store(const HeadGrad &g, const HeadRow
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int j = first + u * step + tid;
+        if constexpr (U >= 8) __builtin_amdgcn_sched_barrier(0);  // (one vector's values at a time)
         if (j >= end) continue;
         float f[VEC];
 #pragma unroll
@@ -613,47 +616,78 @@ struct HeadDistillArgs {
 // place K, the label.  The first wave holds them, place lane + 64 i on a lane, so that they need no
 // barriers of their own; what the other waves need of them goes through LDS with the row's sums.
 constexpr int kHeadPlaces = (kHeadTopMax + 64) / 64;
-struct HeadPlaces {
-    float q[kHeadPlaces], zt[kHeadPlaces], logq[kHeadPlaces];  // probability, student logit, log q
-    int id[kHeadPlaces];                                       // -1: none
-    float has_q, has_l;  // the row has a teacher's term, a label's (0 or 1)
-    bool wrong;          // an id or label past the vocabulary
+struct HeadPlace {
+    int id;          // -1: none
+    float q;         // the teacher's logit, then the probability
+    float zt, logq;  // student's logit, log q
 };
 
 template <int TH> struct HeadDistillLds {
     HeadSums sums[TH / 64];
-    float q[kHeadTopMax + 1];
-    int id[kHeadTopMax + 1];
-    float has_q, has_l;
+    HeadPlace place[kHeadTopMax + 1];
+    float has_q, has_l;  // the row has a teacher's term, a label's (0 or 1)
+    uint8_t slot[2048];  // of the places' ids, the place written there last
 };
+__device__ __forceinline__ uint32_t head_slot(int id) { return (uint32_t)id * 2654435761u >> 21; }
+static_assert(kHeadPlaces == 3 && kHeadTopMax < 256, "places of the first wave");
 
-// (first wave)
+// In steps, each lane's places kept in LDS in between, so that the row can have the registers:
+// the ids and the teacher's logits, the student's logits there (requests to memory without a branch on
+// an id: place after place, their latencies cost 8 us a row of 128), and, once the row's gradient
+// is under way, the softmax.  (First wave.)
+struct HeadPlaceLoads {
+    float zt[kHeadPlaces];
+};
+// Returns whether an id or the label is past the vocabulary.
 template <typename T, int TH>
-__device__ __forceinline__ HeadPlaces head_places(const HeadDistillArgs &a, long long row, const T *z, HeadDistillLds<TH> &s) {
-    const int lane = threadIdx.x;
-    HeadPlaces p;
-    float t[kHeadPlaces], most = -__builtin_inff();
-    bool wrong = false, label = false;
+__device__ __forceinline__ bool head_places_load(const HeadDistillArgs &a, long long row, const T *z, HeadDistillLds<TH> &s,
+                                                 HeadPlaceLoads &l) {
+    int64_t id[kHeadPlaces];
+    float t[kHeadPlaces];
 #pragma unroll
     for (int i = 0; i < kHeadPlaces; ++i) {
-        const int k = lane + 64 * i;
-        p.q[i] = p.zt[i] = p.logq[i] = 0.0f;
-        p.id[i] = -1;
+        const int k = (int)threadIdx.x + 64 * i;
+        id[i] = -1;
         t[i] = -__builtin_inff();
-        if (64 * i > a.K) continue;
-        int64_t id = -1;
         if (k < a.K) {
-            id = a.ids[row * a.K + k];
-            if (id >= 0) t[i] = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + k]);
+            id[i] = a.ids[row * a.K + k];
+            t[i] = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + k]);
         } else if (k == a.K && a.label) {
-            id = a.label[row];
-            label = id >= 0 && id < a.V;
+            id[i] = a.label[row];
         }
-        wrong = wrong || id >= a.V;
-        if (id >= 0 && id < a.V) {
-            p.id[i] = (int)id;
-            p.zt[i] = to_f32<T>(z[id]);
-        }
+    }
+    bool wrong = false, label = false, some = false;
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        const int k = (int)threadIdx.x + 64 * i;
+        const bool in = id[i] >= 0 && id[i] < a.V;
+        l.zt[i] = 0.0f;
+        if (64 * i <= a.K) l.zt[i] = to_f32<T>(z[in ? id[i] : 0]);
+        if (id[i] < 0) t[i] = -__builtin_inff();  // (an empty place, or one of probability 0)
+        if (k <= a.K) s.place[k].id = in ? (int)id[i] : -1;
+        if (k <= a.K) s.place[k].q = t[i];
+        wrong = wrong || id[i] >= a.V;
+        label = label || (k == a.K && in);
+        some = some || t[i] != -__builtin_inff();
+    }
+    const bool has_l = __ballot(label) != 0, has_q = __ballot(some) != 0;
+    if (threadIdx.x == 0) {
+        s.has_q = has_q ? 1.0f : 0.0f;
+        s.has_l = has_l ? 1.0f : 0.0f;
+    }
+    return __ballot(wrong) != 0;
+}
+template <int TH> __device__ __forceinline__ void head_places_keep(const HeadDistillArgs &a, const HeadPlaceLoads &l, HeadDistillLds<TH> &s) {
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i)
+        if ((int)threadIdx.x + 64 * i <= a.K) s.place[threadIdx.x + 64 * i].zt = l.zt[i];
+}
+template <int TH> __device__ __forceinline__ void head_places_softmax(const HeadDistillArgs &a, HeadDistillLds<TH> &s) {
+    float t[kHeadPlaces], q[kHeadPlaces], most = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < kHeadPlaces; ++i) {
+        const int k = (int)threadIdx.x + 64 * i;
+        t[i] = k <= a.K ? s.place[k].q : -__builtin_inff();
         most = fmaxf(most, t[i]);
     }
 #pragma unroll
@@ -661,51 +695,44 @@ __device__ __forceinline__ HeadPlaces head_places(const HeadDistillArgs &a, long
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kHeadPlaces; ++i) {
-        p.logq[i] = (t[i] - most) * a.inv_t;
-        p.q[i] = t[i] != -__builtin_inff() ? expf(p.logq[i]) : 0.0f;  // (-inf: an empty place, or one of probability 0)
-        sum += p.q[i];
+        const bool some = t[i] != -__builtin_inff();
+        t[i] = (t[i] - most) * a.inv_t;
+        q[i] = some ? expf(t[i]) : 0.0f;
+        sum += q[i];
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
     const float ls = logf(sum);
 #pragma unroll
     for (int i = 0; i < kHeadPlaces; ++i) {
-        p.q[i] = sum != 0.0f ? p.q[i] / sum : 0.0f;
-        p.logq[i] -= ls;
-        const int k = lane + 64 * i;
-        if (k <= a.K) {
-            s.q[k] = p.q[i];
-            s.id[k] = p.id[i];
-        }
+        const int k = (int)threadIdx.x + 64 * i;
+        if (k > a.K) continue;
+        s.place[k].q = sum != 0.0f ? q[i] / sum : 0.0f;
+        s.place[k].logq = t[i] - ls;
     }
-    p.has_q = sum != 0.0f ? 1.0f : 0.0f;
-    p.has_l = __ballot(label) != 0 ? 1.0f : 0.0f;
-    p.wrong = __ballot(wrong) != 0;
-    if (lane == 0) {
-        s.has_q = p.has_q;
-        s.has_l = p.has_l;
-    }
-    return p;
 }
 
 // The row's loss (first wave).
-__device__ __forceinline__ float head_distill_loss(const HeadDistillArgs &a, const HeadPlaces &p, const HeadSums &t) {
+template <int TH>
+__device__ __forceinline__ float head_distill_loss(const HeadDistillArgs &a, const HeadSums &t, bool wrong, const HeadDistillLds<TH> &s) {
     float v = 0.0f;
     const float ls = logf(t.s);
 #pragma unroll
     for (int i = 0; i < kHeadPlaces; ++i) {
-        const int k = threadIdx.x + 64 * i;
-        if (p.id[i] < 0) continue;
+        const int k = (int)threadIdx.x + 64 * i;
+        if (k > a.K) continue;
+        const HeadPlace p = s.place[k];
+        if (p.id < 0) continue;
         if (k < a.K) {
-            const float lp = t.s == 0.0f ? -__builtin_inff() : head_scaled_diff(p.zt[i], t.m, a.inv_t) - ls;
-            if (p.q[i] != 0.0f) v += a.alpha * a.temp * a.temp * p.q[i] * (p.logq[i] - lp);
-        } else if (k == a.K) {
-            v += t.s1 == 0.0f ? __builtin_inff() : (1.0f - a.alpha) * (logf(t.s1) - head_scaled_diff(p.zt[i], t.m, 1.0f));
+            const float lp = t.s == 0.0f ? -__builtin_inff() : head_scaled_diff(p.zt, t.m, a.inv_t) - ls;
+            if (p.q != 0.0f) v += a.alpha * a.temp * a.temp * p.q * (p.logq - lp);
+        } else {
+            v += t.s1 == 0.0f ? __builtin_inff() : (1.0f - a.alpha) * (logf(t.s1) - head_scaled_diff(p.zt, t.m, 1.0f));
         }
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    return p.wrong ? __builtin_nanf("") : v;
+    return wrong ? __builtin_nanf("") : v;
 }
 
 __device__ __forceinline__ HeadGrad head_distill_coef(const HeadDistillArgs &a, float has_q, float has_l, float m, float s,
@@ -722,39 +749,79 @@ __device__ __forceinline__ HeadGrad head_distill_coef(const HeadDistillArgs &a, 
 }
 
 // The places' own gradients, after the stream has written the row (first wave): each id is written by
-// the first of the places that have it, with the sum of their parts.
+// the first of the places that have it, with the sum of their parts.  Ids that occur twice are rare, so
+// each place looks only whether its slot of a hash table was taken by another one (comparing each with all
+// cost 9 us a row of 128), and those that lost theirs are compared with all.
 template <typename T, int TH, bool TWO>
-__device__ __forceinline__ void head_place_grads(const HeadDistillArgs &a, const HeadGrad &g, const HeadPlaces &p, float up,
-                                                 T *dz, long long lo, long long hi, const HeadDistillLds<TH> &s) {
+__device__ __forceinline__ void head_place_grads(const HeadDistillArgs &a, const HeadGrad &g, float up, T *dz, long long lo,
+                                                 long long hi, HeadDistillLds<TH> &s) {
     float v[kHeadPlaces];
-    bool mine[kHeadPlaces];
+    int id[kHeadPlaces];
+    __builtin_amdgcn_sched_barrier(0);
     if (threadIdx.x < 64) {
-        float q[kHeadPlaces] = {};
-#pragma unroll
-        for (int i = 0; i < kHeadPlaces; ++i)
-            mine[i] = (int)threadIdx.x + 64 * i <= a.K && p.id[i] >= lo && p.id[i] < hi && !g.zero;
-        for (int k = 0; k < a.K; ++k) {
-            const int id = s.id[k];
-            const float add = s.q[k];
-#pragma unroll
-            for (int i = 0; i < kHeadPlaces; ++i)
-                if (id == p.id[i]) {
-                    mine[i] = mine[i] && k >= (int)threadIdx.x + 64 * i;
-                    q[i] += add;
-                }
-        }
-        const int label = s.id[a.K];
+        const int lane = threadIdx.x;
+        float q[kHeadPlaces];
+        bool lost[kHeadPlaces], mine[kHeadPlaces];
 #pragma unroll
         for (int i = 0; i < kHeadPlaces; ++i) {
-            v[i] = head_grad_at<false, TWO>(g, p.zt[i]) - up * a.alpha * a.temp * q[i];
-            if (label == p.id[i]) v[i] -= up * (1.0f - a.alpha);
+            const int k = lane + 64 * i;
+            id[i] = k < a.K ? s.place[k].id : -1;
+            q[i] = k < a.K ? s.place[k].q : 0.0f;
+            if (id[i] >= 0) s.slot[head_slot(id[i])] = (uint8_t)k;
+        }
+        wave_lds_sync();
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i) {
+            mine[i] = id[i] >= 0;
+            lost[i] = mine[i] && s.slot[head_slot(id[i])] != lane + 64 * i;
+        }
+        const float own[kHeadPlaces] = {q[0], q[1], q[2]};
+        for (;;) {
+            int twice = -1;
+#pragma unroll
+            for (int i = 0; i < kHeadPlaces; ++i) {
+                const uint64_t m = __ballot(lost[i]);
+                if (m && twice < 0) twice = __builtin_amdgcn_readlane(id[i], __builtin_ctzll(m));
+            }
+            if (twice < 0) break;
+            float sum = 0.0f;
+            int first = -1;
+#pragma unroll
+            for (int i = 0; i < kHeadPlaces; ++i)
+                for (uint64_t m = __ballot(id[i] == twice); m; m &= m - 1) {
+                    const int l = __builtin_ctzll(m);
+                    sum += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(own[i]), l));
+                    if (first < 0) first = l + 64 * i;
+                }
+#pragma unroll
+            for (int i = 0; i < kHeadPlaces; ++i)
+                if (id[i] == twice) {
+                    q[i] = sum;
+                    mine[i] = lane + 64 * i == first;
+                    lost[i] = false;
+                }
+        }
+        const int label = s.place[a.K].id;
+        bool among = false;  // (the label is one of the teacher's ids: it goes with that place)
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i) among = among || __ballot(label >= 0 && id[i] == label) != 0;
+#pragma unroll
+        for (int i = 0; i < kHeadPlaces; ++i) {
+            const int k = lane + 64 * i;
+            if (k == a.K && !among) {
+                id[i] = label;
+                mine[i] = label >= 0;
+            }
+            v[i] = head_grad_at<false, TWO>(g, k <= a.K ? s.place[k].zt : 0.0f) - up * a.alpha * a.temp * q[i];
+            if (label >= 0 && label == id[i]) v[i] -= up * (1.0f - a.alpha);
+            if (!mine[i] || id[i] < lo || id[i] >= hi || g.zero) id[i] = -1;
         }
     }
     __syncthreads();
     if (threadIdx.x < 64) {
 #pragma unroll
         for (int i = 0; i < kHeadPlaces; ++i)
-            if (mine[i]) dz[p.id[i]] = from_f32<T>(v[i]);
+            if (id[i] >= 0) dz[id[i]] = from_f32<T>(v[i]);
     }
 }
 
@@ -767,39 +834,41 @@ __device__ __forceinline__ void head_distill_write(const HeadDistillArgs &a, lon
 // workgroup's registers, U vectors a thread, and is read once; else the gradient reads it again, from
 // what the caches still hold of it.
 template <typename T, int TH, int U, bool TWO, bool GRAD, bool HELD>
-__global__ __launch_bounds__(TH, HELD &&U == 8 ? 4 : 1) void qhead_distill_row_kernel(HeadDistillArgs a) {
+__global__ __launch_bounds__(TH, HELD &&U >= 8 ? 4 : 1) void qhead_distill_row_kernel(HeadDistillArgs a) {
     __shared__ HeadDistillLds<TH> s;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     HeadSums t = head_start();
     v4u r[U];
-    HeadPlaces p;
+    HeadPlaceLoads l;
+    bool wrong = false;
     const float up = GRAD ? a.g[row] : 0.0f;
-    if constexpr (HELD) {
-        head_load<T, U>(z, 0, TH, tid, z.nvec, r);
-        if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
-        head_accumulate<T, U, false, TWO>(t, r, a.c);
-    } else {
-        if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
-        for (int first = 0; first < z.nvec; first += U * TH) {
+    head_load<T, U>(z, 0, TH, tid, z.nvec, r);
+    if (tid < 64) {
+        wrong = head_places_load<T, TH>(a, row, z.p, s, l);
+        head_places_keep<TH>(a, l, s);
+        head_places_softmax<TH>(a, s);
+    }
+    head_accumulate<T, U, false, TWO>(t, r, a.c);
+    if constexpr (!HELD)
+        for (int first = U * TH; first < z.nvec; first += U * TH) {
             head_load<T, U>(z, first, TH, tid, z.nvec, r);
             head_accumulate<T, U, false, TWO>(t, r, a.c);
         }
-    }
     t = head_block_join<TH, false, TWO>(t, a.c, s.sums);
     if constexpr (!TWO) t.s1 = t.s;
     if (tid < 64) {
-        const float loss = head_distill_loss(a, p, t);
+        const float loss = head_distill_loss<TH>(a, t, wrong, s);
         if (tid == 0) head_distill_write(a, row, t, loss);
     }
     if constexpr (GRAD) {
+        T *dz = static_cast<T *>(a.dz) + row * a.V;
         HeadGrad g = head_distill_coef(a, s.has_q, s.has_l, t.m, t.s, t.s1, up);
         if constexpr (!TWO) g.a += g.b;  // (T = 1, or no label: one set of probabilities)
-        T *dz = static_cast<T *>(a.dz) + row * a.V;
         if constexpr (HELD) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) asm volatile("" : "+v"(r[u]));  // (unpacked anew: kept, the values fill the registers)
+            for (int u = 0; u < U; ++u) asm volatile("" : "+v"(r[u]));  // (unpacked anew, as above)
             head_grad_store<T, U, false, TWO>(g, z, dz, r, 0, TH, tid, z.nvec);
         } else {
             for (int first = 0; first < z.nvec; first += U * TH) {
@@ -807,7 +876,7 @@ __global__ __launch_bounds__(TH, HELD &&U == 8 ? 4 : 1) void qhead_distill_row_k
                 head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, z.nvec);
             }
         }
-        head_place_grads<T, TH, TWO>(a, g, p, up, dz, 0, a.V, s);
+        head_place_grads<T, TH, TWO>(a, g, up, dz, 0, a.V, s);
     }
 }
 
@@ -834,10 +903,13 @@ template <typename T, bool TWO>
 __global__ __launch_bounds__(64) void qhead_distill_join_kernel(HeadDistillArgs a) {
     __shared__ HeadDistillLds<64> s;
     const long long row = blockIdx.x;
-    const HeadPlaces p = head_places<T, 64>(a, row, static_cast<const T *>(a.z) + row * a.ld, s);
+    HeadPlaceLoads l;
+    const bool wrong = head_places_load<T, 64>(a, row, static_cast<const T *>(a.z) + row * a.ld, s, l);
+    head_places_keep<64>(a, l, s);
+    head_places_softmax<64>(a, s);
     HeadSums t = head_join_parts<false, TWO>(a.part + row * a.splits, a.splits, a.c);
     if constexpr (!TWO) t.s1 = t.s;
-    const float loss = head_distill_loss(a, p, t);
+    const float loss = head_distill_loss<64>(a, t, wrong, s);
     if (threadIdx.x == 0) head_distill_write(a, row, t, loss);
 }
 
@@ -852,9 +924,13 @@ __global__ __launch_bounds__(TH) void qhead_distill_grad_kernel(HeadDistillArgs 
     const float up = a.g[row];
     const float *st = a.stats + 4 * row;
     v4u r[U];
+    HeadPlaceLoads l;
     head_load<T, U>(z, begin, TH, tid, end, r);  // (in flight while the places are read)
-    HeadPlaces p;
-    if (tid < 64) p = head_places<T, TH>(a, row, z.p, s);
+    if (tid < 64) {
+        head_places_load<T, TH>(a, row, z.p, s, l);
+        head_places_keep<TH>(a, l, s);
+        head_places_softmax<TH>(a, s);
+    }
     __syncthreads();
     HeadGrad g = head_distill_coef(a, s.has_q, s.has_l, st[0], st[1], st[2], up);
     if constexpr (!TWO) g.a += g.b;
@@ -862,7 +938,7 @@ __global__ __launch_bounds__(TH) void qhead_distill_grad_kernel(HeadDistillArgs 
         if (first != begin) head_load<T, U>(z, first, TH, tid, end, r);
         head_grad_store<T, U, false, TWO>(g, z, dz, r, first, TH, tid, end);
     }
-    head_place_grads<T, TH, TWO>(a, g, p, up, dz, (long long)begin * HeadRow<T>::VEC,
+    head_place_grads<T, TH, TWO>(a, g, up, dz, (long long)begin * HeadRow<T>::VEC,
                                  min((long long)a.V, (long long)end * HeadRow<T>::VEC), s);
 }
 

@@ -115,10 +115,13 @@ void launch_row_as(const HeadDistillArgs &a, int rows, hipStream_t st) {
     hipLaunchKernelGGL((qhead_distill_row_kernel<T, TH, U, TWO, GRAD, HELD>), dim3(rows), dim3(TH), 0, st, a);
 }
 // The kernel of a workgroup per row by the row's length in vectors.  One wave where a row is short and rows
-// are many (8192 rows of 1000, bf16, step: 24 us against 57 with 256 threads; 4096 of 8000: 45 and 49), else
-// rows held in registers up to 8 vectors a thread (2048 rows of 32768, fp32: 134 us held by 1024 threads, 145
-// to 175 read twice), and beyond that 1024 threads, so that few rows are under way and the second read
-// finds them in the caches (4096 rows of 131072, bf16: 520 us against 650 with 256 threads).
+// are many (8192 rows of 1000, bf16, step: 24 us against 57 with 256 threads; 4096 of 8000: 45 and 49).  The
+// step holds a row in registers, up to 16 vectors a thread, as far as a workgroup reaches: 4096 rows of 131072,
+// bf16, 457 us against 650 (256 threads) and 524 (1024, fewer rows under way, which the caches still hold) read
+// twice; 2048 of 32768, fp32, 114 against 145.  Where two sums make it compute-bound (bf16, label and
+// teacher at a temperature) 16 vectors on 1024 threads lose to the second read: 559 against 524.  16 vectors on
+// fewer threads beat 8 on more (1023 of 50001, bf16, both terms: 68 against 83; 4096 of 32768: 133, 146), but
+// not in fp32 up to 4096 vectors (2048 of 16000: 65, 60).
 template <typename T, bool TWO, bool GRAD> void launch_row(const HeadDistillArgs &a, int rows, hipStream_t st) {
     const int nvec = cdiv(a.V, Elem<T>::VEC);
     const bool many = many_rows(rows);
@@ -130,8 +133,13 @@ template <typename T, bool TWO, bool GRAD> void launch_row(const HeadDistillArgs
     }
     if constexpr (GRAD) {
         if (nvec <= 2048) return launch_row_as<T, 256, 8, TWO, GRAD, true>(a, rows, st);
-        if (nvec <= 4096) return launch_row_as<T, 512, 8, TWO, GRAD, true>(a, rows, st);
-        if (nvec <= 8192) return launch_row_as<T, 1024, 8, TWO, GRAD, true>(a, rows, st);
+        if (nvec <= 4096) {
+            if constexpr (sizeof(T) == 2) return launch_row_as<T, 256, 16, TWO, GRAD, true>(a, rows, st);
+            else return launch_row_as<T, 512, 8, TWO, GRAD, true>(a, rows, st);
+        }
+        if (nvec <= 8192) return launch_row_as<T, 512, 16, TWO, GRAD, true>(a, rows, st);
+        if constexpr (!(TWO && sizeof(T) == 2))
+            if (nvec <= 16384) return launch_row_as<T, 1024, 16, TWO, GRAD, true>(a, rows, st);
         return launch_row_as<T, 1024, 2, TWO, GRAD, false>(a, rows, st);
     }
     launch_row_as<T, kRowThreads, 4, TWO, GRAD, false>(a, rows, st);
