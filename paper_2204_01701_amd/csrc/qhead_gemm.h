@@ -315,7 +315,7 @@ template <int BI, int BJ, int WVI, int NS> constexpr int head_tile_lds() {
     return ring > stage ? ring : stage;
 }
 
-template <typename T, bool ANAT, bool BNAT, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int RING = 0, int NI1 = HeadSrc<T, ANAT, BI, WVI * WVJ>::NI + HeadSrc<T, BNAT, BJ, WVI * WVJ>::NI>
+template <typename T, bool ANAT, bool BNAT, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int NI1>
 __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_kernel(HeadTileArgs a) {
     constexpr int W = WVI * WVJ, TH = 64 * W, WI = BI / WVI, WJ = BJ / WVJ, MI = WI / 32, MJ = WJ / 32;
     constexpr int STAGE = (BI + BJ) * 64, BK = HeadStep<T>::BK;
@@ -357,8 +357,7 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_k
 #pragma unroll
             for (int y = 0; y < MJ; ++y) mfma_chunk<T>(fb[buf][y], fa[buf][x], acc[x][y]);
     };
-    if constexpr (RING == 1) run_ring_single<NS, SA::NI + SB::NI, 2, NI1>(nst, begin, issue, read, mma);
-    else run_ring<NS, SA::NI + SB::NI, NI1>(nst, begin, issue, read, mma);
+    run_ring<NS, SA::NI + SB::NI, NI1>(nst, begin, issue, read, mma);
     // Epilogue, one row of waves at a time: the accumulators go to LDS as rows of C, and come back as
     // eight neighbours a thread, whose global accesses are whole lines.  A pass's residuals are
     // all requested before its hand-over through LDS: one at a time their latency was 21 us a tile.
@@ -406,27 +405,96 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qhead_gemm_k
     }
 }
 
-// The splits' partial products, in their order, and the epilogue.
+// The splits' partial products, in their order, and the epilogue; the splits' loads are requested
+// four at a time.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void qhead_join_kernel(HeadTileArgs a) {
     const HeadGemmArgs &g = a.g;
     const int groups = (g.J + 7) / 8;
     const long long total = (long long)g.I * groups;
+    const size_t stride = (size_t)g.I * g.J;
     for (long long q = (long long)blockIdx.x * kThreads + threadIdx.x; q < total; q += (long long)gridDim.x * kThreads) {
-        const int i = (int)(q / groups), j = (int)(q - (long long)i * groups) * 8;
-        float v[8], b[8] = {};
-        head_load8<float>(a.part + (size_t)i * g.J + j, v, g.J - j);
-        for (int s = 1; s < a.splits; ++s) {
-            float u[8];
-            head_load8<float>(a.part + ((size_t)s * g.I + i) * g.J + j, u, g.J - j);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += u[e];
-        }
-        if (g.o.b) head_load8<float>(g.o.b + j, b, g.J - j);
+        const int i = (int)(q / groups), j = (int)(q - (long long)i * groups) * 8, n = g.J - j;
+        const float *p = a.part + (size_t)i * g.J + j;
+        float v[8] = {}, b[8] = {};
         HeadRaw8<T> raw = {};
-        if (g.o.r && j + 8 <= g.J) raw.load(static_cast<const T *>(g.o.r) + (size_t)i * g.o.ldr + j);
+        if (g.o.r && n >= 8) raw.load(static_cast<const T *>(g.o.r) + (size_t)i * g.o.ldr + j);
+        if (g.o.b) head_load8<float>(g.o.b + j, b, n);
+        for (int s = 0; s < a.splits; s += 4) {
+            float u[4][8];
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (s + x < a.splits) head_load8<float>(p + (s + x) * stride, u[x], n);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (s + x < a.splits) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += u[x][e];
+                }
+        }
         head_epilogue8<T>(g.o, g.J, i, j, v, b, raw);
     }
+}
+
+// --- few rows of x (serving: single tokens) -----------------------------------------------
+// C for I <= 16 rows: bound by reading B (the weights) once.  A workgroup takes 16 rows of B (output
+// columns); its eight waves share t, and each keeps eight 16-byte loads a lane in flight, straight into the
+// operand layout of the 16 x 16 MFMA (whose rows are j, columns i), from any alignment.  The waves'
+// partial products meet in LDS, in their order.
+template <typename T> __device__ __forceinline__ void head_mfma16(const v4u &a, const v4u &b, v4f &acc) {
+    if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), acc, 0, 0, 0);
+    }
+}
+
+// 16 bytes of a row from element t on, zeros from R on.
+template <typename T> __device__ __forceinline__ v4u head_row16(const T *p, int t, int R) {
+    constexpr int VEC = Elem<T>::VEC;
+    v4u v = {0u, 0u, 0u, 0u};
+    if (t + VEC <= R) {
+        v = *reinterpret_cast<const v4u_row *>(p + t);
+    } else if (t < R) {
+        float f[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = t + e < R ? to_f32<T>(p[t + e]) : 0.0f;
+        v = vpack<T>(f);
+    }
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(512) void qhead_few_kernel(HeadGemmArgs g) {
+    constexpr int W = 8, U = 8, STEP = 4 * Elem<T>::VEC;  // t of an MFMA: 32 bf16, 16 fp32
+    __shared__ v4f part[W][64];
+    const int lane = threadIdx.x & 63, wave = wave_id(), row = lane & 15, off = (lane >> 4) * Elem<T>::VEC;
+    const int j0 = blockIdx.x * 16;
+    const T *a = static_cast<const T *>(g.a) + (size_t)min(row, g.I - 1) * g.lda;
+    const T *b = static_cast<const T *>(g.b) + (size_t)min(j0 + row, g.J - 1) * g.ldb;
+    const int ra = row < g.I ? g.R : 0;  // (rows past I are zeros; columns past J are not stored)
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    // wave w takes steps w, w + 8, ...: the workgroup reads whole pieces of B's rows at a time
+    for (int t0 = wave * STEP; t0 < g.R; t0 += U * W * STEP) {
+        v4u fa[U], fb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) fb[u] = head_row16<T>(b, t0 + u * W * STEP + off, g.R);
+#pragma unroll
+        for (int u = 0; u < U; ++u) fa[u] = head_row16<T>(a, t0 + u * W * STEP + off, ra);
+#pragma unroll
+        for (int u = 0; u < U; ++u) head_mfma16<T>(fb[u], fa[u], acc);
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    const int i = threadIdx.x >> 4, j = j0 + (threadIdx.x & 15);  // (lane l holds column l % 16, rows 4 (l / 16) + v)
+    if (threadIdx.x >= 256 || i >= g.I || j >= g.J) return;
+    const int jr = threadIdx.x & 15;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) v += reinterpret_cast<const float *>(&part[w][(jr >> 2) * 16 + i])[jr & 3];
+    head_store<T>(g.o, g.J, i, j, v);
 }
 
 // rows x cols at any stride and alignment -> rows of `out_cols` (whole 16-byte vectors), zeros behind.

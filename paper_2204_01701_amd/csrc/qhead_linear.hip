@@ -1,4 +1,6 @@
 // qhead_linear.hip -- host side of the first-order layer of include/qhead.h.
+#include <cmath>
+
 #include "qhead.h"
 #include "qhead_gemm.h"
 #include "qhost.h"
@@ -39,7 +41,7 @@ struct Product {
     Operand a, b;
 };
 
-enum Tile { TILE_ANY, TILE_128, TILE_256 };
+enum Tile { TILE_ANY, TILE_FEW, TILE_128, TILE_256 };
 struct ProductPlan {
     Tile tile;
     bool pad_a, pad_b;
@@ -48,37 +50,56 @@ struct ProductPlan {
     size_t bytes() const { return a_bytes + b_bytes + part_bytes; }
 };
 
-// al_a, al_b: whether the operands' pointers are (taken to be) 16-byte aligned.
-ProductPlan plan_product(const Product &q, ql_dtype t, bool al_a, bool al_b) {
+// Time of a product in us by tile and splits: rounds of the workgroups over the CUs, each with its ramp and
+// epilogue; per K step of 64 bytes, 0.30 (bf16) or 1.03 (fp32) us with 128 x 128 tiles, also where two
+// share a CU, 0.86 or 3.66 with 256 x 256; the partial sums go out and come back at 4.5 TB/s, and
+// joining them is a launch.  Fitted on 30 shapes from 64 x 4096 x 4096 to 8192 x 8192 x 8192.
+double product_cost(const Product &q, ql_dtype t, bool large, int splits) {
+    const int B = large ? 256 : 128, steps = cdiv(q.R, 64 / (int)esize(t));
+    const double wgs = (double)cdiv(q.I, B) * cdiv(q.J, B) * splits, rounds = std::ceil(wgs / kNumCUs);
+    const double step = t == QL_BF16 ? (large ? 0.86 : 0.30) : (large ? 3.66 : 1.03);
+    const double join = splits > 1 ? 3.5 + 8.0 * splits * (double)q.I * q.J / 4.5e6 : 0.0;
+    return (large ? 8.0 : 5.0) + step * cdiv(steps, splits) * rounds + join;
+}
+
+// al_a, al_b: whether the operands' pointers are (taken to be) 16-byte aligned.  km: both operands have t
+// contiguous.
+ProductPlan plan_product(const Product &q, ql_dtype t, bool km, bool al_a, bool al_b) {
     ProductPlan p{};
     p.splits = 1;
+    const int forced = env_override("QHEAD_TILE", 0);
+    // Up to 16 rows the weights are read in place, whatever their layout (1 row of 4096, 4096 outputs, bf16:
+    // 10 us a call from Python; 128 x 128 tiles over 8 splits 13).
+    if (km && q.I <= 16 && !forced) {
+        p.tile = TILE_FEW;
+        return p;
+    }
     p.pad_a = !direct(q.a, t, al_a);
     p.pad_b = !direct(q.b, t, al_b);
     const double flops = 2.0 * q.I * q.J * std::max(1, q.R);
     const bool fits = (!p.pad_a || pad_fits(q.a, t)) && (!p.pad_b || pad_fits(q.b, t));
-    if (!fits || ((p.pad_a || p.pad_b) && flops < 2e7) || q.R == 0) {
+    if (!fits || ((p.pad_a || p.pad_b) && flops < 2e7) || q.R == 0 || forced == 1) {
         p.pad_a = p.pad_b = false;
         return p;
     }
-    p.tile = cdiv(q.I, 256) * (long long)cdiv(q.J, 256) >= 3 * kNumCUs / 4 ? TILE_256 : TILE_128;
-    const int forced = env_override("QHEAD_TILE", 0);
-    if (forced) p.tile = forced == 256 ? TILE_256 : forced == 128 ? TILE_128 : TILE_ANY;
-    if (p.tile == TILE_ANY) {
-        p.pad_a = p.pad_b = false;
-        return p;
-    }
-    const int B = p.tile == TILE_256 ? 256 : 128, steps = cdiv(q.R, 64 / (int)esize(t));
-    p.ti = cdiv(q.I, B);
-    p.tj = cdiv(q.J, p.tile == TILE_256 && env_override("QHEAD_VAR", 0) ? 128 : B);
-    const long long tiles = (long long)p.ti * p.tj;
+    const int steps = cdiv(q.R, 64 / (int)esize(t));
+    const double cap = (double)kMaxSplitBytes / (4.0 * q.I * q.J);
+    double best = 1e30;
     int want = 1;
-    if (p.tile == TILE_128 && tiles < kNumCUs) {
-        // split t until two workgroups a CU are busy, 8 steps each at least, the partial sums within their cap
-        want = (int)std::min<long long>(2 * kNumCUs / tiles, steps / 8);
-        want = (int)std::min<double>(want, (double)kMaxSplitBytes / (4.0 * q.I * q.J));
-    }
-    want = std::max(1, env_override("QHEAD_SPLITS", want));
-    p.per = cdiv(steps, std::min(want, steps));
+    for (int large = 0; large < 2; ++large)
+        for (int s = 1; s == 1 || (s <= 16 && 4 * s <= steps && s <= cap); ++s) {
+            const double c = product_cost(q, t, large, s);
+            if (c >= best) continue;
+            best = c;
+            p.tile = large ? TILE_256 : TILE_128;
+            want = s;
+        }
+    if (forced) p.tile = forced == 256 ? TILE_256 : TILE_128;
+    want = std::min(std::max(1, env_override("QHEAD_SPLITS", want)), steps);
+    const int B = p.tile == TILE_256 ? 256 : 128;
+    p.ti = cdiv(q.I, B);
+    p.tj = cdiv(q.J, B);
+    p.per = cdiv(steps, want);
     p.splits = cdiv(steps, p.per);
     if (p.pad_a) p.a_bytes = align_up((size_t)q.a.rows * padded_cols(q.a, t) * esize(t));
     if (p.pad_b) p.b_bytes = align_up((size_t)q.b.rows * padded_cols(q.b, t) * esize(t));
@@ -106,20 +127,15 @@ ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_
         hipLaunchKernelGGL((qhead_gemm_any_kernel<T, ANAT, BNAT>), grid, dim3(kThreads), 0, st, g);
         return hip_status();
     }
+    if (p.tile == TILE_FEW) {
+        if constexpr (!ANAT && !BNAT) hipLaunchKernelGGL((qhead_few_kernel<T>), dim3(cdiv(g.J, 16)), dim3(512), 0, st, g);
+        return hip_status();
+    }
     const dim3 grid((unsigned)(a.ti * a.tj * a.splits));
-    const int var = env_override("QHEAD_VAR", 0);
-    if (p.tile == TILE_256 && var == 1)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 4, 1, 0, 2>), grid, dim3(512), 0, st, a);
-    else if (p.tile == TILE_256 && var == 2)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 6, 1, 0, 2>), grid, dim3(512), 0, st, a);
-    else if (p.tile == TILE_256 && var == 3)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 2, 2, 3, 2, 0, 4>), grid, dim3(256), 0, st, a);
-    else if (p.tile == TILE_256 && var == 4)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 128, 4, 2, 3, 2, 1>), grid, dim3(512), 0, st, a);
-    else if (p.tile == TILE_256)
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 4, 4, 1, 0, 2>), grid, dim3(512), 0, st, a);
+    if (p.tile == TILE_256)
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 4, 4, 1, 2>), grid, dim3(512), 0, st, a);
     else
-        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 128, 2, 2, 4, 2>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 128, 2, 2, 4, 2, 4>), grid, dim3(256), 0, st, a);
     if (a.splits > 1)
         hipLaunchKernelGGL((qhead_join_kernel<T>), dim3(grid_1d((long long)g.I * cdiv(g.J, 8))), dim3(kThreads), 0, st, a);
     return hip_status();
@@ -128,7 +144,7 @@ ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_
 template <bool ANAT, bool BNAT>
 ql_status run_product(Product q, const HeadOut &o, ql_dtype t, char *ws, size_t ws_bytes, hipStream_t st) {
     if (q.I == 0 || q.J == 0) return QL_OK;
-    ProductPlan p = plan_product(q, t, aligned16(q.a.p), aligned16(q.b.p));
+    ProductPlan p = plan_product(q, t, !ANAT && !BNAT, aligned16(q.a.p), aligned16(q.b.p));
     if (p.bytes() > ws_bytes) {
         // (a misaligned pointer that the descriptor does not announce)
         p = ProductPlan{};
@@ -194,7 +210,7 @@ extern "C" {
 
 size_t qhead_linear_fwd_workspace_size(const qhead_linear_desc *d) {
     if (!linear_ok(d) || d->m == 0) return 0;
-    return plan_product(fwd_product(d, nullptr, nullptr), d->dtype, !d->unaligned, !d->unaligned).bytes();
+    return plan_product(fwd_product(d, nullptr, nullptr), d->dtype, true, !d->unaligned, !d->unaligned).bytes();
 }
 
 ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void *w, const float *b, const void *r,
@@ -219,8 +235,8 @@ size_t qhead_linear_bwd_workspace_size(const qhead_linear_desc *d) {
     const DzPlan p = plan_dz(d, al);
     const Operand dz = dz_operand(d, p, nullptr, nullptr);
     // the two products run one after the other on the same piece
-    return p.dz_bytes + p.part_bytes + std::max(plan_product(dx_product(d, dz, nullptr), d->dtype, al, al).bytes(),
-                                                plan_product(dw_product(d, dz, nullptr), d->dtype, al, al).bytes());
+    return p.dz_bytes + p.part_bytes + std::max(plan_product(dx_product(d, dz, nullptr), d->dtype, false, al, al).bytes(),
+                                                plan_product(dw_product(d, dz, nullptr), d->dtype, false, al, al).bytes());
 }
 
 ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void *w, const void *dy, const void *z,
