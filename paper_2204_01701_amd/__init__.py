@@ -620,82 +620,85 @@ HEAD_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 HEAD_MAX_TOP = 128  # QHEAD_MAX_TOP of qhead.h
 
 
-class _HeadOperands:
-    """Checks the tensors of one call and collects their pointers.
+# A small call is a few microseconds of GPU work, so the checks are one loop with a few
+# attribute reads per tensor; what they refuse is put into words by _head_refuse.
 
-    The first tensor sets the device; each one has to be on it, of its role's
-    dtype and shape, with contiguous rows."""
+def _head_first(t, what):
+    """Device index, torch dtype and dtype code of the call's first matrix."""
+    import torch
+    index, dtype = t.get_device(), t.dtype
+    if index < 0:
+        raise ValueError(f"{what}: a CUDA device tensor is required, got one on {t.device}")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: {t.dim()} dimensions, a matrix is required")
+    if dtype is torch.bfloat16:
+        return index, dtype, QL_BF16
+    if dtype is torch.float32:
+        return index, dtype, QL_F32
+    raise ValueError(f"{what}: dtype {dtype}, bfloat16 or float32 is required")
 
-    def __init__(self, t, dims=2):
-        import torch
-        self.torch = torch
-        self.index = t.get_device()
-        if self.index < 0:
-            raise ValueError(f"a CUDA device tensor is required, got one on {t.device}")
-        if t.dtype is torch.bfloat16:
-            self.code = QL_BF16
-        elif t.dtype is torch.float32:
-            self.code = QL_F32
-        else:
-            raise ValueError(f"dtype {t.dtype}: bfloat16 or float32 is required")
-        if t.dim() != dims:
-            raise ValueError(f"{t.dim()} dimensions, a matrix is required")
-        self.dtype = t.dtype
-        self.ptrs = []
 
-    def _take(self, name, t, shape, dtype):
-        if t.get_device() != self.index:
-            raise ValueError(f"{name}: on {t.device}, the other tensors on cuda:{self.index}")
-        if t.dtype is not dtype:
-            raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
-        self.ptrs.append(t.data_ptr())
+def _head_refuse(name, t, shape, dtype, index):
+    if t.get_device() != index:
+        raise ValueError(f"{name}: on {t.device}, the other tensors on cuda:{index}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    raise ValueError(f"{name}: must be contiguous")
 
-    def rows(self, name, t, shape):
-        """A matrix of the first tensor's dtype; returns its row stride."""
+
+def _head_rows(name, t, shape, dtype, index):
+    """(pointer, row stride) of a matrix whose rows are contiguous and may lie apart; None: (NULL, row length)."""
+    cols = shape[1]
+    if t is None:
+        return None, cols
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _head_refuse(name, t, shape, dtype, index)
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if shape[0] <= 1 or cols == 0:
+        ld = cols
+    elif ld < cols:
+        raise ValueError(f"{name}: rows overlap (row stride {ld} of {cols} elements)")
+    return t.data_ptr(), ld
+
+
+def _head_dense(index, *operands):
+    """Pointers of contiguous tensors given as (name, tensor or None, shape, dtype)."""
+    ptrs = []
+    for name, t, shape, dtype in operands:
         if t is None:
-            self.ptrs.append(None)
-            return shape[1]
-        self._take(name, t, shape, self.dtype)
-        ld, step = t.stride()
-        if step != 1 and shape[1] > 1:
-            raise ValueError(f"{name}: the elements of a row must be contiguous")
-        if shape[0] <= 1 or shape[1] == 0:
-            return shape[1]
-        if ld < shape[1]:
-            raise ValueError(f"{name}: rows overlap (row stride {ld} of {shape[1]} elements)")
-        return ld
+            ptrs.append(None)
+            continue
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+            _head_refuse(name, t, shape, dtype, index)
+        ptrs.append(t.data_ptr())
+    return ptrs
 
-    def dense(self, name, t, shape, dtype=None):
-        """A contiguous tensor, or None."""
-        if t is None:
-            self.ptrs.append(None)
-            return
-        self._take(name, t, shape, self.dtype if dtype is None else dtype)
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: must be contiguous")
 
-    def unaligned(self, *which):
-        """Whether one of these tensors (by their order) is off 16-byte alignment."""
-        return int(any(self.ptrs[i] & 15 for i in which))
-
-    def call(self, name, desc, query, workspace, stream):
-        L = lib()
-        if stream is None:
-            st = _current_stream(self.index)
-        else:
-            st = stream if isinstance(stream, int) else stream.cuda_stream
-        ref = ctypes.byref(desc)
-        if query is None:
-            _check(name, getattr(L, name)(ref, *self.ptrs, st))
-            return
-        if workspace is None:
-            need = getattr(L, query)(ref)
-            wp, wn = (None, 0) if need == 0 else _workspace(None, need, self.torch.device("cuda", self.index), stream)
-        else:
+def _head_call(name, query, desc, ptrs, index, workspace, stream):
+    """The entry point on checked pointers; query: its workspace query, or None if it takes no workspace."""
+    L = lib()
+    if stream is None:
+        st = _current_stream(index)
+    else:
+        st = stream if isinstance(stream, int) else stream.cuda_stream
+    ref = ctypes.byref(desc)
+    if query is None:
+        status = getattr(L, name)(ref, *ptrs, st)
+    else:
+        if workspace is not None:
             wp, wn = _workspace(workspace, 0, None)
-        _check(name, getattr(L, name)(ref, *self.ptrs, wp, wn, st))
+        else:
+            wp, wn = None, getattr(L, query)(ref)
+            if wn:
+                import torch
+                wp, wn = _workspace(None, wn, torch.device("cuda", index), stream)
+        status = getattr(L, name)(ref, *ptrs, wp, wn, st)
+    if status != 0:
+        raise QLError(name, status)
 
 
 def _head_act(act):
@@ -705,39 +708,53 @@ def _head_act(act):
         raise ValueError(f"act {act!r}: one of {', '.join(HEAD_ACTS)} is required") from None
 
 
+def _unaligned(*ptrs):
+    return 1 if any(p is not None and p & 15 for p in ptrs) else 0
+
+
 def qhead_linear_fwd(x, w, b, res, y, z=None, act="none", workspace=None, stream=None):
     """y = act(x w^T + b) + res; z, if given, receives x w^T + b.
 
     x (m, k), w (n, k), y, res and z (m, n) of one dtype, b (n) float32; b and res may be None."""
-    o = _HeadOperands(x)
+    i, dt, code = _head_first(x, "x")
     m, k = x.shape
     n = w.shape[0]
-    ldx = o.rows("x", x, (m, k))
-    ldw = o.rows("w", w, (n, k))
-    o.dense("b", b, (n,), o.torch.float32)
-    ldr = o.rows("res", res, (m, n))
-    ldy = o.rows("y", y, (m, n))
-    o.dense("z", z, (m, n))
-    o.call("qhead_linear_fwd", HeadLinearDesc(m, k, n, ldx, ldw, ldr, ldy, o.code, _head_act(act), o.unaligned(0, 1)),
-           "qhead_linear_fwd_workspace_size", workspace, stream)
+    px, ldx = _head_rows("x", x, (m, k), dt, i)
+    pw, ldw = _head_rows("w", w, (n, k), dt, i)
+    pr, ldr = _head_rows("res", res, (m, n), dt, i)
+    py, ldy = _head_rows("y", y, (m, n), dt, i)
+    pb, pz = _head_dense(i, ("b", b, (n,), _float32()), ("z", z, (m, n), dt))
+    _head_call("qhead_linear_fwd", "qhead_linear_fwd_workspace_size",
+               HeadLinearDesc(m, k, n, ldx, ldw, ldr, ldy, code, _head_act(act), _unaligned(px, pw)),
+               (px, pw, pb, pr, py, pz), i, workspace, stream)
 
 
 def qhead_linear_bwd(x, w, dy, z=None, dx=None, dw=None, db=None, act="none", workspace=None, stream=None):
     """The gradients of qhead_linear_fwd from dy = dl/dy and the z it stored (z may be None for act "none").
 
     dx (m, k) and dw (n, k) of the dtype of x, db (n) float32; each may be None."""
-    o = _HeadOperands(x)
+    i, dt, code = _head_first(x, "x")
     m, k = x.shape
     n = w.shape[0]
-    ldx = o.rows("x", x, (m, k))
-    ldw = o.rows("w", w, (n, k))
-    ldy = o.rows("dy", dy, (m, n))
-    o.dense("z", z, (m, n))
-    o.dense("dx", dx, (m, k))
-    o.dense("dw", dw, (n, k))
-    o.dense("db", db, (n,), o.torch.float32)
-    o.call("qhead_linear_bwd", HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, o.code, _head_act(act), o.unaligned(0, 1, 2)),
-           "qhead_linear_bwd_workspace_size", workspace, stream)
+    px, ldx = _head_rows("x", x, (m, k), dt, i)
+    pw, ldw = _head_rows("w", w, (n, k), dt, i)
+    pdy, ldy = _head_rows("dy", dy, (m, n), dt, i)
+    rest = _head_dense(i, ("z", z, (m, n), dt), ("dx", dx, (m, k), dt), ("dw", dw, (n, k), dt), ("db", db, (n,), _float32()))
+    _head_call("qhead_linear_bwd", "qhead_linear_bwd_workspace_size",
+               HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, code, _head_act(act), _unaligned(px, pw, pdy)),
+               (px, pw, pdy, *rest), i, workspace, stream)
+
+
+def _float32():
+    return _torch_types()[0]
+
+
+def _torch_types(types=[]):
+    """(float32, int64) of torch, which importing this module does not import."""
+    if not types:
+        import torch
+        types += [torch.float32, torch.int64]
+    return types
 
 
 def qhead_logprobs_fwd(logits, target, logp, entropy=None, lse=None, top_logp=None, top_ids=None, stats=None,
@@ -747,50 +764,44 @@ def qhead_logprobs_fwd(logits, target, logp, entropy=None, lse=None, top_logp=No
     logits (rows, vocab); target (rows) int64, negative where there is none; logp, entropy, lse
     (rows) float32; top_logp float32 and top_ids int64 (rows, K): the K most likely tokens;
     stats (rows, 2) float32: for qhead_logprobs_bwd."""
-    o = _HeadOperands(logits)
-    f32, i64 = o.torch.float32, o.torch.int64
+    i, dt, code = _head_first(logits, "logits")
+    f32, i64 = _torch_types()
     rows, vocab = logits.shape
-    ld = o.rows("logits", logits, (rows, vocab))
+    p, ld = _head_rows("logits", logits, (rows, vocab), dt, i)
     if (top_logp is None) != (top_ids is None):
         raise ValueError("top_logp and top_ids: both or neither")
     top = 0 if top_logp is None else top_logp.shape[-1]
-    o.dense("target", target, (rows,), i64)
-    o.dense("logp", logp, (rows,), f32)
-    o.dense("entropy", entropy, (rows,), f32)
-    o.dense("lse", lse, (rows,), f32)
-    o.dense("top_logp", top_logp, (rows, top), f32)
-    o.dense("top_ids", top_ids, (rows, top), i64)
-    o.dense("stats", stats, (rows, 2), f32)
-    o.call("qhead_logprobs_fwd", HeadRowsDesc(rows, vocab, ld, top, o.code, temperature, 0.0),
-           "qhead_logprobs_fwd_workspace_size", workspace, stream)
+    r, k = (rows,), (rows, top)
+    ptrs = _head_dense(i, ("target", target, r, i64), ("logp", logp, r, f32), ("entropy", entropy, r, f32), ("lse", lse, r, f32),
+                       ("top_logp", top_logp, k, f32), ("top_ids", top_ids, k, i64), ("stats", stats, (rows, 2), f32))
+    _head_call("qhead_logprobs_fwd", "qhead_logprobs_fwd_workspace_size",
+               HeadRowsDesc(rows, vocab, ld, top, code, temperature, 0.0), (p, *ptrs), i, workspace, stream)
 
 
 def qhead_logprobs_bwd(logits, target, stats, entropy, g, h, dlogits, temperature=1.0, stream=None):
     """dlogits (rows, vocab) from g = dl/dlogp and h = dl/dentropy (rows, float32; h may be None)."""
-    o = _HeadOperands(logits)
-    f32 = o.torch.float32
+    i, dt, code = _head_first(logits, "logits")
+    f32, i64 = _torch_types()
     rows, vocab = logits.shape
-    ld = o.rows("logits", logits, (rows, vocab))
-    o.dense("target", target, (rows,), o.torch.int64)
-    o.dense("stats", stats, (rows, 2), f32)
-    o.dense("entropy", entropy, (rows,), f32)
-    o.dense("g", g, (rows,), f32)
-    o.dense("h", h, (rows,), f32)
-    o.dense("dlogits", dlogits, (rows, vocab))
-    o.call("qhead_logprobs_bwd", HeadRowsDesc(rows, vocab, ld, 0, o.code, temperature, 0.0), None, None, stream)
+    p, ld = _head_rows("logits", logits, (rows, vocab), dt, i)
+    r = (rows,)
+    ptrs = _head_dense(i, ("target", target, r, i64), ("stats", stats, (rows, 2), f32), ("entropy", entropy, r, f32),
+                       ("g", g, r, f32), ("h", h, r, f32), ("dlogits", dlogits, (rows, vocab), dt))
+    _head_call("qhead_logprobs_bwd", None, HeadRowsDesc(rows, vocab, ld, 0, code, temperature, 0.0), (p, *ptrs), i, None, stream)
 
 
 def _head_distill(logits, t_ids, t_logits, labels, temperature, alpha):
-    o = _HeadOperands(logits)
+    """(device index, dtype, rows, vocab, descriptor, pointers) of what the distillation calls share."""
+    i, dt, code = _head_first(logits, "logits")
     rows, vocab = logits.shape
-    ld = o.rows("logits", logits, (rows, vocab))
+    p, ld = _head_rows("logits", logits, (rows, vocab), dt, i)
     if (t_ids is None) != (t_logits is None):
         raise ValueError("t_ids and t_logits: both or neither")
     top = 0 if t_ids is None else t_ids.shape[-1]
-    o.dense("t_ids", t_ids, (rows, top), o.torch.int64)
-    o.dense("t_logits", t_logits, (rows, top))
-    o.dense("labels", labels, (rows,), o.torch.int64)
-    return o, rows, vocab, HeadRowsDesc(rows, vocab, ld, top, o.code, temperature, alpha)
+    i64 = _torch_types()[1]
+    ptrs = _head_dense(i, ("t_ids", t_ids, (rows, top), i64), ("t_logits", t_logits, (rows, top), dt),
+                       ("labels", labels, (rows,), i64))
+    return i, dt, rows, vocab, HeadRowsDesc(rows, vocab, ld, top, code, temperature, alpha), (p, *ptrs)
 
 
 def qhead_distill_fwd(logits, t_ids, t_logits, labels, loss, stats=None, temperature=1.0, alpha=1.0, workspace=None,
@@ -799,26 +810,23 @@ def qhead_distill_fwd(logits, t_ids, t_logits, labels, loss, stats=None, tempera
 
     logits (rows, vocab); t_ids int64 (negative: an empty place) and t_logits (rows, K), or both None; labels
     (rows) int64 (negative: none), or None; loss float32; stats (rows, 4) float32: for qhead_distill_bwd."""
-    o, rows, _, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
-    o.dense("loss", loss, (rows,), o.torch.float32)
-    o.dense("stats", stats, (rows, 4), o.torch.float32)
-    o.call("qhead_distill_fwd", d, "qhead_distill_workspace_size", workspace, stream)
+    i, _, rows, _, d, ptrs = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    more = _head_dense(i, ("loss", loss, (rows,), _float32()), ("stats", stats, (rows, 4), _float32()))
+    _head_call("qhead_distill_fwd", "qhead_distill_workspace_size", d, (*ptrs, *more), i, workspace, stream)
 
 
 def qhead_distill_bwd(logits, t_ids, t_logits, labels, stats, g, dlogits, temperature=1.0, alpha=1.0, stream=None):
     """dlogits (rows, vocab) from g = dl/dloss (rows, float32) and the stats of the forward."""
-    o, rows, vocab, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
-    o.dense("stats", stats, (rows, 4), o.torch.float32)
-    o.dense("g", g, (rows,), o.torch.float32)
-    o.dense("dlogits", dlogits, (rows, vocab))
-    o.call("qhead_distill_bwd", d, None, None, stream)
+    i, dt, rows, vocab, d, ptrs = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    more = _head_dense(i, ("stats", stats, (rows, 4), _float32()), ("g", g, (rows,), _float32()),
+                       ("dlogits", dlogits, (rows, vocab), dt))
+    _head_call("qhead_distill_bwd", None, d, (*ptrs, *more), i, None, stream)
 
 
 def qhead_distill_step(logits, t_ids, t_logits, labels, g, loss, dlogits, temperature=1.0, alpha=1.0, workspace=None,
                        stream=None):
     """The loss and its gradient in one call, for row weights g that are known beforehand."""
-    o, rows, vocab, d = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
-    o.dense("g", g, (rows,), o.torch.float32)
-    o.dense("loss", loss, (rows,), o.torch.float32)
-    o.dense("dlogits", dlogits, (rows, vocab))
-    o.call("qhead_distill_step", d, "qhead_distill_workspace_size", workspace, stream)
+    i, dt, rows, vocab, d, ptrs = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
+    more = _head_dense(i, ("g", g, (rows,), _float32()), ("loss", loss, (rows,), _float32()),
+                       ("dlogits", dlogits, (rows, vocab), dt))
+    _head_call("qhead_distill_step", "qhead_distill_workspace_size", d, (*ptrs, *more), i, workspace, stream)

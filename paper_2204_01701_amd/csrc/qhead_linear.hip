@@ -41,7 +41,9 @@ struct Product {
     Operand a, b;
 };
 
-enum Tile { TILE_ANY, TILE_FEW, TILE_128, TILE_256 };
+enum Tile { TILE_ANY, TILE_FEW, TILE_64, TILE_128, TILE_256 };
+int tile_rows(Tile t) { return t == TILE_256 ? 256 : 128; }
+int tile_cols(Tile t) { return t == TILE_256 ? 256 : t == TILE_128 ? 128 : 64; }
 struct ProductPlan {
     Tile tile;
     bool pad_a, pad_b;
@@ -51,15 +53,20 @@ struct ProductPlan {
 };
 
 // Time of a product in us by tile and splits: rounds of the workgroups over the CUs, each with its ramp and
-// epilogue; per K step of 64 bytes, 0.30 (bf16) or 1.03 (fp32) us with 128 x 128 tiles, also where two
-// share a CU, 0.86 or 3.66 with 256 x 256; the partial sums go out and come back at 4.5 TB/s, and
-// joining them is a launch.  Fitted on 30 shapes from 64 x 4096 x 4096 to 8192 x 8192 x 8192.
-double product_cost(const Product &q, ql_dtype t, bool large, int splits) {
-    const int B = large ? 256 : 128, steps = cdiv(q.R, 64 / (int)esize(t));
-    const double wgs = (double)cdiv(q.I, B) * cdiv(q.J, B) * splits, rounds = std::ceil(wgs / kNumCUs);
-    const double step = t == QL_BF16 ? (large ? 0.86 : 0.30) : (large ? 3.66 : 1.03);
+// epilogue; per K step of 64 bytes, also where two share a CU, kStepUs; the partial sums go out and come
+// back at 4.5 TB/s, and joining them is a launch.  Fitted on 30 shapes from 64 x 4096 x 4096 to 8192 x 8192 x 8192.
+// 256 x 256 tiles copy the fewest bytes per product; the small ones are for outputs of few tiles
+// (1021 x 1537, 1000 deep, fp32: 200 tiles of 128 x 64 fill the CUs without a split).
+constexpr double kStepUs[2][3] = {{0.54, 1.03, 3.66}, {0.20, 0.30, 0.86}};  // fp32, bf16; tiles 64, 128, 256
+double product_cost(const Product &q, ql_dtype t, Tile tile, int splits) {
+    const int steps = cdiv(q.R, 64 / (int)esize(t));
+    const double wgs = (double)cdiv(q.I, tile_rows(tile)) * cdiv(q.J, tile_cols(tile)) * splits;
     const double join = splits > 1 ? 3.5 + 8.0 * splits * (double)q.I * q.J / 4.5e6 : 0.0;
-    return (large ? 8.0 : 5.0) + step * cdiv(steps, splits) * rounds + join;
+    return (tile == TILE_256 ? 8.0 : 5.0) + kStepUs[t == QL_BF16][tile - TILE_64] * cdiv(steps, splits) * std::ceil(wgs / kNumCUs) + join;
+}
+// ... of the kernel for any layout, which loads element by element (64 x 64 tiles, four workgroups a CU)
+double any_cost(const Product &q, ql_dtype t) {
+    return 4.0 + 1.6 * cdiv(q.R, 64 / (int)esize(t)) * std::ceil((double)cdiv(q.I, 64) * cdiv(q.J, 64) / (4 * kNumCUs));
 }
 
 // al_a, al_b: whether the operands' pointers are (taken to be) 16-byte aligned.  km: both operands have t
@@ -76,9 +83,8 @@ ProductPlan plan_product(const Product &q, ql_dtype t, bool km, bool al_a, bool 
     }
     p.pad_a = !direct(q.a, t, al_a);
     p.pad_b = !direct(q.b, t, al_b);
-    const double flops = 2.0 * q.I * q.J * std::max(1, q.R);
     const bool fits = (!p.pad_a || pad_fits(q.a, t)) && (!p.pad_b || pad_fits(q.b, t));
-    if (!fits || ((p.pad_a || p.pad_b) && flops < 2e7) || q.R == 0 || forced == 1) {
+    if (!fits || q.R == 0 || forced == 1) {
         p.pad_a = p.pad_b = false;
         return p;
     }
@@ -86,19 +92,24 @@ ProductPlan plan_product(const Product &q, ql_dtype t, bool km, bool al_a, bool 
     const double cap = (double)kMaxSplitBytes / (4.0 * q.I * q.J);
     double best = 1e30;
     int want = 1;
-    for (int large = 0; large < 2; ++large)
+    for (Tile tile : {TILE_64, TILE_128, TILE_256})
         for (int s = 1; s == 1 || (s <= 16 && 4 * s <= steps && s <= cap); ++s) {
-            const double c = product_cost(q, t, large, s);
+            const double c = product_cost(q, t, tile, s);
             if (c >= best) continue;
             best = c;
-            p.tile = large ? TILE_256 : TILE_128;
+            p.tile = tile;
             want = s;
         }
-    if (forced) p.tile = forced == 256 ? TILE_256 : TILE_128;
+    // (a copy is a launch of 3 us and more)
+    if ((p.pad_a || p.pad_b) && !forced && any_cost(q, t) < best + 3.0 * ((int)p.pad_a + (int)p.pad_b)) {
+        p.tile = TILE_ANY;
+        p.pad_a = p.pad_b = false;
+        return p;
+    }
+    if (forced) p.tile = forced == 256 ? TILE_256 : forced == 128 ? TILE_128 : TILE_64;
     want = std::min(std::max(1, env_override("QHEAD_SPLITS", want)), steps);
-    const int B = p.tile == TILE_256 ? 256 : 128;
-    p.ti = cdiv(q.I, B);
-    p.tj = cdiv(q.J, B);
+    p.ti = cdiv(q.I, tile_rows(p.tile));
+    p.tj = cdiv(q.J, tile_cols(p.tile));
     p.per = cdiv(steps, want);
     p.splits = cdiv(steps, p.per);
     if (p.pad_a) p.a_bytes = align_up((size_t)q.a.rows * padded_cols(q.a, t) * esize(t));
@@ -134,8 +145,10 @@ ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_
     const dim3 grid((unsigned)(a.ti * a.tj * a.splits));
     if (p.tile == TILE_256)
         hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 256, 256, 2, 4, 4, 1, 2>), grid, dim3(512), 0, st, a);
-    else
+    else if (p.tile == TILE_128)
         hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 128, 2, 2, 4, 2, 4>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((qhead_gemm_kernel<T, ANAT, BNAT, 128, 64, 2, 2, 4, 2, 3>), grid, dim3(256), 0, st, a);
     if (a.splits > 1)
         hipLaunchKernelGGL((qhead_join_kernel<T>), dim3(grid_1d((long long)g.I * cdiv(g.J, 8))), dim3(kThreads), 0, st, a);
     return hip_status();
@@ -184,7 +197,7 @@ DzPlan plan_dz(const qhead_linear_desc *d, bool al) {
     const Operand dy{nullptr, d->m, d->n, d->ldy, false};
     p.store = d->act != QL_ACT_NONE || !direct(dy, d->dtype, al);
     p.ld = padded_cols(dy, d->dtype);
-    p.rpp = std::max(32, cdiv(d->m, 256));
+    p.rpp = std::max(32, cdiv(d->m, 128));
     p.parts = std::max(1, cdiv(d->m, p.rpp));
     p.dz_bytes = p.store ? align_up((size_t)d->m * p.ld * esize(d->dtype)) : 0;
     p.part_bytes = align_up((size_t)p.parts * d->n * sizeof(float));

@@ -116,7 +116,7 @@ def test_larger(m, k, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
-@pytest.mark.parametrize("tile,splits", [(128, 1), (128, 3), (256, 1), (256, 2), (1, 1)])
+@pytest.mark.parametrize("tile,splits", [(128, 1), (128, 3), (256, 1), (256, 2), (64, 1), (64, 2), (1, 1)])
 @pytest.mark.parametrize("m,k,n", [(300, 200, 264), (520, 1040, 128), (70, 96, 1031)])
 def test_every_tile(m, k, n, tile, splits, dtype, monkeypatch):
     """Each tile on the same product, whatever the size would choose."""
