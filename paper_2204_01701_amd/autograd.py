@@ -259,11 +259,21 @@ def quad_linear(x, wa, wb=None, wc=None, ba=None, bb=None, bc=None, recompute=Fa
 
 def _matrix(t):
     """(..., c) as a matrix whose rows are contiguous and do not overlap (a view where there is one)."""
-    t = t.reshape(-1, t.shape[-1]) if t.numel() else t.new_empty((t.shape[:-1].numel(), t.shape[-1]))
+    if t.dim() != 2:
+        t = t.reshape(-1, t.shape[-1]) if t.numel() else t.new_empty((t.shape[:-1].numel(), t.shape[-1]))
     rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-        t = t.contiguous()
-    return t
+    ld, step = t.stride()
+    return t.contiguous() if (cols > 1 and step != 1) or (rows > 1 and ld < cols) else t
+
+
+def _column(t, rows):
+    """A gradient or target per row as a contiguous vector."""
+    return (t if t.dim() == 1 else t.reshape(rows)).contiguous()
+
+
+def _float_column(t, rows):
+    t = _column(t, rows)
+    return t if t.dtype is torch.float32 else t.float()
 
 
 class LinearActFunction(torch.autograd.Function):
@@ -314,20 +324,21 @@ class TokenLogprobsFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, target, temperature, top):
         ctx.set_materialize_grads(False)
-        _same_device(logits, target)
-        z = _matrix(logits)
-        rows, lead = z.shape[0], logits.shape[:-1]
-        if target.shape != lead or target.dtype != torch.int64:
+        lead = logits.shape[:-1]
+        if target.shape != lead or target.dtype is not torch.int64:
             raise ValueError(f"target must be int64 of shape {tuple(lead)}, got {target.dtype} {tuple(target.shape)}")
-        t = target.reshape(rows).contiguous()
-        logp, entropy = torch.empty((2, rows), device=z.device).unbind(0)
-        stats = torch.empty((rows, 2), device=z.device) if ctx.needs_input_grad[0] else None
-        top_logp = torch.empty((rows, top), device=z.device) if top else None
-        top_ids = torch.empty((rows, top), device=z.device, dtype=torch.int64) if top else None
-        qhead_logprobs_fwd(z, t, logp, entropy, None, top_logp, top_ids, stats, temperature=temperature)
-        ctx.temperature, ctx.shape = temperature, logits.shape
-        ctx.save_for_backward(z, t, stats, entropy)
-        out = logp.view(lead), entropy.view(lead)
+        z = _matrix(logits)
+        rows, dev = z.shape[0], z.device
+        t = _column(target, rows)
+        logp, entropy = torch.empty(rows, device=dev), torch.empty(rows, device=dev)
+        stats = torch.empty((rows, 2), device=dev) if ctx.needs_input_grad[0] else None
+        top_logp = torch.empty((rows, top), device=dev) if top else None
+        top_ids = torch.empty((rows, top), device=dev, dtype=torch.int64) if top else None
+        qhead_logprobs_fwd(z, t, logp, entropy, None, top_logp, top_ids, stats, temperature)
+        if stats is not None:
+            ctx.temperature, ctx.shape = temperature, logits.shape
+            ctx.save_for_backward(z, t, stats, entropy)
+        out = (logp, entropy) if len(lead) == 1 else (logp.view(lead), entropy.view(lead))
         if not top:
             return out
         more = top_logp.view(lead + (top,)), top_ids.view(lead + (top,))
@@ -336,15 +347,15 @@ class TokenLogprobsFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, g, h, *_):
-        z, t, stats, entropy = ctx.saved_tensors
         if g is None and h is None:
             return None, None, None, None
+        z, t, stats, entropy = ctx.saved_tensors
         rows = z.shape[0]
-        g = g.reshape(rows).contiguous().float() if g is not None else torch.zeros(rows, device=z.device)
-        h = h.reshape(rows).contiguous().float() if h is not None else None
+        g = _float_column(g, rows) if g is not None else torch.zeros(rows, device=z.device)
+        h = _float_column(h, rows) if h is not None else None
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
-        qhead_logprobs_bwd(z, t, stats, entropy, g, h, dz, temperature=ctx.temperature)
-        return dz.view(ctx.shape), None, None, None
+        qhead_logprobs_bwd(z, t, stats, entropy.view(rows), g, h, dz, ctx.temperature)
+        return dz if dz.shape == ctx.shape else dz.view(ctx.shape), None, None, None
 
 
 def token_logprobs(logits, target, temperature=1.0, top=0):
@@ -359,30 +370,33 @@ def token_logprobs(logits, target, temperature=1.0, top=0):
 class DistillLossFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, t_ids, t_logits, labels, temperature, alpha):
-        _same_device(logits, t_ids, t_logits, labels)
-        z = _matrix(logits)
-        rows, lead = z.shape[0], logits.shape[:-1]
-        for name, t in (("teacher_ids", t_ids), ("teacher_logits", t_logits)):
-            if t is not None and t.shape[:-1] != lead:
-                raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit logits of shape {tuple(logits.shape)}")
+        lead = logits.shape[:-1]
+        if (t_ids is not None and t_ids.shape[:-1] != lead) or (t_logits is not None and t_logits.shape[:-1] != lead):
+            raise ValueError(f"the teacher's places do not fit logits of shape {tuple(logits.shape)}")
         if labels is not None and labels.shape != lead:
             raise ValueError(f"labels: shape {tuple(labels.shape)}, expected {tuple(lead)}")
-        ids = t_ids.reshape(rows, t_ids.shape[-1]).contiguous() if t_ids is not None else None
-        tz = t_logits.reshape(rows, t_logits.shape[-1]).to(z.dtype).contiguous() if t_logits is not None else None
-        y = labels.reshape(rows).contiguous() if labels is not None else None
-        loss = torch.empty(rows, device=z.device)
-        stats = torch.empty((rows, 4), device=z.device) if ctx.needs_input_grad[0] else None
-        qhead_distill_fwd(z, ids, tz, y, loss, stats, temperature=temperature, alpha=alpha)
-        ctx.save_for_backward(z, ids, tz, y, stats)
-        ctx.how, ctx.shape = dict(temperature=temperature, alpha=alpha), logits.shape
-        return loss.view(lead)
+        z = _matrix(logits)
+        rows, dev = z.shape[0], z.device
+        if t_ids is not None and t_logits is not None:
+            if t_ids.dim() != 2:
+                t_ids, t_logits = (v.reshape(rows, v.shape[-1]) for v in (t_ids, t_logits))
+            t_ids, t_logits = t_ids.contiguous(), t_logits.to(z.dtype).contiguous()
+        if labels is not None:
+            labels = _column(labels, rows)
+        loss = torch.empty(rows, device=dev)
+        stats = torch.empty((rows, 4), device=dev) if ctx.needs_input_grad[0] else None
+        qhead_distill_fwd(z, t_ids, t_logits, labels, loss, stats, temperature, alpha)
+        if stats is not None:
+            ctx.save_for_backward(z, t_ids, t_logits, labels, stats)
+            ctx.how, ctx.shape = (temperature, alpha), logits.shape
+        return loss if len(lead) == 1 else loss.view(lead)
 
     @staticmethod
     def backward(ctx, g):
-        z, ids, tz, y, stats = ctx.saved_tensors
+        z, ids, tz, labels, stats = ctx.saved_tensors
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
-        qhead_distill_bwd(z, ids, tz, y, stats, g.reshape(z.shape[0]).contiguous().float(), dz, **ctx.how)
-        return dz.view(ctx.shape), None, None, None, None, None
+        qhead_distill_bwd(z, ids, tz, labels, stats, _float_column(g, z.shape[0]), dz, *ctx.how)
+        return dz if dz.shape == ctx.shape else dz.view(ctx.shape), None, None, None, None, None
 
 
 def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1.0, alpha=1.0):

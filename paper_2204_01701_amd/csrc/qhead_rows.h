@@ -39,7 +39,7 @@ template <typename T> struct HeadRow {
     static constexpr int VEC = Elem<T>::VEC;
     const T *p;
     int V, nfull, nvec;  // elements, whole vectors, vectors with the partial one
-    __device__ __forceinline__ HeadRow(const T *row, int v) : p(row), V(v), nfull(v / VEC), nvec((v + VEC - 1) / VEC) {}
+    __device__ __forceinline__ HeadRow(const T *row, int v) : p(row), V(v), nfull(v / VEC), nvec((v - 1) / VEC + 1) {}
     __device__ __forceinline__ v4u load(int j) const { return *reinterpret_cast<const v4u_any *>(p + (size_t)j * VEC); }
     // The vector behind the whole ones, -inf past the row's end.
     __device__ __forceinline__ v4u partial() const {

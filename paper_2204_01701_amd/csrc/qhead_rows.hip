@@ -54,7 +54,7 @@ Split grad_split(const qhead_rows_desc *d) { return split_rows(d->rows, vectors(
 
 template <typename T> void launch_logprobs(const HeadLogprobArgs &a, int rows, hipStream_t st) {
     const dim3 grid((unsigned)((long long)rows * a.splits));
-    const int nvec = cdiv(a.V, Elem<T>::VEC);
+    const int nvec = cdiv((long long)a.V, Elem<T>::VEC);
     // one wave where a row is at most one vector a lane, or short and one of many
     const bool one = nvec <= 64, wave = nvec <= 1024 && many_rows(rows);
     if (a.K) {
@@ -123,7 +123,7 @@ void launch_row_as(const HeadDistillArgs &a, int rows, hipStream_t st) {
 // fewer threads beat 8 on more (1023 of 50001, bf16, both terms: 68 against 83; 4096 of 32768: 133, 146), but
 // not in fp32 up to 4096 vectors (2048 of 16000: 65, 60).
 template <typename T, bool TWO, bool GRAD> void launch_row(const HeadDistillArgs &a, int rows, hipStream_t st) {
-    const int nvec = cdiv(a.V, Elem<T>::VEC);
+    const int nvec = cdiv((long long)a.V, Elem<T>::VEC);
     const bool many = many_rows(rows);
     if (nvec <= 64) return launch_row_as<T, 64, 1, TWO, GRAD, GRAD>(a, rows, st);
     if (nvec <= 256 && many) return launch_row_as<T, 64, 4, TWO, GRAD, GRAD>(a, rows, st);
