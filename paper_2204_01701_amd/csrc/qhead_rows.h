@@ -335,11 +335,42 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
     __syncthreads();
 }
 
+// Candidates well over K (short rows, whose blocks bound little): bounded once more by themselves, since
+// ranking takes n^2 steps (4000 rows of 600, K = 128, bf16: 189 us without).
+template <int TH> __device__ __forceinline__ void head_top_prune(HeadTopLds<TH> &s, int K) {
+    constexpr int CAP = head_cap(TH), PER = CAP / TH, W = TH / 64;
+    const int tid = threadIdx.x, n = s.n;
+    uint64_t mine[PER];
+    uint32_t key[PER];
+    int own = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        mine[q] = q * TH + tid < n ? s.buf[q * TH + tid] : 0;
+        key[q] = (uint32_t)(mine[q] >> 32);
+        own += min(max(n - q * TH - (tid & ~63), 0), 64);
+    }
+    uint32_t least = own ? head_wave_kth(key, (K * own + n - 1) / n) : 0xffffffffu;
+    if ((tid & 63) == 0) s.kth[tid >> 6] = least;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) least = min(least, s.kth[w]);
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    int kept = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) kept += mine[q] != 0 && key[q] >= least ? 1 : 0;
+    int at = head_append(kept, &s.n);
+#pragma unroll
+    for (int q = 0; q < PER; ++q)
+        if (mine[q] != 0 && key[q] >= least) s.buf[at++] = mine[q];
+    __syncthreads();
+}
+
 // The K largest of vectors [start, end) of a row, into s.best.  While they were read, s.top got the upper
 // halves of the largest keys of blocks of `rows` x one vector a thread; quarter[i]: the thread's largest
 // value in blocks i mod 4.  These maxima belong to distinct elements, so a value that K of them reach
-// (each wave contributing its share of K) bounds the K-th largest from below; only blocks that reach
-// it are read again: a little more than K of them, whatever the row's length.
+// (each wave contributing a share of K by how many it has) bounds the K-th largest from below; only
+// blocks that reach it are read again: a little more than K of them, whatever the row's length.
 template <typename T, int TH>
 __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z, const float (&quarter)[4], int K, int start,
                                          int end, int rows) {
@@ -349,7 +380,15 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
 #pragma unroll
     for (int i = 0; i < 4; ++i)  // (a maximum of -inf may stand for nothing, or for NaN: it vouches for neither)
         key[i] = quarter[i] > -__builtin_inff() ? head_key(quarter[i]) : 0u;
-    uint32_t least = head_wave_kth(key, (K + W - 1) / W);
+    int all = 0, own = 0;  // maxima there are in the workgroup, in this wave
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = end - start - i * rows * TH;
+        all += min(max(left, 0), TH);
+        own += min(max(left - (tid & ~63), 0), 64);
+    }
+    uint32_t least = K <= all ? head_wave_kth(key, (K * own + all - 1) / all) : 0u;
+    if (own == 0) least = 0xffffffffu;
     if (lane == 0) s.kth[tid >> 6] = least;
     if (tid == 0) s.n = s.blocks = 0;
     __syncthreads();
@@ -375,6 +414,7 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
         __syncthreads();
     }
     if (blocks > CAP || s.n > CAP) head_top_crowd<T, TH>(s, z, K, start, end, least);
+    if (s.n > K + K / 2 + 64) head_top_prune<TH>(s, K);
     head_rank<TH>(s.buf, s.n, s.best, K);
 }
 

@@ -55,8 +55,9 @@ Split grad_split(const qhead_rows_desc *d) { return split_rows(d->rows, vectors(
 template <typename T> void launch_logprobs(const HeadLogprobArgs &a, int rows, hipStream_t st) {
     const dim3 grid((unsigned)((long long)rows * a.splits));
     const int nvec = cdiv((long long)a.V, Elem<T>::VEC);
-    // one wave where a row is at most one vector a lane, or short and one of many
-    const bool one = nvec <= 64, wave = nvec <= 1024 && many_rows(rows);
+    // One wave where a row is at most one vector a lane, or short and one of many, unless K is large for the bound
+    // that its few lanes' maxima give (4000 rows of 700, K = 64, bf16: 64 us, four waves 20).
+    const bool one = nvec <= 64, wave = nvec <= 1024 && 4 * a.K <= nvec && many_rows(rows);
     if (a.K) {
         if (one) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, true>), grid, dim3(64), 0, st, a);
         else if (wave) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 4, true>), grid, dim3(64), 0, st, a);

@@ -93,7 +93,8 @@ def _check_score(z, zd, target, top, t):
 
 
 SIZES = [(3, 1, 1), (5, 2, 2), (4, 7, 7), (6, 10, 3), (3, 63, 20), (2, 64, 64), (3, 257, 128), (2, 512, 40), (2, 513, 128), (3, 1000, 5),
-         (2, 2049, 64), (2, 4099, 20), (1, 16384, 128), (2, 33001, 64), (1, 70001, 128), (600, 130, 4), (0, 50, 3)]
+         (2, 2049, 64), (2, 4099, 20), (1, 16384, 128), (2, 33001, 64), (1, 70001, 128), (600, 130, 4), (0, 50, 3),
+         (3, 1600, 128), (3, 1040, 128), (2, 2040, 64), (2100, 600, 128), (2100, 700, 64), (2100, 3001, 64)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
