@@ -204,7 +204,7 @@ template <int TH> struct HeadTopLds {
     };
     uint64_t best[kHeadTopMax];          // the K best in order
     uint16_t block[CAP];
-    uint32_t kth[TH / 64];
+    int hist[256], pick[2];
     int wave[TH / 64];
     int n, blocks;                       // candidates and blocks found (those past CAP were not kept)
 };
@@ -221,6 +221,55 @@ template <int N> __device__ __forceinline__ uint32_t head_wave_kth(const uint32_
 #pragma unroll
         for (int i = 0; i < N; ++i) n += __popcll(__ballot(key[i] >= up));
         if (n >= j) t = up;
+    }
+    return t;
+}
+
+// The same over the workgroup, exactly: two histograms of 8 bits, read from their upper ends by the first
+// wave.  (Each wave's share of j, and the least of their answers, took fewer barriers but bounded rows whose
+// large values lie together, sorted ones say, by far too little: 1333 us for 4096 rows of 32768, K = 64.)
+// Keys of 0 are none; 0 if there are fewer than j.
+template <int TH, int N> __device__ __forceinline__ uint32_t head_block_kth(const uint32_t (&key)[N], int j, int *hist, int *pick) {
+    if constexpr (TH == 64) return head_wave_kth(key, j);
+    const int tid = threadIdx.x;
+    uint32_t t = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (key[i] != 0 && (half == 0 || key[i] >> 24 == t >> 24)) atomicAdd(&hist[key[i] >> (half ? 16 : 24) & 255], 1);
+        __syncthreads();
+        if (tid < 64) {
+            int c[4], sum = 0;  // this lane's four bins, and the keys above them
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * tid - i];
+            int x = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(x, o);
+                if (tid >= o) x += y;
+            }
+            const int total = __shfl(x, 63);
+            int above = x - sum;
+            if (tid == 0 && total < j) pick[0] = -1;
+            if (above < j && x >= j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (above < j && above + c[i] >= j) {
+                        pick[0] = 255 - 4 * tid - i;
+                        pick[1] = j - above;
+                    }
+                    above += c[i];
+                }
+            }
+        }
+        __syncthreads();
+        const int bin = pick[0];
+        if (bin < 0) return 0;  // (the same for all)
+        j = pick[1];
+        t |= (uint32_t)bin << (half ? 16 : 24);
     }
     return t;
 }
@@ -296,7 +345,7 @@ template <typename T> __device__ __forceinline__ uint64_t head_key_of(const v4u 
 
 // Too many candidates (equal values, mostly: a masked or constant row): the K-th largest key of the
 // vectors [start, end) by bisection over re-reads, then what lies above it and the first ones equal
-// to it in the order of their indices.  Leaves K candidates.
+// to it in the order of their indices.  Leaves K candidates or more.
 template <typename T, int TH>
 __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<T> &z, int K, int start, int end, uint32_t least) {
     constexpr int VEC = Elem<T>::VEC;
@@ -308,6 +357,23 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
         head_prefix<TH>(n, total, s.wave);
         return total;
     };
+    if (least <= kKeyNegInf) {  // a mask that leaves few: all of them are candidates
+        const int finite = count(kKeyNegInf + 1);
+        if (finite >= K && finite <= head_cap(TH)) {
+            if (tid == 0) s.n = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int j = start + tid; j < end; j += TH) {
+                v4u r;
+                uint32_t mine = head_mask<T>(z, j, end, kKeyNegInf + 1, r);
+                if (!mine) continue;
+                int to = atomicAdd(&s.n, __popc(mine));
+                for (; mine; mine &= mine - 1, ++to) s.buf[to] = head_key_of<T>(r, __builtin_ctz(mine), j * VEC + __builtin_ctz(mine));
+            }
+            __syncthreads();
+            return;
+        }
+    }
     uint32_t lo = least, hi = 0xffffffffu;  // count(lo) >= K > count(hi)
     if (count(lo + 1) < K) hi = lo + 1;     // rows of one value, and, in two more counts, masked ones
     if (hi - lo > 1 && lo < kKeyNegInf && count(kKeyNegInf + 1) < K) hi = kKeyNegInf + 1;
@@ -338,22 +404,17 @@ __device__ __forceinline__ void head_top_crowd(HeadTopLds<TH> &s, const HeadRow<
 // Candidates well over K (short rows, whose blocks bound little): bounded once more by themselves, since
 // ranking takes n^2 steps (4000 rows of 600, K = 128, bf16: 189 us without).
 template <int TH> __device__ __forceinline__ void head_top_prune(HeadTopLds<TH> &s, int K) {
-    constexpr int CAP = head_cap(TH), PER = CAP / TH, W = TH / 64;
+    constexpr int PER = head_cap(TH) / TH;
     const int tid = threadIdx.x, n = s.n;
     uint64_t mine[PER];
     uint32_t key[PER];
-    int own = 0;
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
         mine[q] = q * TH + tid < n ? s.buf[q * TH + tid] : 0;
         key[q] = (uint32_t)(mine[q] >> 32);
-        own += min(max(n - q * TH - (tid & ~63), 0), 64);
     }
-    uint32_t least = own ? head_wave_kth(key, (K * own + n - 1) / n) : 0xffffffffu;
-    if ((tid & 63) == 0) s.kth[tid >> 6] = least;
+    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick);
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) least = min(least, s.kth[w]);
     if (tid == 0) s.n = 0;
     __syncthreads();
     int kept = 0;
@@ -368,32 +429,21 @@ template <int TH> __device__ __forceinline__ void head_top_prune(HeadTopLds<TH> 
 
 // The K largest of vectors [start, end) of a row, into s.best.  While they were read, s.top got the upper
 // halves of the largest keys of blocks of `rows` x one vector a thread; quarter[i]: the thread's largest
-// value in blocks i mod 4.  These maxima belong to distinct elements, so a value that K of them reach
-// (each wave contributing a share of K by how many it has) bounds the K-th largest from below; only
-// blocks that reach it are read again: a little more than K of them, whatever the row's length.
+// value in blocks i mod 4.  These maxima belong to distinct elements, so the K-th largest of them bounds
+// the row's K-th from below; only blocks that reach it are read again: little more than K of them,
+// whatever the row's length.
 template <typename T, int TH>
 __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z, const float (&quarter)[4], int K, int start,
                                          int end, int rows) {
-    constexpr int VEC = Elem<T>::VEC, W = TH / 64, CAP = head_cap(TH);
-    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int VEC = Elem<T>::VEC, CAP = head_cap(TH);
+    const int tid = threadIdx.x;
     uint32_t key[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)  // (a maximum of -inf may stand for nothing, or for NaN: it vouches for neither)
         key[i] = quarter[i] > -__builtin_inff() ? head_key(quarter[i]) : 0u;
-    int all = 0, own = 0;  // maxima there are in the workgroup, in this wave
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int left = end - start - i * rows * TH;
-        all += min(max(left, 0), TH);
-        own += min(max(left - (tid & ~63), 0), 64);
-    }
-    uint32_t least = K <= all ? head_wave_kth(key, (K * own + all - 1) / all) : 0u;
-    if (own == 0) least = 0xffffffffu;
-    if (lane == 0) s.kth[tid >> 6] = least;
     if (tid == 0) s.n = s.blocks = 0;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) least = min(least, s.kth[w]);
+    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick);
+    if constexpr (TH == 64) __syncthreads();
     uint32_t mask = 0;
     for (int g = 0; start + g * rows * TH + tid < end; ++g) mask |= s.top[g * TH + tid] >= least >> 16 ? 1u << g : 0u;
     int at = head_append(__popc(mask), &s.blocks);
@@ -522,8 +572,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
     extern __shared__ uint64_t cand[];  // splits x K
     __shared__ uint64_t best[kHeadTopMax];
-    __shared__ uint32_t wave[4];
-    __shared__ int n;
+    __shared__ int hist[256], pick[2], n;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x, K = a.K, keys = a.splits * K;
     constexpr int PER = kHeadJoinKeys / 256;
@@ -536,12 +585,8 @@ __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArg
         uint32_t key[PER];
 #pragma unroll
         for (int q = 0; q < PER; ++q) key[q] = (uint32_t)(mine[q] >> 32);
-        uint32_t least = head_wave_kth(key, (K + 3) / 4);
         if (tid == 0) n = 0;
-        if ((tid & 63) == 0) wave[tid >> 6] = least;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 4; ++w) least = min(least, wave[w]);
+        const uint32_t least = head_block_kth<256>(key, K, hist, pick);
         int kept = 0;
 #pragma unroll
         for (int q = 0; q < PER; ++q) kept += mine[q] != 0 && key[q] >= least ? 1 : 0;
