@@ -55,7 +55,8 @@ extern "C" {
   copies that the descriptor shows (odd strides and sizes), and those of
   misaligned pointers if `unaligned` is set.  With a misaligned pointer and the
   flag unset results are the same, at lower speed.
- * Sizes: m >= 0, k >= 1, n >= 1, each below 2^31.
+ * Sizes: m >= 0, k >= 1, n >= 1; QL_EUNSUPPORTED within 65536 of 2^31, or where a product
+ * whose operands cannot be copied has more than 65535 x 64 columns.
  * ------------------------------------------------------------------------- */
 typedef enum { QL_ACT_NONE = 0, QL_ACT_RELU = 1, QL_ACT_GELU = 2, QL_ACT_GELU_TANH = 3, QL_ACT_SILU = 4 } ql_act;
 

@@ -8,7 +8,7 @@ library; this module only marshals arguments through ctypes: torch tensors
 become device pointers, the current HIP stream becomes the stream argument,
 and workspaces are allocated with torch when the caller passes none.
 
-Function names, argument order and layouts match ``include/qlayer.h``:
+Function names, argument order and layouts match ``include/qlayer.h`` (and ``qnet.h``, ``qhead.h``):
 activations NHWC, conv weights OHWI, dense X B x I and W O x I, biases and
 weight/bias gradients float32.  Every function raises ``QLError`` on a
 non-zero status.  There is no fallback: if the library is not built, the

@@ -18,6 +18,12 @@ bool linear_ok(const qhead_linear_desc *d) {
            (int)d->act >= QL_ACT_NONE && (int)d->act <= QL_ACT_SILU && d->ldx >= d->k && d->ldw >= d->k;
 }
 
+// (the kernels' counters run past a size by up to a few thousand)
+bool sizes_fit(const qhead_linear_desc *d) {
+    constexpr int most = 0x7fffffff - 65536;
+    return d->m <= most && d->k <= most && d->n <= most;
+}
+
 // --- one product ------------------------------------------------------------------------
 // An operand as the caller has it: `rows` rows of `cols` elements.  NAT: t is the row index.
 struct Operand {
@@ -76,7 +82,7 @@ ProductPlan plan_product(const Product &q, ql_dtype t, bool km, bool al_a, bool 
     p.splits = 1;
     const int forced = env_override("QHEAD_TILE", 0);
     // Up to 16 rows the weights are read in place, whatever their layout (1 row of 4096, 4096 outputs, bf16:
-    // 10 us a call from Python; 128 x 128 tiles over 8 splits 13).
+    // 11 us a call from Python; 128 x 128 tiles over 8 splits 13).
     if (km && q.I <= 16 && !forced) {
         p.tile = TILE_FEW;
         return p;
@@ -229,6 +235,7 @@ size_t qhead_linear_fwd_workspace_size(const qhead_linear_desc *d) {
 ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void *w, const float *b, const void *r,
                            void *y, void *z, void *workspace, size_t workspace_bytes, void *stream) {
     if (!linear_ok(d) || d->ldy < d->n || (r && d->ldr < d->n)) return QL_EINVAL;
+    if (!sizes_fit(d)) return QL_EUNSUPPORTED;
     if (d->m == 0) return QL_OK;
     if (!x || !w || !y) return QL_EINVAL;
     const void *ptrs[] = {x, w, r, y, z};
@@ -256,6 +263,7 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
                            void *dx, void *dw, float *db, void *workspace, size_t workspace_bytes, void *stream) {
     if (!linear_ok(d) || d->ldy < d->n) return QL_EINVAL;
     if (!dx && !dw && !db) return QL_EINVAL;
+    if (!sizes_fit(d)) return QL_EUNSUPPORTED;
     if (d->m > 0 && (!dy || (d->act != QL_ACT_NONE && !z) || (dx && !w) || (dw && !x))) return QL_EINVAL;
     const void *ptrs[] = {x, w, dy, z, dx, dw};
     for (const void *p : ptrs)

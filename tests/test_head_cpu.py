@@ -56,6 +56,12 @@ def test_linear_refuses_descriptors(L, bad):
         assert L.qhead_linear_bwd(lin(**bad), P, P, P, P, P, P, P, P, BIG, None) == EINVAL
 
 
+def test_linear_refuses_sizes_at_the_end_of_int(L):
+    for big in (dict(m=2**31 - 2), dict(k=2**31 - 2), dict(n=2**31 - 2)):
+        assert L.qhead_linear_fwd(lin(**big), P, P, P, P, P, None, P, BIG, None) == EUNSUPPORTED
+        assert L.qhead_linear_bwd(lin(**big), P, P, P, P, P, P, P, P, BIG, None) == EUNSUPPORTED
+
+
 def test_linear_refuses_pointers(L):
     for i in (0, 1, 4):  # x, w, y
         args = [P, P, P, P, P, None]
