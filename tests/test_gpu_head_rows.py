@@ -340,3 +340,47 @@ def test_long_offsets():
     want, grad, el, eg = ref.distill(host, ti.cpu(), tl.bfloat16().cpu(), None, 1.0, 1.0, torch.ones(5))
     ref.near(loss, want, el, torch.float32)
     ref.near(dz, grad, eg, torch.bfloat16)
+
+
+LONG = [(256, 2000, 20), (256, 9001, 128), (300, 20011, 64), (256, 40009, 32), (256, 70001, 20), (256, 140003, 128), (2100, 100, 7),
+        (2100, 601, 64), (2100, 2003, 128), (2100, 7001, 20)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("rows,vocab,top", LONG)
+def test_whole_rows(rows, vocab, top, dtype):
+    """Rows enough that each has a workgroup (or a wave) of its own, at every length that a kernel is chosen by; a few
+    of them, with special ones among these, against the definitions."""
+    special = _special(vocab, dtype, 5)
+    z = _logits(rows, vocab, dtype, 20)
+    at = torch.linspace(0, rows - 1, len(special) + 4).long()
+    z[at[:len(special)]] = special
+    g = _gen(rows, vocab, 21)
+    target = torch.randint(-1, vocab, (rows,), generator=g)
+    ids, tz = _teacher(rows, vocab, top, dtype, 22)
+    up = torch.randn(rows, generator=g)
+    zd = _place(z, 1, 2)
+    logp, ent, lse, tl, ti, stats = _score(zd, target, top, 1.3)
+    sub = z[at]
+    rl, rh, rs, el, eh, es = ref.logprobs(sub, target[at], 1.3)
+    for got, want, bound in ((logp, rl, el), (ent, rh, eh), (lse, rs, es)):
+        ref.near(got[at.to(DEV)], want, bound, torch.float32)
+    assert torch.equal(ti.cpu()[at], ref.rank(sub)[:, :top])
+    dz, ok = _guarded((rows, vocab), dtype)
+    ql.qhead_logprobs_bwd(zd, target.to(DEV), stats, ent, up.to(DEV), None, dz, temperature=1.3)
+    ref.near(dz[at.to(DEV)], *ref.logprobs_grad(sub, target[at], 1.3, up[at], None), dtype)
+    assert ok()
+    dev = lambda v: v.to(DEV)  # noqa: E731
+    for t, alpha, label in ((2.0, 1.0, None), (2.0, 0.4, target), (1.0, 0.4, target)):
+        want, grad, el, eg = ref.distill(sub, ids[at], tz[at], None if label is None else label[at], t, alpha, up[at])
+        more = (dev(ids), dev(tz), None if label is None else dev(label))
+        (loss, ok0), (dz, ok1) = _guarded((rows,), torch.float32), _guarded((rows, vocab), dtype)
+        ql.qhead_distill_step(zd, *more, dev(up), loss, dz, temperature=t, alpha=alpha)
+        ref.near(loss[at.to(DEV)], want, el, torch.float32)
+        ref.near(dz[at.to(DEV)], grad, eg, dtype)
+        assert ok0() and ok1()
+        ql.qhead_distill_fwd(zd, *more, loss, temperature=t, alpha=alpha)
+        ref.near(loss[at.to(DEV)], want, el, torch.float32)
+        over = z.to(DEV)  # in place
+        ql.qhead_distill_step(over, *more, dev(up), loss, over, temperature=t, alpha=alpha)
+        assert torch.equal(over.nan_to_num(3.0), dz.nan_to_num(3.0))
