@@ -539,17 +539,25 @@ __global__ __launch_bounds__(kThreads) void qhead_dz_kernel(const T *dy, long lo
     const int begin = blockIdx.y * rpp, end = min(m, begin + rpp);
     float s[8] = {};
     if (j < n)
-        for (int i = begin + rg; i < end; i += 8) {
-            float v[8], u[8];
-            head_load8<T>(dy + (size_t)i * ldy + j, v, n - j);
-            if (act != HEAD_NONE) {
-                head_load8<T>(z + (size_t)i * n + j, u, n - j);
-                head_slopes<8>(act, u, v);
-            }
-            // (elements behind the row's end loaded as 0 stay 0: a padded dz has zeros there)
-            if (dz) head_store8<T>(dz + (size_t)i * ldd + j, v, (int)min(ldd - j, 8LL));
+        for (int i0 = begin + rg; i0 < end; i0 += 32) {
+            float v[4][8], u[4][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += v[e];
+            for (int x = 0; x < 4; ++x) {  // (four rows requested together)
+                const int i = i0 + 8 * x;
+                if (i >= end) continue;
+                head_load8<T>(dy + (size_t)i * ldy + j, v[x], n - j);
+                if (act != HEAD_NONE) head_load8<T>(z + (size_t)i * n + j, u[x], n - j);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int i = i0 + 8 * x;
+                if (i >= end) continue;
+                if (act != HEAD_NONE) head_slopes<8>(act, u[x], v[x]);
+                // (elements behind the row's end loaded as 0 stay 0: a padded dz has zeros there)
+                if (dz) head_store8<T>(dz + (size_t)i * ldd + j, v[x], (int)min(ldd - j, 8LL));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += v[x][e];
+            }
         }
     if (!part) return;
 #pragma unroll

@@ -203,10 +203,11 @@ DzPlan plan_dz(const qhead_linear_desc *d, bool al) {
     const Operand dy{nullptr, d->m, d->n, d->ldy, false};
     p.store = d->act != QL_ACT_NONE || !direct(dy, d->dtype, al);
     p.ld = padded_cols(dy, d->dtype);
-    p.rpp = std::max(32, cdiv(d->m, 128));
+    // (up to 64 rows are one part, whose sums are db itself: a launch less)
+    p.rpp = d->m <= 64 ? std::max(1, d->m) : std::max(32, cdiv(d->m, 128));
     p.parts = std::max(1, cdiv(d->m, p.rpp));
     p.dz_bytes = p.store ? align_up((size_t)d->m * p.ld * esize(d->dtype)) : 0;
-    p.part_bytes = align_up((size_t)p.parts * d->n * sizeof(float));
+    p.part_bytes = p.parts > 1 ? align_up((size_t)p.parts * d->n * sizeof(float)) : 0;
     return p;
 }
 
@@ -276,11 +277,11 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
     const DzPlan p = plan_dz(d, !d->unaligned);
     char *ws = static_cast<char *>(workspace);
     void *dz = p.store && (dx || dw) ? ws : nullptr;
-    float *part = db ? reinterpret_cast<float *>(ws + p.dz_bytes) : nullptr;
-    if (dz || part) {
+    float *part = db && p.parts > 1 ? reinterpret_cast<float *>(ws + p.dz_bytes) : db;
+    if (dz || db) {
         if (d->dtype == QL_BF16) launch_dz<uint16_t>(d, p, dy, z, dz, part, st);
         else launch_dz<float>(d, p, dy, z, dz, part, st);
-        if (db) hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(cdiv(d->n, 32)), dim3(kThreads), 0, st, part, p.parts, d->n, db);
+        if (db && p.parts > 1) hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(cdiv(d->n, 32)), dim3(kThreads), 0, st, part, p.parts, d->n, db);
         const ql_status s = hip_status();
         if (s != QL_OK) return s;
     }
