@@ -231,51 +231,76 @@ template <int N> __device__ __forceinline__ uint32_t head_wave_kth(const uint32_
     return t;
 }
 
-// The same over the workgroup, exactly: two histograms of 8 bits, read from their upper ends by the first
-// wave.  (Each wave's share of j, and the least of their answers, took fewer barriers but bounded rows whose
-// large values lie together, sorted ones say, by far too little: 1333 us for 4096 rows of 32768, K = 64.)
-// Keys of 0 are none; 0 if there are fewer than j.
-template <int TH, int N> __device__ __forceinline__ uint32_t head_block_kth(const uint32_t (&key)[N], int j, int *hist, int *pick) {
+// First wave: the bin at which the counts of hist[0 .. 255], taken in order, reach j (pick[0], -1: they do
+// not), and how many of j are left for it (pick[1]).
+__device__ __forceinline__ void head_hist_pick(const int *hist, int j, int *pick) {
+    const int lane = threadIdx.x;
+    int c[4], sum = 0;  // this lane's four bins
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += c[i] = hist[4 * lane + i];
+    int x = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    int before = x - sum;
+    if (lane == 63 && x < j) pick[0] = -1;
+    if (before < j && x >= j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (before < j && before + c[i] >= j) {
+                pick[0] = 4 * lane + i;
+                pick[1] = j - before;
+            }
+            before += c[i];
+        }
+    }
+}
+
+// The same over the workgroup, exactly, by histograms of the keys' upper halves.  (Each wave's share of j, and
+// the least of their answers, took no barriers but bounded rows whose large values lie together, sorted
+// ones say, by far too little: 1333 us for 4096 rows of 32768, K = 64.)  First by distance from the largest key, where
+// 256 bins are two octaves of bf16 and spread the counts; where fewer than j are so near, by the upper
+// byte, then the lower.  Keys of 0 are none; 0 if there are fewer than j.
+template <int TH, int N>
+__device__ __forceinline__ uint32_t head_block_kth(const uint32_t (&key)[N], int j, int *hist, int *pick, int *wave) {
     if constexpr (TH == 64) return head_wave_kth(key, j);
     const int tid = threadIdx.x;
-    uint32_t t = 0;
+    int most = 0;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int i = 0; i < N; ++i) most = max(most, (int)(key[i] >> 16));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) most = max(most, __shfl_xor(most, o));
+    if (tid < 256) hist[tid] = 0;
+    if ((tid & 63) == 0) wave[tid >> 6] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < TH / 64; ++w) most = max(most, wave[w]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int d = most - (int)(key[i] >> 16);
+        if (key[i] != 0 && d < 256) atomicAdd(&hist[d], 1);
+    }
+    __syncthreads();
+    if (tid < 64) head_hist_pick(hist, j, pick);
+    __syncthreads();
+    if (pick[0] >= 0) return (uint32_t)(most - pick[0]) << 16;
+    uint32_t t = 0;
+#pragma unroll 1
+    for (int shift = 24; shift >= 16; shift -= 8) {
+        __syncthreads();
         if (tid < 256) hist[tid] = 0;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (key[i] != 0 && (half == 0 || key[i] >> 24 == t >> 24)) atomicAdd(&hist[key[i] >> (half ? 16 : 24) & 255], 1);
+            if (key[i] != 0 && (shift == 24 || key[i] >> 24 == t >> 24)) atomicAdd(&hist[255 - (key[i] >> shift & 255)], 1);
         __syncthreads();
-        if (tid < 64) {
-            int c[4], sum = 0;  // this lane's four bins, and the keys above them
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * tid - i];
-            int x = sum;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int y = __shfl_up(x, o);
-                if (tid >= o) x += y;
-            }
-            const int total = __shfl(x, 63);
-            int above = x - sum;
-            if (tid == 0 && total < j) pick[0] = -1;
-            if (above < j && x >= j) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (above < j && above + c[i] >= j) {
-                        pick[0] = 255 - 4 * tid - i;
-                        pick[1] = j - above;
-                    }
-                    above += c[i];
-                }
-            }
-        }
+        if (tid < 64) head_hist_pick(hist, j, pick);
         __syncthreads();
-        const int bin = pick[0];
-        if (bin < 0) return 0;  // (the same for all)
+        if (pick[0] < 0) return 0;  // (the same for all)
         j = pick[1];
-        t |= (uint32_t)bin << (half ? 16 : 24);
+        t |= (uint32_t)(255 - pick[0]) << shift;
     }
     return t;
 }
@@ -419,7 +444,7 @@ template <int TH> __device__ __forceinline__ void head_top_prune(HeadTopLds<TH> 
         mine[q] = q * TH + tid < n ? s.buf[q * TH + tid] : 0;
         key[q] = (uint32_t)(mine[q] >> 32);
     }
-    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick);
+    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick, s.wave);
     __syncthreads();
     if (tid == 0) s.n = 0;
     __syncthreads();
@@ -448,7 +473,7 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
     for (int i = 0; i < 4; ++i)  // (a maximum of -inf may stand for nothing, or for NaN: it vouches for neither)
         key[i] = quarter[i] > -__builtin_inff() ? head_key(quarter[i]) : 0u;
     if (tid == 0) s.n = s.blocks = 0;
-    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick);
+    const uint32_t least = head_block_kth<TH>(key, K, s.hist, s.pick, s.wave);
     if constexpr (TH == 64) __syncthreads();
     uint32_t mask = 0;
     for (int g = 0; start + g * rows * TH + tid < end; ++g) mask |= s.top[g * TH + tid] >= least >> 16 ? 1u << g : 0u;
@@ -583,7 +608,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArgs a) {
     extern __shared__ uint64_t cand[];  // splits x K
     __shared__ uint64_t best[kHeadTopMax];
-    __shared__ int hist[256], pick[2], n;
+    __shared__ int hist[256], pick[2], wave[4], n;
     const long long row = blockIdx.x;
     const int tid = threadIdx.x, K = a.K, keys = a.splits * K;
     constexpr int PER = kHeadJoinKeys / 256;
@@ -597,7 +622,7 @@ __global__ __launch_bounds__(256) void qhead_logprobs_join_kernel(HeadLogprobArg
 #pragma unroll
         for (int q = 0; q < PER; ++q) key[q] = (uint32_t)(mine[q] >> 32);
         if (tid == 0) n = 0;
-        const uint32_t least = head_block_kth<256>(key, K, hist, pick);
+        const uint32_t least = head_block_kth<256>(key, K, hist, pick, wave);
         int kept = 0;
 #pragma unroll
         for (int q = 0; q < PER; ++q) kept += mine[q] != 0 && key[q] >= least ? 1 : 0;
