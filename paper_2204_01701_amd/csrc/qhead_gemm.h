@@ -539,17 +539,17 @@ __global__ __launch_bounds__(kThreads) void qhead_dz_kernel(const T *dy, long lo
     const int begin = blockIdx.y * rpp, end = min(m, begin + rpp);
     float s[8] = {};
     if (j < n)
-        for (int i0 = begin + rg; i0 < end; i0 += 32) {
-            float v[4][8], u[4][8];
+        for (int i0 = begin + rg; i0 < end; i0 += 16) {
+            float v[2][8], u[2][8];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {  // (four rows requested together)
+            for (int x = 0; x < 2; ++x) {  // (two rows requested together)
                 const int i = i0 + 8 * x;
                 if (i >= end) continue;
                 head_load8<T>(dy + (size_t)i * ldy + j, v[x], n - j);
                 if (act != HEAD_NONE) head_load8<T>(z + (size_t)i * n + j, u[x], n - j);
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int x = 0; x < 2; ++x) {
                 const int i = i0 + 8 * x;
                 if (i >= end) continue;
                 if (act != HEAD_NONE) head_slopes<8>(act, u[x], v[x]);

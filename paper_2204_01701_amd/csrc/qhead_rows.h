@@ -550,7 +550,7 @@ __device__ __forceinline__ void head_logprobs_finish(const HeadLogprobArgs &a, l
 
 // A workgroup per row, or per part of a row where rows are few: one pass for the sums and the blocks'
 // maxima, then the K largest from the blocks that can hold them.  4096 rows of 32768, bf16: 52 us without
-// alternatives, 68 with one, 77 with 64 (the blocks read again come from the memory-side cache,
+// alternatives, 60 with one, 72 with 64 (the blocks read again come from the memory-side cache,
 // and ranking some 70 keys is most of the rest); keeping candidates chunk by chunk and ranking per
 // chunk took 450, and held one workgroup a CU.
 template <typename T, int TH, int U, bool TOP>
