@@ -653,11 +653,12 @@ template <bool ENT, bool TWO> __device__ __forceinline__ float head_grad_at(cons
     return v;
 }
 
+// `more` is added at element `at` (-1: nowhere) by the thread that holds it.
 template <typename T, int U, bool ENT, bool TWO>
 __device__ __forceinline__ void head_grad_store(const HeadGrad &g, const HeadRow<T> &z, T *dz, const v4u (&r)[U], int first,
-                                                int step, int tid, int end) {
+                                                int step, int tid, int end, int at = -1, float more = 0.0f) {
     constexpr int VEC = Elem<T>::VEC;
-    const int whole = min(end, z.nfull);
+    const int whole = min(end, z.nfull), at_vec = at < 0 ? -1 : at / VEC;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int j = first + u * step + tid;
@@ -666,6 +667,11 @@ __device__ __forceinline__ void head_grad_store(const HeadGrad &g, const HeadRow
         float f[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) f[e] = g.zero ? 0.0f : head_grad_at<ENT, TWO>(g, vget<T>(r[u], e));
+        if (j == at_vec) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e == at % VEC) f[e] += more;
+        }
         T *o = dz + (size_t)j * VEC;
         if (j < whole) {
             *reinterpret_cast<v4u_any *>(o) = vpack<T>(f);
@@ -705,17 +711,14 @@ __global__ __launch_bounds__(TH) void qhead_logprobs_grad_kernel(HeadLogprobGrad
     g.e = -h * a.inv_t;
     g.a = -up * a.inv_t + (ENT ? g.e * a.entropy[row] : 0.0f);
     g.zero = (up == 0.0f && h == 0.0f) || s == 0.0f;
-    const long long lo = (long long)begin * HeadRow<T>::VEC, hi = min((long long)a.V, (long long)end * HeadRow<T>::VEC);
-    const bool mine = tid == 0 && given && t >= lo && t < hi;
-    float zt = 0.0f;
-    if (mine) zt = to_f32<T>(z.p[t]);  // (before the stores: the gradient may lie over the logits)
+    // The gradient may lie over the logits: an element is read and written by one thread only, the target's too.
+    const int at = given && !g.zero ? (int)t : -1;
+    const float more = up * a.inv_t;
     for (int first = begin; first < end; first += U * TH) {
         v4u r[U];
         head_load<T, U>(z, first, TH, tid, end, r);
-        head_grad_store<T, U, ENT, false>(g, z, dz, r, first, TH, tid, end);
+        head_grad_store<T, U, ENT, false>(g, z, dz, r, first, TH, tid, end, at, more);
     }
-    __syncthreads();
-    if (mine && !g.zero) dz[t] = from_f32<T>(head_grad_at<ENT, false>(g, zt) + up * a.inv_t);
 }
 
 // --- distillation ------------------------------------------------------------------------
