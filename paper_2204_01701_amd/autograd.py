@@ -36,7 +36,8 @@ The end of a network: ``linear_act`` is a first-order fully-connected layer with
 activation and residual in one call, ``token_logprobs`` the log probabilities of
 given tokens (class labels) with the entropy and the most likely alternatives,
 ``distill_loss`` the loss against a teacher's top logits, mixed with the label's
-cross entropy.  They take leading dimensions of any kind.
+cross entropy.  They take leading dimensions of any kind.  Their gradients cannot be
+differentiated again: under ``create_graph`` a second derivative through them raises.
 """
 from __future__ import annotations
 
@@ -276,6 +277,26 @@ def _float_column(t, rows):
     return t if t.dtype is torch.float32 else t.float()
 
 
+class _Undifferentiable(torch.autograd.Function):
+    """A gradient as a function of what it was computed from, whose own derivative raises."""
+    @staticmethod
+    def forward(ctx, t, *of):
+        return t.view_as(t)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("a gradient of linear_act, token_logprobs or distill_loss is differentiated: the library has no "
+                           "kernels for these functions' second derivatives, they cannot be differentiated twice")
+
+
+def _once(t, *of):
+    """t, a gradient computed from `of`; where a graph is made of the backward (create_graph), tied to them in it: a
+    tensor without a graph would pass for a constant there."""
+    if t is None or not torch.is_grad_enabled() or not any(v is not None and v.requires_grad for v in of):
+        return t
+    return _Undifferentiable.apply(t, *of)
+
+
 class LinearActFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, b, res, act):
@@ -292,7 +313,7 @@ class LinearActFunction(torch.autograd.Function):
         z = torch.empty_like(y) if act != "none" and any(ctx.needs_input_grad[:3]) else None
         qhead_linear_fwd(xm, wm, b.contiguous().float() if b is not None else None,
                          _matrix(res.to(x.dtype)) if res is not None else None, y, z, act=act)
-        ctx.save_for_backward(xm, wm, z)
+        ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
         ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
         ctx.bdtype = b.dtype if b is not None else None
         ctx.rdtype = res.dtype if res is not None else None
@@ -300,15 +321,17 @@ class LinearActFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, gy):
-        x, w, z = ctx.saved_tensors
+        x, w, z, *leaves = ctx.saved_tensors
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
         dx = torch.empty(x.shape, device=x.device, dtype=x.dtype) if gx else None
         dw = torch.empty(w.shape, device=x.device, dtype=x.dtype) if gw else None
         db = torch.empty(w.shape[0], device=x.device) if gb else None
         if gx or gw or gb:
             qhead_linear_bwd(x, w, _matrix(gy), z, dx, dw, db, act=ctx.act)
-        return (dx.view(ctx.xshape) if gx else None, dw.to(ctx.wdtype) if gw else None,
-                db.to(ctx.bdtype) if gb else None, gy.to(ctx.rdtype) if gr else None, None)
+        of = leaves if ctx.act != "none" else (None, None, None)  # through act'(z)
+        return (_once(dx.view(ctx.xshape), gy, leaves[1], *of) if gx else None,
+                _once(dw.to(ctx.wdtype), gy, leaves[0], *of) if gw else None,
+                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, None)
 
 
 def linear_act(x, weight, bias=None, residual=None, act="none"):
@@ -337,7 +360,7 @@ class TokenLogprobsFunction(torch.autograd.Function):
         qhead_logprobs_fwd(z, t, logp, entropy, None, top_logp, top_ids, stats, temperature)
         if stats is not None:
             ctx.temperature, ctx.shape = temperature, logits.shape
-            ctx.save_for_backward(z, t, stats, entropy)
+            ctx.save_for_backward(z, t, stats, entropy, logits)
         out = (logp, entropy) if len(lead) == 1 else (logp.view(lead), entropy.view(lead))
         if not top:
             return out
@@ -349,13 +372,13 @@ class TokenLogprobsFunction(torch.autograd.Function):
     def backward(ctx, g, h, *_):
         if g is None and h is None:
             return None, None, None, None
-        z, t, stats, entropy = ctx.saved_tensors
-        rows = z.shape[0]
+        z, t, stats, entropy, logits = ctx.saved_tensors
+        rows, of = z.shape[0], (g, h, logits)
         g = _float_column(g, rows) if g is not None else torch.zeros(rows, device=z.device)
         h = _float_column(h, rows) if h is not None else None
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
         qhead_logprobs_bwd(z, t, stats, entropy.view(rows), g, h, dz, ctx.temperature)
-        return dz if dz.shape == ctx.shape else dz.view(ctx.shape), None, None, None
+        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), *of), None, None, None
 
 
 def token_logprobs(logits, target, temperature=1.0, top=0):
@@ -387,16 +410,16 @@ class DistillLossFunction(torch.autograd.Function):
         stats = torch.empty((rows, 4), device=dev) if ctx.needs_input_grad[0] else None
         qhead_distill_fwd(z, t_ids, t_logits, labels, loss, stats, temperature, alpha)
         if stats is not None:
-            ctx.save_for_backward(z, t_ids, t_logits, labels, stats)
+            ctx.save_for_backward(z, t_ids, t_logits, labels, stats, logits)
             ctx.how, ctx.shape = (temperature, alpha), logits.shape
         return loss if len(lead) == 1 else loss.view(lead)
 
     @staticmethod
     def backward(ctx, g):
-        z, ids, tz, labels, stats = ctx.saved_tensors
+        z, ids, tz, labels, stats, logits = ctx.saved_tensors
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
         qhead_distill_bwd(z, ids, tz, labels, stats, _float_column(g, z.shape[0]), dz, *ctx.how)
-        return dz if dz.shape == ctx.shape else dz.view(ctx.shape), None, None, None, None, None
+        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), g, logits), None, None, None, None, None
 
 
 def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1.0, alpha=1.0):
