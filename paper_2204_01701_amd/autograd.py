@@ -299,7 +299,7 @@ def _once(t, *of):
 
 class LinearActFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, b, res, act):
+    def forward(ctx, x, w, b, res, act, train=True):
         _same_device(x, w, b, res)
         if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
             raise ValueError(f"x (..., in) and w (out, in) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
@@ -310,13 +310,14 @@ class LinearActFunction(torch.autograd.Function):
             raise ValueError(f"the residual must have the output's shape {tuple(shape)}, got {tuple(res.shape)}")
         xm, wm = _matrix(x), _matrix(w.to(x.dtype))
         y = torch.empty((xm.shape[0], w.shape[0]), device=x.device, dtype=x.dtype)
-        z = torch.empty_like(y) if act != "none" and any(ctx.needs_input_grad[:3]) else None
+        z = torch.empty_like(y) if train and act != "none" and any(ctx.needs_input_grad[:3]) else None
         qhead_linear_fwd(xm, wm, b.contiguous().float() if b is not None else None,
                          _matrix(res.to(x.dtype)) if res is not None else None, y, z, act=act)
-        ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
-        ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
-        ctx.bdtype = b.dtype if b is not None else None
-        ctx.rdtype = res.dtype if res is not None else None
+        if train:
+            ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
+            ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
+            ctx.bdtype = b.dtype if b is not None else None
+            ctx.rdtype = res.dtype if res is not None else None
         return y.view(shape)
 
     @staticmethod
@@ -331,7 +332,7 @@ class LinearActFunction(torch.autograd.Function):
         of = leaves if ctx.act != "none" else (None, None, None)  # through act'(z)
         return (_once(dx.view(ctx.xshape), gy, leaves[1], *of) if gx else None,
                 _once(dw.to(ctx.wdtype), gy, leaves[0], *of) if gw else None,
-                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, None)
+                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, None, None)
 
 
 def linear_act(x, weight, bias=None, residual=None, act="none"):
@@ -339,13 +340,15 @@ def linear_act(x, weight, bias=None, residual=None, act="none"):
 
     act: "none", "relu", "gelu" (error function), "gelu_tanh" or "silu".  The product, the
     epilogue and the gradients run in the library's kernels in the dtype of x; the
-    pre-activation is kept for the backward in that dtype where there is an activation."""
-    return LinearActFunction.apply(x, weight, bias, residual, act)
+    pre-activation is kept for the backward in that dtype where there is an activation and
+    gradients are on (under no_grad and inference_mode it is not even written)."""
+    # (inside an autograd function gradients are off, and its needs_input_grad does not know of no_grad)
+    return LinearActFunction.apply(x, weight, bias, residual, act, torch.is_grad_enabled())
 
 
 class TokenLogprobsFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, target, temperature, top):
+    def forward(ctx, logits, target, temperature, top, train=True):
         ctx.set_materialize_grads(False)
         lead = logits.shape[:-1]
         if target.shape != lead or target.dtype is not torch.int64:
@@ -354,7 +357,7 @@ class TokenLogprobsFunction(torch.autograd.Function):
         rows, dev = z.shape[0], z.device
         t = _column(target, rows)
         logp, entropy = torch.empty(rows, device=dev), torch.empty(rows, device=dev)
-        stats = torch.empty((rows, 2), device=dev) if ctx.needs_input_grad[0] else None
+        stats = torch.empty((rows, 2), device=dev) if train and ctx.needs_input_grad[0] else None
         top_logp = torch.empty((rows, top), device=dev) if top else None
         top_ids = torch.empty((rows, top), device=dev, dtype=torch.int64) if top else None
         qhead_logprobs_fwd(z, t, logp, entropy, None, top_logp, top_ids, stats, temperature)
@@ -371,14 +374,14 @@ class TokenLogprobsFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g, h, *_):
         if g is None and h is None:
-            return None, None, None, None
+            return None, None, None, None, None
         z, t, stats, entropy, logits = ctx.saved_tensors
         rows, of = z.shape[0], (g, h, logits)
         g = _float_column(g, rows) if g is not None else torch.zeros(rows, device=z.device)
         h = _float_column(h, rows) if h is not None else None
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
         qhead_logprobs_bwd(z, t, stats, entropy.view(rows), g, h, dz, ctx.temperature)
-        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), *of), None, None, None
+        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), *of), None, None, None, None
 
 
 def token_logprobs(logits, target, temperature=1.0, top=0):
@@ -387,12 +390,12 @@ def token_logprobs(logits, target, temperature=1.0, top=0):
     logits (..., vocab); target (...) int64, negative where there is none (log probability 0, no
     gradient from it).  top > 0 adds (top_logp, top_ids) of shape (..., top): the most likely
     tokens, equal logits by rising id (no gradient passes through them)."""
-    return TokenLogprobsFunction.apply(logits, target, temperature, top)
+    return TokenLogprobsFunction.apply(logits, target, temperature, top, torch.is_grad_enabled())
 
 
 class DistillLossFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, t_ids, t_logits, labels, temperature, alpha):
+    def forward(ctx, logits, t_ids, t_logits, labels, temperature, alpha, train=True):
         lead = logits.shape[:-1]
         if (t_ids is not None and t_ids.shape[:-1] != lead) or (t_logits is not None and t_logits.shape[:-1] != lead):
             raise ValueError(f"the teacher's places do not fit logits of shape {tuple(logits.shape)}")
@@ -407,7 +410,7 @@ class DistillLossFunction(torch.autograd.Function):
         if labels is not None:
             labels = _column(labels, rows)
         loss = torch.empty(rows, device=dev)
-        stats = torch.empty((rows, 4), device=dev) if ctx.needs_input_grad[0] else None
+        stats = torch.empty((rows, 4), device=dev) if train and ctx.needs_input_grad[0] else None
         qhead_distill_fwd(z, t_ids, t_logits, labels, loss, stats, temperature, alpha)
         if stats is not None:
             ctx.save_for_backward(z, t_ids, t_logits, labels, stats, logits)
@@ -419,7 +422,7 @@ class DistillLossFunction(torch.autograd.Function):
         z, ids, tz, labels, stats, logits = ctx.saved_tensors
         dz = torch.empty(z.shape, device=z.device, dtype=z.dtype)
         qhead_distill_bwd(z, ids, tz, labels, stats, _float_column(g, z.shape[0]), dz, *ctx.how)
-        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), g, logits), None, None, None, None, None
+        return _once(dz if dz.shape == ctx.shape else dz.view(ctx.shape), g, logits), None, None, None, None, None, None
 
 
 def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1.0, alpha=1.0):
@@ -430,4 +433,4 @@ def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1
     q the softmax of teacher_logits / T over the row's places.  logits (..., vocab); teacher_ids int64
     (negative: an empty place) and teacher_logits (..., K), or both None; labels (...) int64, negative
     where a row has none, or None.  The gradient goes to the logits."""
-    return DistillLossFunction.apply(logits, teacher_ids, teacher_logits, labels, temperature, alpha)
+    return DistillLossFunction.apply(logits, teacher_ids, teacher_logits, labels, temperature, alpha, torch.is_grad_enabled())

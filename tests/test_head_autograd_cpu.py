@@ -97,3 +97,33 @@ def test_first_derivatives_hold_no_graph(calls):
     z = torch.randn(4, 7, requires_grad=True)
     g, = torch.autograd.grad(ag.token_logprobs(z, torch.zeros(4, dtype=torch.int64))[0].sum(), z)
     assert not g.requires_grad
+
+
+@pytest.mark.parametrize("off", [torch.no_grad, torch.inference_mode])
+def test_serving_writes_nothing_for_a_backward(calls, off):
+    """Parameters require gradients, the pass does not: no pre-activation and no statistics are asked for."""
+    z, target = torch.randn(4, 7, requires_grad=True), torch.zeros(4, dtype=torch.int64)
+    with off():
+        y = _linear("gelu")[1]
+        logp = ag.token_logprobs(z, target, top=2)[0]
+        loss = ag.distill_loss(z, None, None, target, alpha=0.0)
+    assert not (y.requires_grad or logp.requires_grad or loss.requires_grad)
+    assert [c["call"] for c in calls] == ["qhead_linear_fwd", "qhead_logprobs_fwd", "qhead_distill_fwd"]
+    assert calls[0]["z"] is None and calls[1]["stats"] is None and calls[2]["stats"] is None
+
+
+def test_training_asks_for_them(calls):
+    z, target = torch.randn(4, 7, requires_grad=True), torch.zeros(4, dtype=torch.int64)
+    _linear("gelu"), ag.token_logprobs(z, target), ag.distill_loss(z, None, None, target, alpha=0.0)
+    assert calls[0]["z"] is not None and calls[1]["stats"] is not None and calls[2]["stats"] is not None
+    _linear("none")
+    assert calls[3]["z"] is None
+
+
+def test_functions_called_with_their_first_arguments_only(calls):
+    x, w = torch.randn(4, 5, requires_grad=True), torch.randn(3, 5, requires_grad=True)
+    z, target = torch.randn(4, 7, requires_grad=True), torch.zeros(4, dtype=torch.int64)
+    ag.LinearActFunction.apply(x, w, None, None, "silu").sum().backward()
+    ag.TokenLogprobsFunction.apply(z, target, 1.0, 0)[0].sum().backward()
+    ag.DistillLossFunction.apply(z, None, None, target, 1.0, 0.5).sum().backward()
+    assert x.grad is not None and w.grad is not None and z.grad is not None
