@@ -86,6 +86,7 @@ typedef struct {
     ql_dtype dtype;
     float temperature;
     float alpha;   /* distillation: share of the teacher's term, 0 .. 1 (ignored by the log probabilities) */
+    int teacher_f32; /* distillation: nonzero where t_logits are float32 though the logits are bf16 */
 } qhead_rows_desc;
 
 #define QHEAD_MAX_TOP 128
@@ -127,7 +128,8 @@ ql_status qhead_logprobs_bwd(const qhead_rows_desc *desc, const void *logits, co
  *              only empty places has no teacher's term.  An id at or above
  *              vocab makes the loss NaN (and takes no part in the gradient).
  *              An id may occur more than once in a row: each place counts.
- *   t_logits : rows x K of `dtype`.  -inf is a place of probability 0.
+ *   t_logits : rows x K of `dtype`, or float32 (teacher_f32; the alternatives of
+ *              qhead_logprobs_fwd are).  -inf is a place of probability 0.
  *   label    : rows int64, or NULL (no label's term).  Negative: a row without
  *              one.  At or above vocab: the loss is NaN, no gradient from it.
  *              The label's term has the weight 1 - alpha also where a row has

@@ -101,7 +101,8 @@ class HeadLinearDesc(ctypes.Structure):
 class HeadRowsDesc(ctypes.Structure):
     """qhead_rows_desc: rows of logits, the places per row, temperature and the teacher's share."""
     _fields_ = [("rows", ctypes.c_int), ("vocab", ctypes.c_int), ("ld", ctypes.c_longlong), ("top", ctypes.c_int),
-                ("dtype", ctypes.c_int), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
+                ("dtype", ctypes.c_int), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float),
+                ("teacher_f32", ctypes.c_int)]
 
 
 def epilogue(scale=None, shift=None, relu=False, stat_sum=None, stat_sumsq=None) -> Epilogue:
@@ -798,18 +799,19 @@ def _head_distill(logits, t_ids, t_logits, labels, temperature, alpha):
     if (t_ids is None) != (t_logits is None):
         raise ValueError("t_ids and t_logits: both or neither")
     top = 0 if t_ids is None else t_ids.shape[-1]
-    i64 = _torch_types()[1]
-    ptrs = _head_dense(i, ("t_ids", t_ids, (rows, top), i64), ("t_logits", t_logits, (rows, top), dt),
+    f32, i64 = _torch_types()
+    t_f32 = t_logits is not None and t_logits.dtype is f32
+    ptrs = _head_dense(i, ("t_ids", t_ids, (rows, top), i64), ("t_logits", t_logits, (rows, top), f32 if t_f32 else dt),
                        ("labels", labels, (rows,), i64))
-    return i, dt, rows, vocab, HeadRowsDesc(rows, vocab, ld, top, code, temperature, alpha), (p, *ptrs)
+    return i, dt, rows, vocab, HeadRowsDesc(rows, vocab, ld, top, code, temperature, alpha, t_f32), (p, *ptrs)
 
 
 def qhead_distill_fwd(logits, t_ids, t_logits, labels, loss, stats=None, temperature=1.0, alpha=1.0, workspace=None,
                       stream=None):
     """loss (rows) = alpha T^2 KL(teacher's top places || softmax(logits / T)) + (1 - alpha) (cross entropy of the label).
 
-    logits (rows, vocab); t_ids int64 (negative: an empty place) and t_logits (rows, K), or both None; labels
-    (rows) int64 (negative: none), or None; loss float32; stats (rows, 4) float32: for qhead_distill_bwd."""
+    logits (rows, vocab); t_ids int64 (negative: an empty place) and t_logits (rows, K; of the logits' dtype or
+    float32), or both None; labels (rows) int64 (negative: none), or None; loss float32; stats (rows, 4) float32: for qhead_distill_bwd."""
     i, _, rows, _, d, ptrs = _head_distill(logits, t_ids, t_logits, labels, temperature, alpha)
     more = _head_dense(i, ("loss", loss, (rows,), _float32()), ("stats", stats, (rows, 4), _float32()))
     _head_call("qhead_distill_fwd", "qhead_distill_workspace_size", d, (*ptrs, *more), i, workspace, stream)

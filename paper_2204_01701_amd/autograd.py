@@ -406,7 +406,9 @@ class DistillLossFunction(torch.autograd.Function):
         if t_ids is not None and t_logits is not None:
             if t_ids.dim() != 2:
                 t_ids, t_logits = (v.reshape(rows, v.shape[-1]) for v in (t_ids, t_logits))
-            t_ids, t_logits = t_ids.contiguous(), t_logits.to(z.dtype).contiguous()
+            if t_logits.dtype is not z.dtype:
+                t_logits = t_logits.float()  # (float32 as it is: only what the caller rounded is rounded)
+            t_ids, t_logits = t_ids.contiguous(), t_logits.contiguous()
         if labels is not None:
             labels = _column(labels, rows)
         loss = torch.empty(rows, device=dev)
@@ -431,6 +433,7 @@ def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1
         alpha T^2 KL(q || softmax(logits / T)) + (1 - alpha) cross_entropy(logits, label),
 
     q the softmax of teacher_logits / T over the row's places.  logits (..., vocab); teacher_ids int64
-    (negative: an empty place) and teacher_logits (..., K), or both None; labels (...) int64, negative
+    (negative: an empty place) and teacher_logits (..., K), or both None: float32 ones, as token_logprobs gives
+    them, are taken in float32 whatever the dtype of the logits; labels (...) int64, negative
     where a row has none, or None.  The gradient goes to the logits."""
     return DistillLossFunction.apply(logits, teacher_ids, teacher_logits, labels, temperature, alpha, torch.is_grad_enabled())

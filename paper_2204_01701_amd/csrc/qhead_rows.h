@@ -729,6 +729,7 @@ struct HeadDistillArgs {
     float c, temp, inv_t, alpha;
     const int64_t *ids;
     const void *tz;
+    bool tz_f32;  // tz are float, whatever T
     const int64_t *label;
     const float *g;
     float *loss, *stats;  // stats: rows x 4, (m, S, S1, 0)
@@ -775,7 +776,7 @@ __device__ __forceinline__ bool head_places_load(const HeadDistillArgs &a, long 
         t[i] = -__builtin_inff();
         if (k < a.K) {
             id[i] = a.ids[row * a.K + k];
-            t[i] = to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + k]);
+            t[i] = a.tz_f32 ? static_cast<const float *>(a.tz)[row * a.K + k] : to_f32<T>(static_cast<const T *>(a.tz)[row * a.K + k]);
         } else if (k == a.K && a.label) {
             id[i] = a.label[row];
         }

@@ -94,7 +94,7 @@ ql_status distill_args(const qhead_rows_desc *d, const void *logits, const int64
     if (!rows_ok(d) || !places_ok(d)) return QL_EINVAL;
     if (d->rows == 0) return QL_OK;
     if (!logits || (d->top && (!t_ids || !t_logits))) return QL_EINVAL;
-    if (!aligned(logits, esize(d->dtype)) || !aligned(t_logits, esize(d->dtype)) || !aligned(t_ids, 8) || !aligned(label, 8))
+    if (!aligned(logits, esize(d->dtype)) || !aligned(t_logits, d->teacher_f32 ? 4 : esize(d->dtype)) || !aligned(t_ids, 8) || !aligned(label, 8))
         return QL_EINVAL;
     const Terms t = distill_terms(d, label);
     a.z = logits;
@@ -107,6 +107,7 @@ ql_status distill_args(const qhead_rows_desc *d, const void *logits, const int64
     a.alpha = d->alpha;
     a.ids = t_ids;
     a.tz = t_logits;
+    a.tz_f32 = d->teacher_f32 != 0;
     a.label = t.label ? label : nullptr;
     return QL_OK;
 }

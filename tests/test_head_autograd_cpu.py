@@ -127,3 +127,14 @@ def test_functions_called_with_their_first_arguments_only(calls):
     ag.TokenLogprobsFunction.apply(z, target, 1.0, 0)[0].sum().backward()
     ag.DistillLossFunction.apply(z, None, None, target, 1.0, 0.5).sum().backward()
     assert x.grad is not None and w.grad is not None and z.grad is not None
+
+
+@pytest.mark.parametrize("student", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("teacher", [torch.bfloat16, torch.float32, torch.float16])
+def test_the_teachers_logits_lose_no_bits(calls, student, teacher):
+    z = torch.randn(4, 7).to(student).requires_grad_(True)
+    tz, ids = torch.randn(4, 3).to(teacher), torch.zeros(4, 3, dtype=torch.int64)
+    ag.distill_loss(z, ids, tz).sum().backward()
+    for c in calls:
+        assert torch.equal(c["t_logits"].double(), tz.double())
+        assert c["t_logits"].dtype in (student, torch.float32)

@@ -1,0 +1,33 @@
+"""What include/qhead.h states of its arguments, held against the entry points without a GPU:
+every call here is refused before anything is launched, or has no rows."""
+import ctypes
+
+import pytest
+
+import paper_2204_01701_amd as ql
+from paper_2204_01701_amd import build as qbuild
+
+OK, EINVAL, EUNSUPPORTED, EWORKSPACE = 0, 1, 2, 3
+P = 0x10000  # stands for a device pointer: refused calls never look behind it
+BF, F = ql.QL_BF16, ql.QL_F32
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def L():
+    if qbuild.is_stale():
+        qbuild.build()
+    return ql.lib()
+
+
+def rows(r=4, v=50, ld=None, top=3, dtype=BF, t=1.0, alpha=0.5, f32=0):
+    return ctypes.byref(ql.HeadRowsDesc(r, v, v if ld is None else ld, top, dtype, t, alpha, f32))
+
+
+def test_a_float32_teacher_is_aligned_to_four_bytes(L):
+    # (a workspace too small ends the calls whose arguments are in order)
+    for f32, dtype, off, want in ((0, BF, 2, EWORKSPACE), (1, BF, 2, EINVAL), (1, BF, 4, EWORKSPACE), (0, F, 2, EINVAL)):
+        d = rows(v=200000, dtype=dtype, f32=f32)
+        assert L.qhead_distill_fwd(d, P, P, P + off, P, P, P, None, 0, None) == want
+        assert L.qhead_distill_step(d, P, P, P + off, P, P, P, P + 64, None, 0, None) == want
+    assert L.qhead_distill_bwd(rows(f32=1), P, P, P + 2, P, P, P, P + 64, None) == EINVAL
