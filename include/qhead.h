@@ -15,6 +15,8 @@
  *    end and the next row's start is neither read nor written.
  *  - Pointers need the alignment of their element only (bf16 2, float 4,
  *    int64 8 bytes); workspaces 16 bytes.
+ *  - A weight gradient is of the operands' dtype unless the caller asks for
+ *    float32 (qlayer.h: always float32).
  *  - Row counts may be 0: the call then launches what zero rows leave to do
  *    (zeros in dw and db) and returns QL_OK.
  *  - Offsets are 64-bit: a matrix may hold more than 2^31 elements.
@@ -46,7 +48,7 @@ extern "C" {
  *
  * Backward, with dy = dl/dy (m x n, ldy), from the stored z:
  *     dz = dy o act'(z),  dx = dz w,  dw = dz^T x,  db = column sums of dz
- *   (dr = dy).  dx : m x k dense, dw : n x k dense of `dtype`; db : n float32.
+ *   (dr = dy).  dx : m x k dense of `dtype`; dw : n x k dense of `dtype`, or float32 (dw_f32); db : n float32.
  *   Each of dx, dw, db may be NULL (not all).  z may be NULL for QL_ACT_NONE;
  *   x is needed for dw, w for dx.  In bf16, dz is rounded once to bf16 as the
  *   operand of both products; db sums it unrounded.  relu'(0) = 0.
@@ -66,6 +68,7 @@ typedef struct {
     ql_dtype dtype;
     ql_act act;
     int unaligned; /* nonzero: one of x, w, dy may not be 16-byte aligned (sizes the workspace for copies) */
+    int dw_f32;    /* backward, nonzero: dw is float32 though the rest is bf16 */
 } qhead_linear_desc;
 
 size_t qhead_linear_fwd_workspace_size(const qhead_linear_desc *desc);

@@ -95,7 +95,7 @@ class HeadLinearDesc(ctypes.Structure):
     """qhead_linear_desc: a first-order fully-connected layer (row strides in elements)."""
     _fields_ = [("m", ctypes.c_int), ("k", ctypes.c_int), ("n", ctypes.c_int), ("ldx", ctypes.c_longlong),
                 ("ldw", ctypes.c_longlong), ("ldr", ctypes.c_longlong), ("ldy", ctypes.c_longlong),
-                ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("unaligned", ctypes.c_int)]
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("unaligned", ctypes.c_int), ("dw_f32", ctypes.c_int)]
 
 
 class HeadRowsDesc(ctypes.Structure):
@@ -733,16 +733,18 @@ def qhead_linear_fwd(x, w, b, res, y, z=None, act="none", workspace=None, stream
 def qhead_linear_bwd(x, w, dy, z=None, dx=None, dw=None, db=None, act="none", workspace=None, stream=None):
     """The gradients of qhead_linear_fwd from dy = dl/dy and the z it stored (z may be None for act "none").
 
-    dx (m, k) and dw (n, k) of the dtype of x, db (n) float32; each may be None."""
+    dx (m, k) of the dtype of x, dw (n, k) of that dtype or float32, db (n) float32; each may be None."""
     i, dt, code = _head_first(x, "x")
     m, k = x.shape
     n = w.shape[0]
     px, ldx = _head_rows("x", x, (m, k), dt, i)
     pw, ldw = _head_rows("w", w, (n, k), dt, i)
     pdy, ldy = _head_rows("dy", dy, (m, n), dt, i)
-    rest = _head_dense(i, ("z", z, (m, n), dt), ("dx", dx, (m, k), dt), ("dw", dw, (n, k), dt), ("db", db, (n,), _float32()))
+    f32 = _float32()
+    dw_f32 = dw is not None and dw.dtype is f32
+    rest = _head_dense(i, ("z", z, (m, n), dt), ("dx", dx, (m, k), dt), ("dw", dw, (n, k), f32 if dw_f32 else dt), ("db", db, (n,), f32))
     _head_call("qhead_linear_bwd", "qhead_linear_bwd_workspace_size",
-               HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, code, _head_act(act), _unaligned(px, pw, pdy)),
+               HeadLinearDesc(m, k, n, ldx, ldw, n, ldy, code, _head_act(act), _unaligned(px, pw, pdy), dw_f32),
                (px, pw, pdy, *rest), i, workspace, stream)
 
 

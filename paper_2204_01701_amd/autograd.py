@@ -325,7 +325,8 @@ class LinearActFunction(torch.autograd.Function):
         x, w, z, *leaves = ctx.saved_tensors
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
         dx = torch.empty(x.shape, device=x.device, dtype=x.dtype) if gx else None
-        dw = torch.empty(w.shape, device=x.device, dtype=x.dtype) if gw else None
+        # (weights kept in float32 get the gradient as it was accumulated)
+        dw = torch.empty(w.shape, device=x.device, dtype=x.dtype if ctx.wdtype is x.dtype else torch.float32) if gw else None
         db = torch.empty(w.shape[0], device=x.device) if gb else None
         if gx or gw or gb:
             qhead_linear_bwd(x, w, _matrix(gy), z, dx, dw, db, act=ctx.act)
@@ -339,7 +340,8 @@ def linear_act(x, weight, bias=None, residual=None, act="none"):
     """act(x weight^T + bias) + residual, with x (..., in), weight (out, in), bias (out), residual (..., out).
 
     act: "none", "relu", "gelu" (error function), "gelu_tanh" or "silu".  The product, the
-    epilogue and the gradients run in the library's kernels in the dtype of x; the
+    epilogue and the gradients run in the library's kernels in the dtype of x (the gradient of a
+    float32 weight leaves them unrounded); the
     pre-activation is kept for the backward in that dtype where there is an activation and
     gradients are on (under no_grad and inference_mode it is not even written)."""
     # (inside an autograd function gradients are off, and its needs_input_grad does not know of no_grad)

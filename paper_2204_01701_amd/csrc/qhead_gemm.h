@@ -104,6 +104,7 @@ struct HeadOut {
     long long ldr;
     void *z;  // dense, I x J
     int act;
+    bool c_f32;  // c is float, whatever T
 };
 
 struct HeadGemmArgs {
@@ -120,7 +121,8 @@ __device__ __forceinline__ void head_store(const HeadOut &o, int J, int i, int j
     float y = acc;
     head_acts<1>(o.act, &y);
     if (o.r) y += to_f32<T>(static_cast<const T *>(o.r)[(size_t)i * o.ldr + j]);
-    static_cast<T *>(o.c)[(size_t)i * o.ldc + j] = from_f32<T>(y);
+    if (o.c_f32) static_cast<float *>(o.c)[(size_t)i * o.ldc + j] = y;
+    else static_cast<T *>(o.c)[(size_t)i * o.ldc + j] = from_f32<T>(y);
 }
 
 // Any sizes and strides, for products too small to gain from copies into whole vectors, and none at all (R = 0):
@@ -299,7 +301,8 @@ __device__ __forceinline__ void head_epilogue8(const HeadOut &o, int J, int i, i
                 if (e < n) v[e] += to_f32<T>(r[e]);
         }
     }
-    head_store8<T>(static_cast<T *>(o.c) + (size_t)i * o.ldc + j, v, n);
+    if (o.c_f32) head_store8<float>(static_cast<float *>(o.c) + (size_t)i * o.ldc + j, v, n);
+    else head_store8<T>(static_cast<T *>(o.c) + (size_t)i * o.ldc + j, v, n);
 }
 
 struct HeadTileArgs {

@@ -246,7 +246,7 @@ ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void
     const size_t need = qhead_linear_fwd_workspace_size(d);
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
-    return run_product<false, false>(fwd_product(d, x, w), HeadOut{y, d->ldy, b, r, d->ldr, z, (int)d->act}, d->dtype,
+    return run_product<false, false>(fwd_product(d, x, w), HeadOut{y, d->ldy, b, r, d->ldr, z, (int)d->act, false}, d->dtype,
                                      static_cast<char *>(workspace), workspace_bytes, static_cast<hipStream_t>(stream));
 }
 
@@ -266,10 +266,10 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
     if (!dx && !dw && !db) return QL_EINVAL;
     if (!sizes_fit(d)) return QL_EUNSUPPORTED;
     if (d->m > 0 && (!dy || (d->act != QL_ACT_NONE && !z) || (dx && !w) || (dw && !x))) return QL_EINVAL;
-    const void *ptrs[] = {x, w, dy, z, dx, dw};
+    const void *ptrs[] = {x, w, dy, z, dx};
     for (const void *p : ptrs)
         if (!aligned(p, esize(d->dtype))) return QL_EINVAL;
-    if (!aligned(db, 4)) return QL_EINVAL;
+    if (!aligned(dw, d->dw_f32 ? 4 : esize(d->dtype)) || !aligned(db, 4)) return QL_EINVAL;
     const size_t need = qhead_linear_bwd_workspace_size(d);
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
@@ -289,12 +289,12 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
     ws += p.dz_bytes + p.part_bytes;
     const size_t left = workspace_bytes - p.dz_bytes - p.part_bytes;
     if (dx) {
-        const ql_status s = run_product<false, true>(dx_product(d, src, w), HeadOut{dx, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE},
+        const ql_status s = run_product<false, true>(dx_product(d, src, w), HeadOut{dx, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE, false},
                                                      d->dtype, ws, left, st);
         if (s != QL_OK) return s;
     }
     if (dw)
-        return run_product<true, true>(dw_product(d, src, x), HeadOut{dw, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE},
+        return run_product<true, true>(dw_product(d, src, x), HeadOut{dw, d->k, nullptr, nullptr, 0, nullptr, QL_ACT_NONE, d->dw_f32 != 0},
                                        d->dtype, ws, left, st);
     return QL_OK;
 }

@@ -138,3 +138,11 @@ def test_the_teachers_logits_lose_no_bits(calls, student, teacher):
     for c in calls:
         assert torch.equal(c["t_logits"].double(), tz.double())
         assert c["t_logits"].dtype in (student, torch.float32)
+
+
+def test_a_float32_weights_gradient_is_asked_for_in_float32(calls):
+    for xt, wt, want in ((torch.bfloat16, torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16, torch.bfloat16),
+                         (torch.float32, torch.bfloat16, torch.float32), (torch.float32, torch.float32, torch.float32)):
+        x, w = torch.randn(4, 5).to(xt), torch.randn(3, 5).to(wt).requires_grad_(True)
+        ag.linear_act(x, w).sum().backward()
+        assert calls[-1]["dw"].dtype is want and w.grad.dtype is wt

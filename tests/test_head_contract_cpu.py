@@ -31,3 +31,11 @@ def test_a_float32_teacher_is_aligned_to_four_bytes(L):
         assert L.qhead_distill_fwd(d, P, P, P + off, P, P, P, None, 0, None) == want
         assert L.qhead_distill_step(d, P, P, P + off, P, P, P, P + 64, None, 0, None) == want
     assert L.qhead_distill_bwd(rows(f32=1), P, P, P + 2, P, P, P, P + 64, None) == EINVAL
+
+
+def test_a_float32_weight_gradient_is_aligned_to_four_bytes(L):
+    def lin(dw_f32):
+        return ctypes.byref(ql.HeadLinearDesc(4, 8, 6, 8, 8, 6, 6, BF, ql.HEAD_ACTS["gelu"], 0, dw_f32))
+
+    for f32, off, want in ((0, 2, EWORKSPACE), (1, 2, EINVAL), (1, 4, EWORKSPACE)):
+        assert L.qhead_linear_bwd(lin(f32), P, P, P, P, P, P + off, P, None, 0, None) == want
