@@ -501,7 +501,7 @@ __device__ __forceinline__ void head_top(HeadTopLds<TH> &s, const HeadRow<T> &z,
 
 struct HeadLogprobArgs {
     const void *z;
-    long long ld;
+    long long ld, row0;     // row0: the launch's first row
     int V, K, splits, per;  // per: vectors of a split
     float c, inv_t;
     const int64_t *target;
@@ -557,8 +557,8 @@ template <typename T, int TH, int U, bool TOP>
 __global__ __launch_bounds__(TH) void qhead_logprobs_kernel(HeadLogprobArgs a) {
     __shared__ HeadSums sums[TH / 64];
     __shared__ HeadTopLds<TOP ? TH : 64> top;
-    const long long row = blockIdx.x / a.splits;
-    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const int in = blockIdx.x / a.splits, sp = blockIdx.x - in * a.splits, tid = threadIdx.x;
+    const long long row = a.row0 + in;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     const int end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
     const HeadTarget g = head_target<T>(a, row);
@@ -685,7 +685,7 @@ __device__ __forceinline__ void head_grad_store(const HeadGrad &g, const HeadRow
 
 struct HeadLogprobGradArgs {
     const void *z;
-    long long ld;
+    long long ld, row0;
     int V, splits, per;
     float c, inv_t;
     const int64_t *target;
@@ -695,8 +695,8 @@ struct HeadLogprobGradArgs {
 
 template <typename T, int TH, int U, bool ENT>
 __global__ __launch_bounds__(TH) void qhead_logprobs_grad_kernel(HeadLogprobGradArgs a) {
-    const long long row = blockIdx.x / a.splits;
-    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const int in = blockIdx.x / a.splits, sp = blockIdx.x - in * a.splits, tid = threadIdx.x;
+    const long long row = a.row0 + in;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     T *dz = static_cast<T *>(a.dz) + row * a.V;
     const int begin = sp * a.per, end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
@@ -724,7 +724,7 @@ __global__ __launch_bounds__(TH) void qhead_logprobs_grad_kernel(HeadLogprobGrad
 // --- distillation ------------------------------------------------------------------------
 struct HeadDistillArgs {
     const void *z;
-    long long ld;
+    long long ld, row0;
     int V, K, splits, per;
     float c, temp, inv_t, alpha;
     const int64_t *ids;
@@ -962,7 +962,7 @@ __device__ __forceinline__ void head_distill_write(const HeadDistillArgs &a, lon
 template <typename T, int TH, int U, bool TWO, bool GRAD, bool HELD>
 __global__ __launch_bounds__(TH, HELD &&U >= 8 ? 4 : 1) void qhead_distill_row_kernel(HeadDistillArgs a) {
     __shared__ HeadDistillLds<TH> s;
-    const long long row = blockIdx.x;
+    const long long row = a.row0 + blockIdx.x;
     const int tid = threadIdx.x;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     HeadSums t = head_start();
@@ -1043,8 +1043,8 @@ __global__ __launch_bounds__(64) void qhead_distill_join_kernel(HeadDistillArgs 
 template <typename T, int TH, int U, bool TWO>
 __global__ __launch_bounds__(TH) void qhead_distill_grad_kernel(HeadDistillArgs a) {
     __shared__ HeadDistillLds<TH> s;
-    const long long row = blockIdx.x / a.splits;
-    const int sp = blockIdx.x - (int)row * a.splits, tid = threadIdx.x;
+    const int in = blockIdx.x / a.splits, sp = blockIdx.x - in * a.splits, tid = threadIdx.x;
+    const long long row = a.row0 + in;
     const HeadRow<T> z(static_cast<const T *>(a.z) + row * a.ld, a.V);
     const int begin = sp * a.per, end = (int)min((long long)z.nvec, (long long)(sp + 1) * a.per);
     T *dz = static_cast<T *>(a.dz) + row * a.V;

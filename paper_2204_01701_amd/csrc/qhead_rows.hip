@@ -52,29 +52,42 @@ Split sums_split(const qhead_rows_desc *d) {
 }
 Split grad_split(const qhead_rows_desc *d) { return split_rows(d->rows, vectors(d), 4 * kNumCUs, 1 << 16, 2 * kRowThreads); }
 
+// launch(args, grid) over all rows, `threads` each: HIP takes fewer than 2^32 threads a launch, so
+// rows beyond half of that go into further ones (rows so many are not split).
+template <typename A, typename F> void over_rows(A a, int rows, int threads, const F &launch) {
+    const int most = (int)((1ll << 31) / threads);
+    for (; a.row0 < rows; a.row0 += most)
+        launch(a, dim3((unsigned)(std::min<long long>(most, rows - a.row0) * a.splits)));
+}
+
+template <typename T, int TH, int U, bool TOP> void launch_logprobs_as(const HeadLogprobArgs &all, int rows, hipStream_t st) {
+    over_rows(all, rows, TH, [&](const HeadLogprobArgs &a, dim3 grid) {
+        hipLaunchKernelGGL((qhead_logprobs_kernel<T, TH, U, TOP>), grid, dim3(TH), 0, st, a);
+    });
+}
 template <typename T> void launch_logprobs(const HeadLogprobArgs &a, int rows, hipStream_t st) {
-    const dim3 grid((unsigned)((long long)rows * a.splits));
     const int nvec = cdiv((long long)a.V, Elem<T>::VEC);
     // One wave where a row is at most one vector a lane, or short and one of many, unless K is large for the bound
     // that its few lanes' maxima give (4000 rows of 700, K = 64, bf16: 64 us, four waves 20).
     const bool one = nvec <= 64, wave = nvec <= 1024 && 4 * a.K <= nvec && many_rows(rows);
     if (a.K) {
-        if (one) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, true>), grid, dim3(64), 0, st, a);
-        else if (wave) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 4, true>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, true>), grid, dim3(kRowThreads), 0, st, a);
+        if (one) launch_logprobs_as<T, 64, 1, true>(a, rows, st);
+        else if (wave) launch_logprobs_as<T, 64, 4, true>(a, rows, st);
+        else launch_logprobs_as<T, kRowThreads, 4, true>(a, rows, st);
     } else {
-        if (one) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 1, false>), grid, dim3(64), 0, st, a);
-        else if (wave) hipLaunchKernelGGL((qhead_logprobs_kernel<T, 64, 4, false>), grid, dim3(64), 0, st, a);
-        else hipLaunchKernelGGL((qhead_logprobs_kernel<T, kRowThreads, 4, false>), grid, dim3(kRowThreads), 0, st, a);
+        if (one) launch_logprobs_as<T, 64, 1, false>(a, rows, st);
+        else if (wave) launch_logprobs_as<T, 64, 4, false>(a, rows, st);
+        else launch_logprobs_as<T, kRowThreads, 4, false>(a, rows, st);
     }
     if (a.splits > 1)
         hipLaunchKernelGGL((qhead_logprobs_join_kernel<T>), dim3(rows), dim3(256), (size_t)a.splits * a.K * 8, st, a);
 }
 
-template <typename T> void launch_logprobs_grad(const HeadLogprobGradArgs &a, int rows, hipStream_t st) {
-    const dim3 grid((unsigned)((long long)rows * a.splits));
-    if (a.h) hipLaunchKernelGGL((qhead_logprobs_grad_kernel<T, kRowThreads, 4, true>), grid, dim3(kRowThreads), 0, st, a);
-    else hipLaunchKernelGGL((qhead_logprobs_grad_kernel<T, kRowThreads, 4, false>), grid, dim3(kRowThreads), 0, st, a);
+template <typename T> void launch_logprobs_grad(const HeadLogprobGradArgs &all, int rows, hipStream_t st) {
+    over_rows(all, rows, kRowThreads, [&](const HeadLogprobGradArgs &a, dim3 grid) {
+        if (a.h) hipLaunchKernelGGL((qhead_logprobs_grad_kernel<T, kRowThreads, 4, true>), grid, dim3(kRowThreads), 0, st, a);
+        else hipLaunchKernelGGL((qhead_logprobs_grad_kernel<T, kRowThreads, 4, false>), grid, dim3(kRowThreads), 0, st, a);
+    });
 }
 
 // Which sums a distillation needs: those at T alone, those at T = 1 alone, or both (`two`).
@@ -113,8 +126,10 @@ ql_status distill_args(const qhead_rows_desc *d, const void *logits, const int64
 }
 
 template <typename T, int TH, int U, bool TWO, bool GRAD, bool HELD>
-void launch_row_as(const HeadDistillArgs &a, int rows, hipStream_t st) {
-    hipLaunchKernelGGL((qhead_distill_row_kernel<T, TH, U, TWO, GRAD, HELD>), dim3(rows), dim3(TH), 0, st, a);
+void launch_row_as(const HeadDistillArgs &all, int rows, hipStream_t st) {
+    over_rows(all, rows, TH, [&](const HeadDistillArgs &a, dim3 grid) {
+        hipLaunchKernelGGL((qhead_distill_row_kernel<T, TH, U, TWO, GRAD, HELD>), grid, dim3(TH), 0, st, a);
+    });
 }
 // The kernel of a workgroup per row by the row's length in vectors.  One wave where a row is short and rows
 // are many (8192 rows of 1000, bf16, step: 24 us against 57 with 256 threads; 4096 of 8000: 45 and 49).  The
@@ -150,9 +165,10 @@ template <typename T, bool TWO> void launch_parts(const HeadDistillArgs &a, int 
     hipLaunchKernelGGL((qhead_distill_part_kernel<T, kRowThreads, 4, TWO>), dim3(rows * a.splits), dim3(kRowThreads), 0, st, a);
     hipLaunchKernelGGL((qhead_distill_join_kernel<T, TWO>), dim3(rows), dim3(64), 0, st, a);
 }
-template <typename T, bool TWO> void launch_distill_grad(const HeadDistillArgs &a, int rows, hipStream_t st) {
-    hipLaunchKernelGGL((qhead_distill_grad_kernel<T, kRowThreads, 4, TWO>), dim3((unsigned)((long long)rows * a.splits)),
-                       dim3(kRowThreads), 0, st, a);
+template <typename T, bool TWO> void launch_distill_grad(const HeadDistillArgs &all, int rows, hipStream_t st) {
+    over_rows(all, rows, kRowThreads, [&](const HeadDistillArgs &a, dim3 grid) {
+        hipLaunchKernelGGL((qhead_distill_grad_kernel<T, kRowThreads, 4, TWO>), grid, dim3(kRowThreads), 0, st, a);
+    });
 }
 
 // FN<T, TWO>(args...) for the descriptor's type
@@ -240,7 +256,7 @@ ql_status qhead_logprobs_bwd(const qhead_rows_desc *d, const void *logits, const
         if (!aligned(p, 4)) return QL_EINVAL;
     if (!aligned(target, 8) || !aligned(logits, esize(d->dtype)) || !aligned(dlogits, esize(d->dtype))) return QL_EINVAL;
     const Split s = grad_split(d);
-    const HeadLogprobGradArgs a{logits, d->ld, d->vocab, s.splits, s.per, kLog2e / d->temperature, 1.0f / d->temperature,
+    const HeadLogprobGradArgs a{logits, d->ld, 0, d->vocab, s.splits, s.per, kLog2e / d->temperature, 1.0f / d->temperature,
                                 target, stats, entropy, g, h, dlogits};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (d->dtype == QL_BF16) launch_logprobs_grad<uint16_t>(a, d->rows, st);
