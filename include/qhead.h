@@ -52,13 +52,12 @@ extern "C" {
  *   Each of dx, dw, db may be NULL (not all).  z may be NULL for QL_ACT_NONE;
  *   x is needed for dw, w for dx.  In bf16, dz is rounded once to bf16 as the
  *   operand of both products; db sums it unrounded.  relu'(0) = 0.
-  Operands whose rows are not whole, aligned 16-byte vectors are copied into the
-  workspace where a product is large enough to gain by it; the query covers the
-  copies that the descriptor shows (odd strides and sizes), and those of
-  misaligned pointers if `unaligned` is set.  With a misaligned pointer and the
-  flag unset results are the same, at lower speed.
- * Sizes: m >= 0, k >= 1, n >= 1; QL_EUNSUPPORTED within 65536 of 2^31, or where a product
- * whose operands cannot be copied has more than 65535 x 64 columns.
+ * Operands whose rows are not whole, aligned 16-byte vectors are copied into the
+ * workspace where a product is large enough to gain by it; the query covers the
+ * copies that the descriptor shows (odd strides and sizes), and those of
+ * misaligned pointers if `unaligned` is set.  With a misaligned pointer and the
+ * flag unset results keep their accuracy, at lower speed.
+ * Sizes: m >= 0, k >= 1, n >= 1; QL_EUNSUPPORTED within 65536 of 2^31.
  * ------------------------------------------------------------------------- */
 typedef enum { QL_ACT_NONE = 0, QL_ACT_RELU = 1, QL_ACT_GELU = 2, QL_ACT_GELU_TANH = 3, QL_ACT_SILU = 4 } ql_act;
 

@@ -112,6 +112,7 @@ struct HeadGemmArgs {
     long long lda, ldb;  // row strides: of i (KM) or t (NAT)
     int I, J, R;
     HeadOut o;
+    int i0, j0;  // a launch's first row and column of C, where C takes more than one (few rows, any layout)
 };
 
 template <typename T>
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void qhead_gemm_any_kernel(HeadGemmArgs g
     constexpr int KT = 64 / (int)sizeof(T), ROW = 80;
     __shared__ __attribute__((aligned(16))) char la[64 * ROW], lb[64 * ROW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int i0 = blockIdx.x * 64, j0 = blockIdx.y * 64;
+    const int i0 = g.i0 + blockIdx.x * 64, j0 = g.j0 + blockIdx.y * 64;
     const T *A = static_cast<const T *>(g.a), *B = static_cast<const T *>(g.b);
     f32x16_t acc = {};
     auto stage = [&](const T *p, long long ld, bool nat, int r0, int rows, int t0, char *l) {
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(512) void qhead_few_kernel(HeadGemmArgs g) {
     constexpr int W = 8, U = 8, STEP = 4 * Elem<T>::VEC;  // t of an MFMA: 32 bf16, 16 fp32
     __shared__ v4f part[W][64];
     const int lane = threadIdx.x & 63, wave = wave_id(), row = lane & 15, off = (lane >> 4) * Elem<T>::VEC;
-    const int j0 = blockIdx.x * 16;
+    const int j0 = g.j0 + blockIdx.x * 16;
     const T *a = static_cast<const T *>(g.a) + (size_t)min(row, g.I - 1) * g.lda;
     const T *b = static_cast<const T *>(g.b) + (size_t)min(j0 + row, g.J - 1) * g.ldb;
     const int ra = row < g.I ? g.R : 0;  // (rows past I are zeros; columns past J are not stored)
@@ -574,11 +575,11 @@ __global__ __launch_bounds__(kThreads) void qhead_dz_kernel(const T *dy, long lo
     part[(size_t)blockIdx.y * n + c] = t;
 }
 
-// db: 32 columns a workgroup, eight threads each.
+// db: 32 columns a workgroup, eight threads each; j0: the launch's first column.
 template <int = 0>
-__global__ __launch_bounds__(kThreads) void qhead_colsum_kernel(const float *part, int parts, int n, float *db) {
+__global__ __launch_bounds__(kThreads) void qhead_colsum_kernel(const float *part, int parts, int n, int j0, float *db) {
     __shared__ float sum[8][32];
-    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, j = j0 + blockIdx.x * 32 + c;
     float s = 0.0f;
     if (j < n)
         for (int p = r; p < parts; p += 8) s += part[(size_t)p * n + j];

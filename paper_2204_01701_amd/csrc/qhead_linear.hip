@@ -24,6 +24,13 @@ bool sizes_fit(const qhead_linear_desc *d) {
     return d->m <= most && d->k <= most && d->n <= most;
 }
 
+// HIP takes fewer than 2^32 threads a launch, and 65535 rows of blocks: launch(first, blocks) over
+// `size` elements, `each` a block, at most `most` blocks a launch.
+template <typename F> void in_launches(int size, int each, long long most, const F &launch) {
+    for (long long first = 0; first < size; first += most * each)
+        launch((int)first, (unsigned)std::min<long long>(most, cdiv(size - first, each)));
+}
+
 // --- one product ------------------------------------------------------------------------
 // An operand as the caller has it: `rows` rows of `cols` elements.  NAT: t is the row index.
 struct Operand {
@@ -50,6 +57,7 @@ struct Product {
 enum Tile { TILE_ANY, TILE_FEW, TILE_64, TILE_128, TILE_256 };
 int tile_rows(Tile t) { return t == TILE_256 ? 256 : 128; }
 int tile_cols(Tile t) { return t == TILE_256 ? 256 : t == TILE_128 ? 128 : 64; }
+int tile_threads(Tile t) { return t == TILE_256 ? 512 : 256; }
 struct ProductPlan {
     Tile tile;
     bool pad_a, pad_b;
@@ -101,7 +109,9 @@ ProductPlan plan_product(const Product &q, ql_dtype t, bool km, bool al_a, bool 
     for (Tile tile : {TILE_64, TILE_128, TILE_256})
         for (int s = 1; s == 1 || (s <= 16 && 4 * s <= steps && s <= cap); ++s) {
             const double c = product_cost(q, t, tile, s);
-            if (c >= best) continue;
+            // (a launch takes fewer than 2^32 threads; 256 x 256 tiles of any output that fits the memory do)
+            const double threads = (double)cdiv(q.I, tile_rows(tile)) * cdiv(q.J, tile_cols(tile)) * s * tile_threads(tile);
+            if (c >= best || threads >= 4294967296.0) continue;
             best = c;
             p.tile = tile;
             want = s;
@@ -139,13 +149,23 @@ template <typename T, bool ANAT, bool BNAT>
 ql_status launch_product(const ProductPlan &p, const HeadTileArgs &a, hipStream_t st) {
     const HeadGemmArgs &g = a.g;
     if (p.tile == TILE_ANY) {
-        const dim3 grid(cdiv(g.I, 64), cdiv(g.J, 64));
-        if (grid.y > 65535) return QL_EUNSUPPORTED;
-        hipLaunchKernelGGL((qhead_gemm_any_kernel<T, ANAT, BNAT>), grid, dim3(kThreads), 0, st, g);
+        in_launches(g.I, 64, (1ll << 31) / kThreads, [&](int i0, unsigned x) {
+            in_launches(g.J, 64, 32768, [&](int j0, unsigned y) {
+                HeadGemmArgs some = g;
+                some.i0 = i0;
+                some.j0 = j0;
+                hipLaunchKernelGGL((qhead_gemm_any_kernel<T, ANAT, BNAT>), dim3(x, y), dim3(kThreads), 0, st, some);
+            });
+        });
         return hip_status();
     }
     if (p.tile == TILE_FEW) {
-        if constexpr (!ANAT && !BNAT) hipLaunchKernelGGL((qhead_few_kernel<T>), dim3(cdiv(g.J, 16)), dim3(512), 0, st, g);
+        if constexpr (!ANAT && !BNAT)
+            in_launches(g.J, 16, (1ll << 31) / 512, [&](int j0, unsigned x) {
+                HeadGemmArgs some = g;
+                some.j0 = j0;
+                hipLaunchKernelGGL((qhead_few_kernel<T>), dim3(x), dim3(512), 0, st, some);
+            });
         return hip_status();
     }
     const dim3 grid((unsigned)(a.ti * a.tj * a.splits));
@@ -174,7 +194,7 @@ ql_status run_product(Product q, const HeadOut &o, ql_dtype t, char *ws, size_t 
     if (s == QL_OK && p.pad_b)
         s = t == QL_BF16 ? pad_operand<uint16_t>(q.b, ws + p.a_bytes, t, st) : pad_operand<float>(q.b, ws + p.a_bytes, t, st);
     if (s != QL_OK) return s;
-    const HeadTileArgs a{HeadGemmArgs{q.a.p, q.b.p, q.a.ld, q.b.ld, q.I, q.J, q.R, o}, p.ti, p.tj, p.splits, p.per,
+    const HeadTileArgs a{HeadGemmArgs{q.a.p, q.b.p, q.a.ld, q.b.ld, q.I, q.J, q.R, o, 0, 0}, p.ti, p.tj, p.splits, p.per,
                          reinterpret_cast<float *>(ws + p.a_bytes + p.b_bytes)};
     return t == QL_BF16 ? launch_product<uint16_t, ANAT, BNAT>(p, a, st) : launch_product<float, ANAT, BNAT>(p, a, st);
 }
@@ -229,7 +249,7 @@ Operand dz_operand(const qhead_linear_desc *d, const DzPlan &p, const void *dy, 
 extern "C" {
 
 size_t qhead_linear_fwd_workspace_size(const qhead_linear_desc *d) {
-    if (!linear_ok(d) || d->m == 0) return 0;
+    if (!linear_ok(d) || !sizes_fit(d) || d->m == 0) return 0;
     return plan_product(fwd_product(d, nullptr, nullptr), d->dtype, true, !d->unaligned, !d->unaligned).bytes();
 }
 
@@ -251,7 +271,7 @@ ql_status qhead_linear_fwd(const qhead_linear_desc *d, const void *x, const void
 }
 
 size_t qhead_linear_bwd_workspace_size(const qhead_linear_desc *d) {
-    if (!linear_ok(d) || d->ldy < d->n) return 0;
+    if (!linear_ok(d) || !sizes_fit(d) || d->ldy < d->n) return 0;
     const bool al = !d->unaligned;
     const DzPlan p = plan_dz(d, al);
     const Operand dz = dz_operand(d, p, nullptr, nullptr);
@@ -281,7 +301,10 @@ ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void
     if (dz || db) {
         if (d->dtype == QL_BF16) launch_dz<uint16_t>(d, p, dy, z, dz, part, st);
         else launch_dz<float>(d, p, dy, z, dz, part, st);
-        if (db && p.parts > 1) hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(cdiv(d->n, 32)), dim3(kThreads), 0, st, part, p.parts, d->n, db);
+        if (db && p.parts > 1)
+            in_launches(d->n, 32, (1ll << 31) / kThreads, [&](int j0, unsigned x) {
+                hipLaunchKernelGGL(qhead_colsum_kernel<>, dim3(x), dim3(kThreads), 0, st, part, p.parts, d->n, j0, db);
+            });
         const ql_status s = hip_status();
         if (s != QL_OK) return s;
     }
