@@ -33,6 +33,9 @@ typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));  // 16
 
 constexpr float kHeadLowest = -3.402823466e+38f;
 constexpr float kHeadFloor = -1e30f;  // stands for -inf in products with a 0 from the same exponent
+// The same for a log probability, whose product with an upstream gradient comes first: below every one whose
+// probability is not 0 in 32 bits (2^-149 over a sum of up to 2^31), and no more, so that h / T may reach 2e36.
+constexpr float kHeadLowLogp = -128.0f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kHeadTopMax = 128;
@@ -647,7 +650,7 @@ struct HeadGrad {
 template <bool ENT, bool TWO> __device__ __forceinline__ float head_grad_at(const HeadGrad &g, float z) {
     const float x = z - g.m, d = x * g.c, p = head_exp2(d) * g.is;
     float v = g.a;
-    if constexpr (ENT) v += g.e * fmaxf(kLn2 * d - g.ls, kHeadFloor);
+    if constexpr (ENT) v += g.e * fmaxf(kLn2 * d - g.ls, kHeadLowLogp);
     v *= p;
     if constexpr (TWO) v += g.b * (head_exp2(x * kLog2e) * g.is1);
     return v;
