@@ -955,7 +955,8 @@ __device__ __forceinline__ void head_place_grads(const HeadDistillArgs &a, const
 
 __device__ __forceinline__ void head_distill_write(const HeadDistillArgs &a, long long row, const HeadSums &t, float loss) {
     a.loss[row] = loss;
-    if (a.stats) *reinterpret_cast<v4f *>(a.stats + 4 * row) = v4f{t.m, t.s, t.s1, 0.0f};
+    typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));  // (the caller's, at any element)
+    if (a.stats) *reinterpret_cast<v4f_any *>(a.stats + 4 * row) = v4f_any{t.m, t.s, t.s1, 0.0f};
 }
 
 // One workgroup per row: the statistics, the loss and, for GRAD, the gradient.  HELD: the row fits the

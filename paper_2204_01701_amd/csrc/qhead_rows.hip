@@ -277,7 +277,7 @@ ql_status qhead_distill_fwd(const qhead_rows_desc *d, const void *logits, const 
     HeadDistillArgs a{};
     const ql_status ok = distill_args(d, logits, t_ids, t_logits, label, a);
     if (ok != QL_OK || d->rows == 0) return ok;
-    if (!loss || !aligned(loss, 4) || (stats && !aligned16(stats))) return QL_EINVAL;
+    if (!loss || !aligned(loss, 4) || !aligned(stats, 4)) return QL_EINVAL;
     const size_t need = qhead_distill_workspace_size(d);
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
@@ -300,7 +300,7 @@ ql_status qhead_distill_bwd(const qhead_rows_desc *d, const void *logits, const 
     const ql_status ok = distill_args(d, logits, t_ids, t_logits, label, a);
     if (ok != QL_OK || d->rows == 0) return ok;
     if (!stats || !g || !dlogits || (dlogits == logits && d->ld != d->vocab)) return QL_EINVAL;
-    if (!aligned16(stats) || !aligned(g, 4) || !aligned(dlogits, esize(d->dtype))) return QL_EINVAL;
+    if (!aligned(stats, 4) || !aligned(g, 4) || !aligned(dlogits, esize(d->dtype))) return QL_EINVAL;
     const Split s = grad_split(d);
     a.splits = s.splits;
     a.per = s.per;

@@ -39,3 +39,10 @@ def test_a_float32_weight_gradient_is_aligned_to_four_bytes(L):
 
     for f32, off, want in ((0, 2, EWORKSPACE), (1, 2, EINVAL), (1, 4, EWORKSPACE)):
         assert L.qhead_linear_bwd(lin(f32), P, P, P, P, P, P + off, P, None, 0, None) == want
+
+
+def test_the_distillations_statistics_are_aligned_to_their_elements(L):
+    # (a workspace too small, or g misaligned, ends the calls whose stats are in order)
+    for off, want in ((4, EWORKSPACE), (8, EWORKSPACE), (2, EINVAL)):
+        assert L.qhead_distill_fwd(rows(v=200000), P, P, P, P, P, P + off, None, 0, None) == want
+    assert L.qhead_distill_bwd(rows(), P, P, P, P, P + 2, P, P + 64, None) == EINVAL
