@@ -16,13 +16,16 @@ constexpr int kRowThreads = 256;
 // Rows enough to fill the GPU with one wave each (eight a CU at least).
 bool many_rows(int rows) { return rows >= 8 * kNumCUs; }
 
+// (log2(e) / T is a factor of every exponent: infinite, it would make the largest logit's 0 a NaN)
 bool rows_ok(const qhead_rows_desc *d) {
     return d && d->rows >= 0 && d->vocab > 0 && d->ld >= d->vocab && (d->dtype == QL_F32 || d->dtype == QL_BF16) &&
-           std::isfinite(d->temperature) && d->temperature > 0.0f;
+           std::isfinite(d->temperature) && d->temperature > 0.0f && std::isfinite(kLog2e / d->temperature);
 }
 bool top_ok(const qhead_rows_desc *d) { return d->top >= 0 && d->top <= QHEAD_MAX_TOP && d->top <= d->vocab; }
+// (T^2 is a factor of the loss)
 bool places_ok(const qhead_rows_desc *d) {
-    return d->top >= 0 && d->top <= QHEAD_MAX_TOP && d->alpha >= 0.0f && d->alpha <= 1.0f;
+    return d->top >= 0 && d->top <= QHEAD_MAX_TOP && d->alpha >= 0.0f && d->alpha <= 1.0f &&
+           std::isfinite(d->temperature * d->temperature);
 }
 size_t esize(ql_dtype t) { return t == QL_BF16 ? 2 : 4; }
 int vec(ql_dtype t) { return t == QL_BF16 ? 8 : 4; }

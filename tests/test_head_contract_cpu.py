@@ -46,3 +46,16 @@ def test_the_distillations_statistics_are_aligned_to_their_elements(L):
     for off, want in ((4, EWORKSPACE), (8, EWORKSPACE), (2, EINVAL)):
         assert L.qhead_distill_fwd(rows(v=200000), P, P, P, P, P, P + off, None, 0, None) == want
     assert L.qhead_distill_bwd(rows(), P, P, P, P, P + 2, P, P + 64, None) == EINVAL
+
+
+@pytest.mark.parametrize("t,scores,distils", [(4.2e-39, False, False), (1e-44, False, False), (4.3e-39, True, True), (1e-30, True, True),
+                                              (1.8e19, True, True), (1.9e19, True, False), (3e38, True, False)])
+def test_temperatures_that_float32_cannot_carry_are_refused(L, t, scores, distils):
+    d, want = rows(v=200000, t=t), {True: EWORKSPACE, False: EINVAL}
+    assert L.qhead_logprobs_fwd(d, P, P, P, P, P, P, P, P, None, 0, None) == want[scores]
+    assert L.qhead_distill_fwd(d, P, P, P, P, P, P, None, 0, None) == want[distils]
+    assert L.qhead_distill_step(d, P, P, P, P, P, P, P + 64, None, 0, None) == want[distils]
+    if not scores:
+        assert L.qhead_logprobs_bwd(d, P, P, P, P, P, P, P + 64, None) == EINVAL
+    if not distils:
+        assert L.qhead_distill_bwd(d, P, P, P, P, P, P, P + 64, None) == EINVAL
