@@ -113,6 +113,8 @@ typedef struct {
  * be NULL), from the stats and entropy of the forward (entropy NULL if h is):
  *     dz_j = 1/T [ g (1[j = t] - p_j) - h p_j (log p_j + entropy) ]
  *   dlogits : rows x vocab dense of `dtype`; may be the logits if ld == vocab.
+ *   A row with a NaN or +inf has a gradient of NaN, unless nothing reaches it:
+ *   with h = 0, and g = 0 or no target, a row's gradient is 0 whatever it holds.
  * ------------------------------------------------------------------------- */
 size_t qhead_logprobs_fwd_workspace_size(const qhead_rows_desc *desc);
 ql_status qhead_logprobs_fwd(const qhead_rows_desc *desc, const void *logits, const int64_t *target, float *logp,
@@ -131,11 +133,13 @@ ql_status qhead_logprobs_bwd(const qhead_rows_desc *desc, const void *logits, co
  *   t_ids    : rows x K int64.  A negative id is an empty place; a row with
  *              only empty places has no teacher's term.  An id at or above
  *              vocab makes the loss NaN (and takes no part in the gradient).
+ *              With alpha = 0 neither ids nor t_logits are looked at.
  *              An id may occur more than once in a row: each place counts.
  *   t_logits : rows x K of `dtype`, or float32 (teacher_f32; the alternatives of
  *              qhead_logprobs_fwd are).  -inf is a place of probability 0.
  *   label    : rows int64, or NULL (no label's term).  Negative: a row without
  *              one.  At or above vocab: the loss is NaN, no gradient from it.
+ *              With alpha = 1 labels are not looked at.
  *              The label's term has the weight 1 - alpha also where a row has
  *              no teacher's places, and the teacher's alpha where it has no label.
  *   loss     : rows float32.
@@ -150,8 +154,10 @@ ql_status qhead_logprobs_bwd(const qhead_rows_desc *desc, const void *logits, co
  * _step: both in one call, for a g that is known beforehand: the logits are
  *        read from memory once.
  * A row whose logits are all -inf has p = 0: loss +inf if it has a teacher's
- * place of positive probability or a label, else 0.  A NaN or +inf among a
- * row's logits makes its loss and its gradient NaN.
+ * place of positive probability or a label, else 0.  A NaN or +inf among the
+ * logits of a row with a term makes its loss NaN, and its gradient unless g = 0;
+ * a row without a term has a loss and a gradient of 0, and one with g = 0 a
+ * gradient of 0, whatever they hold.
  * ------------------------------------------------------------------------- */
 size_t qhead_distill_workspace_size(const qhead_rows_desc *desc);
 ql_status qhead_distill_fwd(const qhead_rows_desc *desc, const void *logits, const int64_t *t_ids, const void *t_logits,
