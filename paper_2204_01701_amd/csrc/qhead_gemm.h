@@ -450,8 +450,8 @@ __global__ __launch_bounds__(kThreads) void qhead_join_kernel(HeadTileArgs a) {
 // C for I <= 16 rows: bound by reading B (the weights) once.  A workgroup takes 16 rows of B (output
 // columns); its eight waves share t, and each keeps eight 16-byte loads a lane in flight, straight into the
 // operand layout of the 16 x 16 MFMA (whose rows are j, columns i), from any alignment.  The waves'
-// partial products meet in LDS, in their order.  1 to 16 rows of 4096 onto 4096, bf16: 11 us a call, 33.6 MB;
-// 16 loads in flight a lane are no faster (the ramp of a launch is half of the time).
+// partial products meet in LDS, in their order.  1 to 16 rows of 4096 onto 4096, bf16: 12 us a call, 33.6 MB
+// (fp32: 24 to 27); 16 loads in flight a lane are no faster (the ramp of a launch is half of the time).
 template <typename T> __device__ __forceinline__ void head_mfma16(const v4u &a, const v4u &b, v4f &acc) {
     if constexpr (sizeof(T) == 2) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
@@ -532,6 +532,9 @@ __global__ __launch_bounds__(kThreads) void qhead_pad_kernel(const T *p, long lo
 
 // The backward's start: dz = dy o act'(z) (rows of ldd, where asked for) and the column sums of the
 // unrounded dz over `rpp` rows as partial sums [part][n], joined below in the order of parts.
+// In bf16 dz is rounded once, to be the operand of both products' bf16 MFMAs, as an activation's gradient
+// is wherever it passes between two bf16 operators; kept in two halves it would double the products.  dx and
+// dw are then off by 0.0023 (norms) where their own rounding to bf16 makes 0.0017.
 // A workgroup takes 256 columns, eight a thread, eight rows at a time.  Bound by memory: 4096 x 8192, bf16,
 // in 46 us (4.4 TB/s).
 template <typename T>
