@@ -152,8 +152,9 @@ def _power(e):
 def _pack(x):
     """The checkpoint of a matrix of finite values: q (rows, cols) int8 and the blocks' e + 127 (rows, blocks) uint8."""
     b = _blocks(x.float())
-    part, power = torch.frexp(b.abs().amax(2))  # amax = part 2^power, part in [1/2, 1)
-    e = torch.where(part > 127 / 128, power - 6, power - 7).clamp_min(-126)
+    top = b.abs().amax(2)
+    part, power = torch.frexp(top)  # top = part 2^power, part in [1/2, 1)
+    e = torch.where(part > 127 / 128, power - 6, power - 7).clamp_min(-126).masked_fill(top == 0, -126)
     q = torch.round(b * _power(-e)[..., None])
     return q.view(x.shape[0], -1)[:, : x.shape[1]].to(torch.int8).contiguous(), (e + 127).to(torch.uint8)
 
