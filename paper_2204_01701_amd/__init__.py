@@ -8,7 +8,7 @@ library; this module only marshals arguments through ctypes: torch tensors
 become device pointers, the current HIP stream becomes the stream argument,
 and workspaces are allocated with torch when the caller passes none.
 
-Function names, argument order and layouts match ``include/qlayer.h`` (and ``qnet.h``, ``qhead.h``):
+Function names, argument order and layouts match ``include/qlayer.h`` (and ``qnet.h``, ``qhead.h``, ``qblock.h``):
 activations NHWC, conv weights OHWI, dense X B x I and W O x I, biases and
 weight/bias gradients float32.  Every function raises ``QLError`` on a
 non-zero status.  There is no fallback: if the library is not built, the
@@ -35,6 +35,8 @@ __all__ = [
     "HEAD_ACTS", "HEAD_MAX_TOP", "HeadLinearDesc", "HeadRowsDesc",
     "qhead_linear_fwd", "qhead_linear_bwd", "qhead_logprobs_fwd", "qhead_logprobs_bwd",
     "qhead_distill_fwd", "qhead_distill_bwd", "qhead_distill_step",
+    "BLOCK_KEEP", "BlockKeepDesc", "BlockNormDesc", "BlockGatedDesc",
+    "qblock_pack8", "qblock_unpack8", "qblock_norm_fwd", "qblock_norm_bwd", "qblock_gated_fwd", "qblock_gated_bwd",
 ]
 
 QL_F32 = 0
@@ -103,6 +105,24 @@ class HeadRowsDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("vocab", ctypes.c_int), ("ld", ctypes.c_longlong), ("top", ctypes.c_int),
                 ("dtype", ctypes.c_int), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float),
                 ("teacher_f32", ctypes.c_int)]
+
+
+class BlockKeepDesc(ctypes.Structure):
+    """qblock_keep_desc: a matrix whose 8-bit checkpoint is written or read."""
+    _fields_ = [("rows", ctypes.c_longlong), ("cols", ctypes.c_int), ("ld", ctypes.c_longlong), ("dtype", ctypes.c_int)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    """qblock_norm_desc: group normalization over n x hw x c."""
+    _fields_ = [("n", ctypes.c_int), ("hw", ctypes.c_int), ("c", ctypes.c_int), ("groups", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class BlockGatedDesc(ctypes.Structure):
+    """qblock_gated_desc: a gated layer (row strides in elements)."""
+    _fields_ = [("m", ctypes.c_int), ("k", ctypes.c_int), ("n", ctypes.c_int), ("ldx", ctypes.c_longlong),
+                ("ldw", ctypes.c_longlong), ("ldh", ctypes.c_longlong), ("dtype", ctypes.c_int), ("act", ctypes.c_int),
+                ("unaligned", ctypes.c_int), ("dw_f32", ctypes.c_int)]
 
 
 def epilogue(scale=None, shift=None, relu=False, stat_sum=None, stat_sumsq=None) -> Epilogue:
@@ -195,6 +215,17 @@ def lib():
         f = getattr(L, f"qhead_{name}_workspace_size")
         f.argtypes = [d]
         f.restype = _sz
+    # the blocks trained with activations in 8 bits (include/qblock.h)
+    bk, bn, bg = ctypes.POINTER(BlockKeepDesc), ctypes.POINTER(BlockNormDesc), ctypes.POINTER(BlockGatedDesc)
+    for name, d, tensors, space in (("pack8", bk, 3, False), ("unpack8", bk, 3, False), ("norm_fwd", bn, 8, True),
+                                    ("norm_bwd", bn, 11, True), ("gated_fwd", bg, 9, True), ("gated_bwd", bg, 12, True)):
+        f = getattr(L, f"qblock_{name}")
+        f.argtypes = [d] + [_vp] * tensors + ([_vp, _sz] if space else []) + [_vp]
+        f.restype = ctypes.c_int
+        if space:
+            f = getattr(L, f"qblock_{name}_workspace_size")
+            f.argtypes = [d]
+            f.restype = _sz
     _lib = L
     return L
 
@@ -834,3 +865,155 @@ def qhead_distill_step(logits, t_ids, t_logits, labels, g, loss, dlogits, temper
     more = _head_dense(i, ("g", g, (rows,), _float32()), ("loss", loss, (rows,), _float32()),
                        ("dlogits", dlogits, (rows, vocab), dt))
     _head_call("qhead_distill_step", "qhead_distill_workspace_size", d, (*ptrs, *more), i, workspace, stream)
+
+
+# --- blocks trained with activations in 8 bits (include/qblock.h) ----------------
+
+BLOCK_KEEP = 32  # QBLOCK_KEEP of qblock.h: neighbours that share a power of two in a checkpoint
+
+
+def _block_call(name, query, desc, ptrs, index, workspace, stream):
+    """_head_call with the tensors' device as the current one."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return _head_call(name, query, desc, ptrs, index, workspace, stream)
+    with torch.cuda.device(index):
+        return _head_call(name, query, desc, ptrs, index, workspace, stream)
+
+
+def _kept_dense(index, q, e, lead, cols):
+    """Pointers of a checkpoint of `lead` rows of `cols` values, both or neither given."""
+    if (q is None) != (e is None):
+        raise ValueError("q and e: both or neither")
+    import torch
+    return _head_dense(index, ("q", q, (*lead, cols), torch.int8), ("e", e, (*lead, -(-cols // BLOCK_KEEP)), torch.uint8))
+
+
+def qblock_pack8(x, q, e, stream=None):
+    """The checkpoint of x (rows, cols) in 8 bits: q (rows, cols) int8 and e (rows, ceil(cols / 32)) uint8.
+
+    Blocks of 32 neighbours of a row share a power of two 2^(e - 127); a value reads back as q 2^(e - 127)."""
+    i, dt, code = _head_first(x, "x")
+    rows, cols = x.shape
+    p, ld = _head_rows("x", x, (rows, cols), dt, i)
+    _block_call("qblock_pack8", None, BlockKeepDesc(rows, cols, ld, code), (p, *_kept_dense(i, q, e, (rows,), cols)), i, None, stream)
+
+
+def qblock_unpack8(q, e, x, stream=None):
+    """x (rows, cols), bfloat16 or float32, from its checkpoint; exact in either type."""
+    i, dt, code = _head_first(x, "x")
+    rows, cols = x.shape
+    p, ld = _head_rows("x", x, (rows, cols), dt, i)
+    _block_call("qblock_unpack8", None, BlockKeepDesc(rows, cols, ld, code), (*_kept_dense(i, q, e, (rows,), cols), p), i, None, stream)
+
+
+def _block_norm(t, what, groups):
+    """(index, dtype, code, n, hw, c) of a dense channels-last map of two dimensions or more."""
+    if t.dim() < 2:
+        raise ValueError(f"{what}: {t.dim()} dimensions, (n, ..., c) is required")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    n, c = t.shape[0], t.shape[-1]
+    i, dt, code = _head_first(t if t.dim() == 2 else t.view(n, -1) if t.numel() else t.new_empty((n, 0)), what)
+    if not isinstance(groups, int) or groups < 1 or c < 1 or c % groups:
+        raise ValueError(f"groups {groups!r}: a whole number that divides the {c} channels is required")
+    hw = 1
+    for size in t.shape[1:-1]:
+        hw *= size
+    if hw < 1:
+        raise ValueError(f"{what}: shape {tuple(t.shape)} has no pixels")
+    return i, dt, code, n, hw, c
+
+
+def qblock_norm_fwd(x, groups, gamma, beta, y, mean=None, rstd=None, q=None, e=None, act="none", eps=1e-5, workspace=None, stream=None):
+    """y = act(gamma (x - mean) rstd + beta), mean and rstd over the pixels and channels of each of `groups` groups of a sample.
+
+    x and y (n, ..., c), channels last (y may be x); gamma and beta (c) float32 or None; mean and rstd (n, groups) float32, for
+    qblock_norm_bwd, or None; q (n, ..., c) int8 and e (n, ..., ceil(c / 32)) uint8, or None: receive x's checkpoint."""
+    i, dt, code, n, hw, c = _block_norm(x, "x", groups)
+    f32 = _float32()
+    ptrs = _head_dense(i, ("x", x, x.shape, dt), ("gamma", gamma, (c,), f32), ("beta", beta, (c,), f32), ("y", y, x.shape, dt),
+                       ("mean", mean, (n, groups), f32), ("rstd", rstd, (n, groups), f32))
+    _block_call("qblock_norm_fwd", "qblock_norm_fwd_workspace_size", BlockNormDesc(n, hw, c, groups, code, _head_act(act), eps),
+                (*ptrs, *_kept_rows(i, q, e, x.shape)), i, workspace, stream)
+
+
+def _kept_rows(index, q, e, shape):
+    """A checkpoint of a map, given in the map's shape or as (pixels, c)."""
+    if q is not None and q.dim() == 2 and len(shape) != 2:
+        pixels = 1
+        for size in shape[:-1]:
+            pixels *= size
+        shape = (pixels, shape[-1])
+    return _kept_dense(index, q, e, tuple(shape[:-1]), shape[-1])
+
+
+def qblock_norm_bwd(dy, x, groups, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, q=None, e=None, act="none",
+                    workspace=None, stream=None):
+    """The gradients of qblock_norm_fwd from dy, the statistics it left, and x or (x None) its checkpoint q, e.
+
+    dx of the shape and dtype of dy (may be dy or x), dgamma and dbeta (c) float32; each may be None."""
+    i, dt, code, n, hw, c = _block_norm(dy, "dy", groups)
+    f32 = _float32()
+    if x is None and q is None:
+        raise ValueError("x or its checkpoint q, e is required")
+    ptrs = _head_dense(i, ("dy", dy, dy.shape, dt), ("x", x, dy.shape, dt))
+    rest = _head_dense(i, ("gamma", gamma, (c,), f32), ("beta", beta, (c,), f32), ("mean", mean, (n, groups), f32),
+                       ("rstd", rstd, (n, groups), f32), ("dx", dx, dy.shape, dt), ("dgamma", dgamma, (c,), f32), ("dbeta", dbeta, (c,), f32))
+    _block_call("qblock_norm_bwd", "qblock_norm_bwd_workspace_size", BlockNormDesc(n, hw, c, groups, code, _head_act(act), 1.0),
+                (*ptrs, *_kept_rows(i, q, e, dy.shape), *rest), i, workspace, stream)
+
+
+def _gated_weights(index, wg, wu, shape, dt):
+    pg, ldg = _head_rows("wg", wg, shape, dt, index)
+    pu, ldu = _head_rows("wu", wu, shape, dt, index)
+    if ldg != ldu:
+        raise ValueError(f"wg and wu: row strides {ldg} and {ldu}, one stride is required")
+    return pg, pu, ldg
+
+
+def qblock_gated_fwd(x, wg, wu, bg, bu, h, z=None, q=None, e=None, act="silu", workspace=None, stream=None):
+    """h = act(x wg^T + bg) * (x wu^T + bu).
+
+    x (m, k), wg and wu (n, k) with one row stride, h (m, n), of one dtype; bg and bu (n) float32 or None; z (2, m, n) of that
+    dtype, or None: receives both factors' inputs x wg^T + bg and x wu^T + bu; q (2, m, n) int8 and e (2, m, ceil(n / 32)) uint8, or
+    None: receive their checkpoint."""
+    i, dt, code = _head_first(x, "x")
+    m, k = x.shape
+    n = wg.shape[0]
+    px, ldx = _head_rows("x", x, (m, k), dt, i)
+    pg, pu, ldw = _gated_weights(i, wg, wu, (n, k), dt)
+    ph, ldh = _head_rows("h", h, (m, n), dt, i)
+    f32 = _float32()
+    pbg, pbu, pz = _head_dense(i, ("bg", bg, (n,), f32), ("bu", bu, (n,), f32), ("z", z, (2, m, n), dt))
+    _block_call("qblock_gated_fwd", "qblock_gated_fwd_workspace_size",
+                BlockGatedDesc(m, k, n, ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), 0),
+                (px, pg, pu, pbg, pbu, ph, pz, *_kept_dense(i, q, e, (2, m), n)), i, workspace, stream)
+
+
+def qblock_gated_bwd(x, wg, wu, dh, z=None, dx=None, dwg=None, dwu=None, dbg=None, dbu=None, q=None, e=None, act="silu",
+                     workspace=None, stream=None):
+    """The gradients of qblock_gated_fwd from dh (m, n), and z or (z None) its checkpoint q, e.
+
+    dx (m, k) of the dtype of dh; dwg and dwu (n, k) of that dtype or float32, both or neither; dbg and dbu (n) float32; each may be
+    None.  x may be None where the weights' gradients are not asked for."""
+    i, dt, code = _head_first(dh, "dh")
+    m, n = dh.shape
+    k = wg.shape[-1]
+    px, ldx = _head_rows("x", x, (m, k), dt, i)
+    pg, pu, ldw = _gated_weights(i, wg, wu, (n, k), dt)
+    pdh, ldh = _head_rows("dh", dh, (m, n), dt, i)
+    if (dwg is None) != (dwu is None):
+        raise ValueError("dwg and dwu: both or neither")
+    if dwg is not None and x is None:
+        raise ValueError("x is required for the weights' gradients")
+    if z is None and q is None and m:
+        raise ValueError("z or its checkpoint q, e is required")
+    f32 = _float32()
+    dw_f32 = dwg is not None and dwg.dtype is f32
+    dw = f32 if dw_f32 else dt
+    pz, = _head_dense(i, ("z", z, (2, m, n), dt))
+    rest = _head_dense(i, ("dx", dx, (m, k), dt), ("dwg", dwg, (n, k), dw), ("dwu", dwu, (n, k), dw), ("dbg", dbg, (n,), f32), ("dbu", dbu, (n,), f32))
+    _block_call("qblock_gated_bwd", "qblock_gated_bwd_workspace_size",
+                BlockGatedDesc(m, k, n, ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), dw_f32),
+                (px, pg, pu, pdh, pz, *_kept_dense(i, q, e, (2, m), n), *rest), i, workspace, stream)

@@ -38,6 +38,14 @@ given tokens (class labels) with the entropy and the most likely alternatives,
 ``distill_loss`` the loss against a teacher's top logits, mixed with the label's
 cross entropy.  They take leading dimensions of any kind.  Their gradients cannot be
 differentiated again: under ``create_graph`` a second derivative through them raises.
+
+A block trained with its activations in 8 bits: ``group_norm_act`` (group normalization
+with an activation) and ``gated_linear`` (two projections, an activation, their product),
+under the same terms.  They, ``linear_act`` and the quadratic layers take
+``checkpoint="int8"``, the third memory mode beside saving and recomputing: what the backward
+reads of the activations (X, T_a and T_b, pre-activations) is kept in 8 bits, blocks of 32
+channels with a power of two each (include/qblock.h), and the gradients are formed from these
+values.  The outputs are those without it, bit for bit.
 """
 from __future__ import annotations
 
@@ -48,10 +56,12 @@ from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL
                qlayer_conv2d_bwd_weight, qlayer_conv2d_fwd, qlayer_conv2d_fwd_ex,
                qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex,
                qhead_distill_bwd, qhead_distill_fwd, qhead_linear_bwd, qhead_linear_fwd, qhead_logprobs_bwd,
-               qhead_logprobs_fwd)
+               qhead_logprobs_fwd, BLOCK_KEEP, qblock_gated_bwd, qblock_gated_fwd, qblock_norm_bwd, qblock_norm_fwd,
+               qblock_pack8, qblock_unpack8)
 
 __all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction", "linear_act", "token_logprobs",
-           "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction"]
+           "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction", "group_norm_act",
+           "gated_linear", "GroupNormActFunction", "GatedLinearFunction"]
 
 
 def _qdtype(t: torch.Tensor) -> int:
@@ -60,6 +70,10 @@ def _qdtype(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return QL_F32
     raise TypeError(f"unsupported dtype {t.dtype}: use bfloat16 or float32")
+
+
+def _tdtype(code: int) -> torch.dtype:
+    return torch.bfloat16 if code == QL_BF16 else torch.float32
 
 
 def _nhwc(t: torch.Tensor) -> torch.Tensor:
@@ -97,6 +111,32 @@ def _cast_grads(gs, dtype):
     return out + [None] * (len(gs) - len(out))
 
 
+def _kept(checkpoint):
+    """Whether activations are kept in 8 bits."""
+    if checkpoint not in (None, "int8"):
+        raise ValueError(f'checkpoint {checkpoint!r}: None or "int8" is required')
+    return checkpoint is not None
+
+
+def _pack(t):
+    """The 8-bit checkpoint (q, e) of a tensor, in blocks of its last dimension (None: none)."""
+    if t is None:
+        return None, None
+    rows = t if t.dim() == 2 else t.view(-1, t.shape[-1])
+    q = torch.empty(rows.shape, device=t.device, dtype=torch.int8)
+    e = torch.empty((rows.shape[0], -(-rows.shape[1] // BLOCK_KEEP)), device=t.device, dtype=torch.uint8)
+    qblock_pack8(rows, q, e)
+    return q, e
+
+
+def _unpack(q, e, dtype, shape=None):
+    if q is None:
+        return None
+    t = torch.empty(q.shape, device=q.device, dtype=dtype)
+    qblock_unpack8(q, e, t)
+    return t if shape is None else t.view(shape)
+
+
 def _terms(ws, nt):
     if any(w is None for w in ws[:nt]):
         raise ValueError(f"the neuron type has {nt} weighted terms")
@@ -106,7 +146,7 @@ def _terms(ws, nt):
 class QuadConv2dFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, wa, wb, wc, ba, bb, bc, stride, pad, recompute, neuron=QL_NEURON_QUADRA, relu=False,
-                groups=1):
+                groups=1, checkpoint=None):
         N, C, H, W = x.shape
         O, C2, KH, KW = wa.shape
         nt = NEURON_TERMS[neuron]
@@ -131,7 +171,11 @@ class QuadConv2dFunction(torch.autograd.Function):
         # output y' (the ReLU mask) included: an in-place change of any of them
         # then fails the version check instead of silently changing the
         # gradients, and no reference cycle through ctx keeps them alive.
-        ctx.save_for_backward(xn, *wn, *bl, ta, tb, y if relu else None)
+        ctx.kept = _kept(checkpoint) and any(ctx.needs_input_grad[:7])
+        if ctx.kept:
+            ctx.save_for_backward(*_pack(xn), *wn, *bl, *_pack(ta), *_pack(tb), y if relu else None)
+        else:
+            ctx.save_for_backward(xn, *wn, *bl, ta, tb, y if relu else None)
         ctx.desc, ctx.recompute, ctx.has_bias, ctx.nt, ctx.neuron = d, recompute, b is not None, nt, neuron
         ctx.wdtype = wa.dtype
         return y.permute(0, 3, 1, 2)
@@ -139,7 +183,13 @@ class QuadConv2dFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, gy):
         d, nt = ctx.desc, ctx.nt
-        xn, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
+        if ctx.kept:
+            xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
+            y_shape = (d.n, d.ho, d.wo, d.o)
+            xn = _unpack(xq, xe, _tdtype(d.dtype), (d.n, d.h, d.w, d.c))
+            ta, tb = _unpack(taq, tae, xn.dtype, y_shape), _unpack(tbq, tbe, xn.dtype, y_shape)
+        else:
+            xn, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
         wn, bl = [wa, wb, wc], [ba, bb, bc]
         if ctx.neuron == QL_NEURON_T2:
             ta = xn  # its input gradient takes X in place of a saved map
@@ -163,7 +213,7 @@ class QuadConv2dFunction(torch.autograd.Function):
             dx = dxn.permute(0, 3, 1, 2) if need_x else None
             dw = [g.permute(0, 3, 1, 2) if g is not None else None for g in _cast_grads(dwn, ctx.wdtype)]
             db = db or [None, None, None]
-            return (dx, *dw, *db, None, None, None, None, None, None)
+            return (dx, *dw, *db, *[None] * 7)
         if need_x:
             dxn = torch.empty_like(xn)
             if ctx.neuron == QL_NEURON_T24:  # (the chain rule through X o X needs X)
@@ -181,12 +231,12 @@ class QuadConv2dFunction(torch.autograd.Function):
             dw = [g.permute(0, 3, 1, 2) if g is not None else None for g in _cast_grads(dwn, ctx.wdtype)]
         dw = dw or [None, None, None]
         db = db or [None, None, None]
-        return (dx, *dw, *db, None, None, None, None, None, None)
+        return (dx, *dw, *db, *[None] * 7)
 
 
 class QuadLinearFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, wa, wb, wc, ba, bb, bc, recompute, neuron=QL_NEURON_QUADRA, relu=False):
+    def forward(ctx, x, wa, wb, wc, ba, bb, bc, recompute, neuron=QL_NEURON_QUADRA, relu=False, checkpoint=None):
         if x.dim() != 2 or wa.dim() != 2:
             raise ValueError("x must be (B, I) and the weights (O, I)")
         B, I = x.shape
@@ -209,7 +259,11 @@ class QuadLinearFunction(torch.autograd.Function):
             qlayer_linear_fwd_ex(d, xc, *wl, *bl, y, ta, tb, epi=epilogue(relu=True))
         else:
             qlayer_linear_fwd(d, xc, *wl, *bl, y, ta, tb)
-        ctx.save_for_backward(xc, *wl, *bl, ta, tb, y if relu else None)
+        ctx.kept = _kept(checkpoint) and any(ctx.needs_input_grad[:7])
+        if ctx.kept:
+            ctx.save_for_backward(*_pack(xc), *wl, *bl, *_pack(ta), *_pack(tb), y if relu else None)
+        else:
+            ctx.save_for_backward(xc, *wl, *bl, ta, tb, y if relu else None)
         ctx.desc, ctx.recompute, ctx.has_bias, ctx.nt, ctx.neuron = d, recompute, b is not None, nt, neuron
         ctx.wdtype = wa.dtype
         return y
@@ -217,7 +271,12 @@ class QuadLinearFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, gy):
         d, nt = ctx.desc, ctx.nt
-        xc, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
+        if ctx.kept:
+            xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
+            xc = _unpack(xq, xe, _tdtype(d.dtype))
+            ta, tb = _unpack(taq, tae, xc.dtype), _unpack(tbq, tbe, xc.dtype)
+        else:
+            xc, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
         wl, bl = [wa, wb, wc], [ba, bb, bc]
         if ctx.neuron == QL_NEURON_T2:
             pass  # the dense backward takes X itself
@@ -229,7 +288,7 @@ class QuadLinearFunction(torch.autograd.Function):
         need_x, need_w = ctx.needs_input_grad[0], any(ctx.needs_input_grad[1:4])
         need_b = ctx.has_bias and any(ctx.needs_input_grad[4:7])
         if not (need_x or need_w or need_b):
-            return (None,) * 10
+            return (None,) * 11
         dx = torch.empty_like(xc) if need_x else None
         dw = [torch.empty(wl[0].shape, device=xc.device, dtype=torch.float32) if i < nt else None
               for i in range(3)] if (need_w or need_b) else None
@@ -241,19 +300,25 @@ class QuadLinearFunction(torch.autograd.Function):
             qlayer_linear_bwd(d, xc, gyc, ta, tb, *wl, dx, *(dw or [None] * 3), *(db or [None] * 3))
         dw = _cast_grads(dw, ctx.wdtype) if dw is not None else [None, None, None]
         db = db or [None, None, None]
-        return (dx, *dw, *db, None, None, None)
+        return (dx, *dw, *db, *[None] * 4)
 
 
 def quad_conv2d(x, wa, wb=None, wc=None, ba=None, bb=None, bc=None, stride=1, pad=0, recompute=False,
-                neuron=QL_NEURON_QUADRA, relu=False, groups=1):
-    """Quadratic 2-D convolution layer (NCHW-shaped tensors, channels_last memory)."""
-    return QuadConv2dFunction.apply(x, wa, wb, wc, ba, bb, bc, stride, pad, recompute, neuron, relu, groups)
+                neuron=QL_NEURON_QUADRA, relu=False, groups=1, checkpoint=None):
+    """Quadratic 2-D convolution layer (NCHW-shaped tensors, channels_last memory).
+
+    checkpoint="int8" keeps X and, unless recompute, T_a and T_b in 8 bits for the backward."""
+    _kept(checkpoint)
+    return QuadConv2dFunction.apply(x, wa, wb, wc, ba, bb, bc, stride, pad, recompute, neuron, relu, groups,
+                                    checkpoint if torch.is_grad_enabled() else None)
 
 
 def quad_linear(x, wa, wb=None, wc=None, ba=None, bb=None, bc=None, recompute=False, neuron=QL_NEURON_QUADRA,
-                relu=False):
-    """Quadratic fully-connected layer: x (B, I), weights (O, I)."""
-    return QuadLinearFunction.apply(x, wa, wb, wc, ba, bb, bc, recompute, neuron, relu)
+                relu=False, checkpoint=None):
+    """Quadratic fully-connected layer: x (B, I), weights (O, I); checkpoint as in quad_conv2d."""
+    _kept(checkpoint)
+    return QuadLinearFunction.apply(x, wa, wb, wc, ba, bb, bc, recompute, neuron, relu,
+                                    checkpoint if torch.is_grad_enabled() else None)
 
 
 # --- the end of a network -----------------------------------------------------------
@@ -285,8 +350,9 @@ class _Undifferentiable(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, _):
-        raise RuntimeError("a gradient of linear_act, token_logprobs or distill_loss is differentiated: the library has no "
-                           "kernels for these functions' second derivatives, they cannot be differentiated twice")
+        raise RuntimeError("a gradient of linear_act, token_logprobs, distill_loss, group_norm_act or gated_linear is "
+                           "differentiated: the library has no kernels for these functions' second derivatives, they cannot "
+                           "be differentiated twice")
 
 
 def _once(t, *of):
@@ -297,9 +363,15 @@ def _once(t, *of):
     return _Undifferentiable.apply(t, *of)
 
 
+def _tie(x):
+    """For _once where x itself is not kept: an empty tensor that stands in x's place in the graph, in a tuple (so that no
+    function takes it for an input)."""
+    return (x[..., :0].clone() if x.requires_grad and torch.is_grad_enabled() else None,)
+
+
 class LinearActFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, b, res, act, train=True):
+    def forward(ctx, x, w, b, res, act, train=True, checkpoint=None, tie=None):
         _same_device(x, w, b, res)
         if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
             raise ValueError(f"x (..., in) and w (out, in) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
@@ -314,16 +386,27 @@ class LinearActFunction(torch.autograd.Function):
         qhead_linear_fwd(xm, wm, b.contiguous().float() if b is not None else None,
                          _matrix(res.to(x.dtype)) if res is not None else None, y, z, act=act)
         if train:
-            ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
-            ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
+            ctx.kept = _kept(checkpoint)
+            if ctx.kept:
+                # (of x only what the weight's gradient reads)
+                ctx.save_for_backward(*_pack(xm if ctx.needs_input_grad[1] else None), wm, *_pack(z), tie[0], w, b)
+            else:
+                ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
+            ctx.act, ctx.xshape, ctx.wdtype, ctx.xdtype = act, x.shape, w.dtype, x.dtype
             ctx.bdtype = b.dtype if b is not None else None
             ctx.rdtype = res.dtype if res is not None else None
         return y.view(shape)
 
     @staticmethod
     def backward(ctx, gy):
-        x, w, z, *leaves = ctx.saved_tensors
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
+        if ctx.kept:
+            xq, xe, w, zq, ze, *leaves = ctx.saved_tensors
+            x, z = _unpack(xq, xe, ctx.xdtype), _unpack(zq, ze, ctx.xdtype)
+            if x is None:  # (the gradients asked for do not read it)
+                x = torch.empty((ctx.xshape[:-1].numel(), w.shape[1]), device=w.device, dtype=ctx.xdtype)
+        else:
+            x, w, z, *leaves = ctx.saved_tensors
         dx = torch.empty(x.shape, device=x.device, dtype=x.dtype) if gx else None
         # (weights kept in float32 get the gradient as it was accumulated)
         dw = torch.empty(w.shape, device=x.device, dtype=x.dtype if ctx.wdtype is x.dtype else torch.float32) if gw else None
@@ -333,19 +416,21 @@ class LinearActFunction(torch.autograd.Function):
         of = leaves if ctx.act != "none" else (None, None, None)  # through act'(z)
         return (_once(dx.view(ctx.xshape), gy, leaves[1], *of) if gx else None,
                 _once(dw.to(ctx.wdtype), gy, leaves[0], *of) if gw else None,
-                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, None, None)
+                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 4)
 
 
-def linear_act(x, weight, bias=None, residual=None, act="none"):
+def linear_act(x, weight, bias=None, residual=None, act="none", checkpoint=None):
     """act(x weight^T + bias) + residual, with x (..., in), weight (out, in), bias (out), residual (..., out).
 
     act: "none", "relu", "gelu" (error function), "gelu_tanh" or "silu".  The product, the
     epilogue and the gradients run in the library's kernels in the dtype of x (the gradient of a
     float32 weight leaves them unrounded); the
     pre-activation is kept for the backward in that dtype where there is an activation and
-    gradients are on (under no_grad and inference_mode it is not even written)."""
+    gradients are on (under no_grad and inference_mode it is not even written).  checkpoint="int8": x and the
+    pre-activation are kept in 8 bits."""
+    kept = _kept(checkpoint)
     # (inside an autograd function gradients are off, and its needs_input_grad does not know of no_grad)
-    return LinearActFunction.apply(x, weight, bias, residual, act, torch.is_grad_enabled())
+    return LinearActFunction.apply(x, weight, bias, residual, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)
 
 
 class TokenLogprobsFunction(torch.autograd.Function):
@@ -439,3 +524,126 @@ def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1
     them, are taken in float32 whatever the dtype of the logits; labels (...) int64, negative
     where a row has none, or None.  The gradient goes to the logits."""
     return DistillLossFunction.apply(logits, teacher_ids, teacher_logits, labels, temperature, alpha, torch.is_grad_enabled())
+
+
+# --- blocks trained with activations in 8 bits ----------------------------------------
+
+class GroupNormActFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, eps, act, train=True, checkpoint=None, tie=None):
+        _same_device(x, weight, bias)
+        if x.dim() not in (2, 4):
+            raise ValueError(f"x (N, C, H, W) or (N, C) is required, got {tuple(x.shape)}")
+        c = x.shape[1]
+        for name, t in (("weight", weight), ("bias", bias)):
+            if t is not None and t.shape != (c,):
+                raise ValueError(f"the {name} must have {c} elements")
+        xn = _nhwc(x) if x.dim() == 4 else x.contiguous()
+        gamma, beta = (t.contiguous().float() if t is not None else None for t in (weight, bias))
+        y = torch.empty(xn.shape, device=x.device, dtype=x.dtype)
+        train = train and any(ctx.needs_input_grad[:3])
+        kept = train and _kept(checkpoint)
+        stats = torch.empty((2, x.shape[0], max(groups, 1)), device=x.device) if train else (None, None)
+        q = e = None
+        if kept:
+            q = torch.empty(xn.shape, device=x.device, dtype=torch.int8)
+            e = torch.empty(xn.shape[:-1] + (-(-c // BLOCK_KEEP),), device=x.device, dtype=torch.uint8)
+        qblock_norm_fwd(xn, groups, gamma, beta, y, stats[0], stats[1], q, e, act, eps)
+        if train:
+            ctx.save_for_backward(None if kept else xn, q, e, gamma, beta, stats, tie[0] if kept else x, weight, bias)
+            ctx.groups, ctx.act, ctx.image = groups, act, x.dim() == 4
+        return y.permute(0, 3, 1, 2) if x.dim() == 4 else y
+
+    @staticmethod
+    def backward(ctx, gy):
+        x, q, e, gamma, beta, stats, *leaves = ctx.saved_tensors
+        gx, gw, gb = ctx.needs_input_grad[:3]
+        dtype = x.dtype if x is not None else gy.dtype
+        dy = gy.to(dtype)
+        dy = _nhwc(dy) if ctx.image else dy.contiguous()
+        c = dy.shape[-1]
+        dx = torch.empty(dy.shape, device=dy.device, dtype=dtype) if gx else None
+        dgamma = torch.empty(c, device=dy.device) if gw else None
+        dbeta = torch.empty(c, device=dy.device) if gb else None
+        if gx or gw or gb:
+            qblock_norm_bwd(dy, x, ctx.groups, gamma, beta, stats[0], stats[1], dx, dgamma, dbeta, q, e, ctx.act)
+        if dx is not None and ctx.image:
+            dx = dx.permute(0, 3, 1, 2)
+        of = (gy, *leaves)
+        return (_once(dx, *of), _once(dgamma.to(leaves[1].dtype), *of) if gw else None,
+                _once(dbeta.to(leaves[2].dtype), *of) if gb else None, *[None] * 6)
+
+
+def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", checkpoint=None):
+    """act(weight (x - mean) / sqrt(var + eps) + bias), mean and variance over the pixels and channels of each group.
+
+    x (N, C, H, W), used in channels_last memory, or (N, C); weight and bias (C) or None; act as in linear_act.
+    The backward reads x, or with checkpoint="int8" what 8 bits of it say."""
+    kept = _kept(checkpoint)
+    return GroupNormActFunction.apply(x, weight, bias, groups, eps, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)
+
+
+class GatedLinearFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, wg, wu, bg, bu, act, train=True, checkpoint=None, tie=None):
+        _same_device(x, wg, wu, bg, bu)
+        if wg.dim() != 2 or x.dim() < 1 or x.shape[-1] != wg.shape[1] or wu.shape != wg.shape:
+            raise ValueError(f"x (..., in) and two weights (out, in) are required, got {tuple(x.shape)}, {tuple(wg.shape)} and "
+                             f"{tuple(wu.shape)}")
+        for b in (bg, bu):
+            if b is not None and b.shape != wg.shape[:1]:
+                raise ValueError(f"each bias must have {wg.shape[0]} elements")
+        xm, wgm, wum = _matrix(x), _matrix(wg.to(x.dtype)), _matrix(wu.to(x.dtype))
+        if wgm.stride() != wum.stride():
+            wgm, wum = wgm.contiguous(), wum.contiguous()
+        m, n = xm.shape[0], wg.shape[0]
+        h = torch.empty((m, n), device=x.device, dtype=x.dtype)
+        train = train and any(ctx.needs_input_grad[:5])
+        kept = train and _kept(checkpoint)
+        z = torch.empty((2, m, n), device=x.device, dtype=x.dtype) if train and not kept else None
+        q = e = None
+        if kept:
+            q = torch.empty((2, m, n), device=x.device, dtype=torch.int8)
+            e = torch.empty((2, m, -(-n // BLOCK_KEEP)), device=x.device, dtype=torch.uint8)
+        qblock_gated_fwd(xm, wgm, wum, bg.contiguous().float() if bg is not None else None,
+                         bu.contiguous().float() if bu is not None else None, h, z, q, e, act)
+        if train:
+            # (of x only what the weights' gradients read)
+            xs = xm if any(ctx.needs_input_grad[1:3]) else None
+            xq, xe = _pack(xs) if kept else (None, None)
+            ctx.save_for_backward(None if kept else xs, xq, xe, wgm, wum, z, q, e, tie[0] if kept else x, wg, wu, bg, bu)
+            ctx.act, ctx.xshape = act, x.shape
+        return h.view(x.shape[:-1] + (n,))
+
+    @staticmethod
+    def backward(ctx, gh):
+        x, xq, xe, wg, wu, z, q, e, *leaves = ctx.saved_tensors
+        gx, gwg, gwu, gbg, gbu = ctx.needs_input_grad[:5]
+        dtype, dev, gw = wg.dtype, wg.device, gwg or gwu
+        dh = _matrix(gh.to(dtype))
+        if xq is not None and gw:
+            x = _unpack(xq, xe, dtype)
+        n, k = wg.shape
+        wdtype = leaves[1].dtype if leaves[1].dtype == leaves[2].dtype == dtype else torch.float32
+        dx = torch.empty((dh.shape[0], k), device=dev, dtype=dtype) if gx else None
+        # (weights kept in float32 get the gradient as it was accumulated)
+        dwg, dwu = (torch.empty((n, k), device=dev, dtype=wdtype) if gw else None for _ in range(2))
+        dbg, dbu = (torch.empty(n, device=dev) if g else None for g in (gbg, gbu))
+        if gx or gw or gbg or gbu:
+            qblock_gated_bwd(x if gw else None, wg, wu, dh, z, dx, dwg, dwu, dbg, dbu, q, e, ctx.act)
+        of = (gh, *leaves)
+
+        def done(t, leaf, wanted):
+            return _once(t.to(leaf.dtype), *of) if wanted else None
+
+        return (_once(dx.view(ctx.xshape), *of) if gx else None, done(dwg, leaves[1], gwg), done(dwu, leaves[2], gwu),
+                done(dbg, leaves[3], gbg), done(dbu, leaves[4], gbu), *[None] * 4)
+
+
+def gated_linear(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", checkpoint=None):
+    """act(x w_gate^T + b_gate) * (x w_up^T + b_up), with x (..., in), weights (out, in), biases (out).
+
+    Both projections, the activation (as in linear_act) and the product run in one kernel in the dtype of x.  The projections
+    are kept for the backward in that dtype, or, and x with them, in 8 bits under checkpoint="int8"."""
+    kept = _kept(checkpoint)
+    return GatedLinearFunction.apply(x, w_gate, w_up, b_gate, b_up, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)

@@ -1,0 +1,231 @@
+// qblock_norm.hip -- host side of the group normalization of include/qblock.h.
+#include <cmath>
+
+#include "qblock_host.h"
+#include "qblock_norm.h"
+
+using namespace ql;
+using namespace ql::host;
+
+namespace {
+
+bool norm_ok(const qblock_norm_desc *d) {
+    return d && d->n >= 0 && d->hw > 0 && d->c > 0 && d->groups > 0 && d->c % d->groups == 0 && float_type(d->dtype) && known_act(d->act);
+}
+bool sizes_fit(const qblock_norm_desc *d) { return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20; }
+
+int log2_up(long long v) {
+    int b = 0;
+    while ((1LL << b) < v) ++b;
+    return b;
+}
+
+struct NormPlan {
+    bool fused;
+    int th, r, u;  // threads, pixels a thread, channels a thread takes as one
+    NormArgs a;    // the geometry
+    size_t part_bytes, chan_bytes;
+    size_t bytes() const { return part_bytes + chan_bytes; }
+};
+
+// The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most.
+void share_samples(NormPlan &p, int n, long long most) {
+    const int snl = log2_up(p.th) - p.a.svl - p.a.pnl;
+    const long long groups = ((long long)n + (1LL << snl) - 1) >> snl;
+    p.a.slots = (int)std::max(1LL, std::min(groups, most));
+    p.a.blocks = (int)((long long)p.a.slots * p.a.chunks * p.a.segs);
+}
+
+// bwd: the backward's plan (its registers hold dy as well, its workgroups share few lines of a.chan).
+// emit: the segments begin at blocks of the checkpoint.
+NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
+    NormPlan p{};
+    NormArgs &a = p.a;
+    const int cpg = d->c / d->groups, es = (int)esize(d->dtype);
+    a.n = d->n, a.hw = d->hw, a.c = d->c, a.groups = d->groups, a.cpg = cpg;
+    a.act = (int)d->act, a.eps = d->eps;
+    p.u = cpg % 8 == 0 ? 8 : 1;
+    a.parts = 1, a.part_c = cpg;
+    // whole groups whose channels are a multiple of a checkpoint's block
+    int unit = 1;
+    if (emit)
+        while (unit < kKeep && (long long)unit * cpg % kKeep) unit *= 2;
+    const int least = std::min(d->groups, unit);
+    auto segment = [&](int gps) {
+        a.gps = std::min(d->groups, (gps + unit - 1) / unit * unit);
+        a.segs = cdiv(d->groups, a.gps);
+        a.svl = log2_up(((long long)a.gps * cpg + 7) / 8);
+        if (emit) a.svl = std::max(a.svl, 2);
+    };
+    // Registers: segments of whole lines (128 bytes; 64 where that does not fit).
+    const int most_r = bwd ? 8 : 16;
+    if (cpg <= 8 * 512 && env_override("QBLOCK_NORM_FUSED", 1))
+        for (int line : {128, 64}) {
+            segment(std::max(least, cdiv(line, cpg * es)));
+            for (int th : {256, 512}) {
+                const int lth = log2_up(th);
+                if (a.svl > lth) continue;
+                const long long need = (d->hw + (1LL << (lth - a.svl)) - 1) >> (lth - a.svl);
+                const int fits = th == 256 ? 8 : most_r;
+                if (need > fits) continue;
+                p.fused = true;
+                p.th = th;
+                a.pnl = lth - a.svl;
+                p.r = need <= 2 ? 2 : need <= 8 ? 8 : 16;
+                // several samples a workgroup, as long as their lanes have room and all CUs work
+                while (a.pnl > 0 && ((long long)p.r << (a.pnl - 1)) >= d->hw) --a.pnl;
+                a.chunks = 1;
+                a.chunk_px = d->hw;
+                share_samples(p, d->n, bwd ? std::max(1, cdiv(4 * kNumCUs, a.segs)) : (1 << 20) / a.segs + 1);
+                if (bwd) p.chan_bytes = align_up((size_t)a.slots * d->c * sizeof(float2));
+                return p;
+            }
+        }
+    // Chunks: segments of up to 512 channels, or a part of a group of up to 2048.
+    p.th = kThreads;
+    p.r = 8;
+    if (cpg > 2048) {
+        a.gps = 1;
+        a.part_c = 2048;
+        a.parts = cdiv(cpg, 2048);
+        a.segs = d->groups * a.parts;
+        a.svl = 8;
+    } else {
+        segment(std::max(least, 512 / cpg));
+        if ((long long)a.gps * cpg > 2048) {  // (the checkpoint is written by itself then)
+            unit = 1;
+            segment(std::max(1, 2048 / cpg));
+        }
+    }
+    a.pnl = 8 - a.svl;
+    const int batch = p.r << a.pnl;
+    const long long batches = cdiv(d->hw, batch), want = std::max(1LL, 8LL * kNumCUs / std::max(1LL, (long long)std::max(1, d->n) * a.segs));
+    // (at most 16 batches: a thread's sums stay short)
+    const long long per = std::min(16LL, std::max((batches + 63) / 64, (batches + want - 1) / want));
+    a.chunk_px = (int)std::min<long long>(d->hw, per * batch);
+    a.chunks = cdiv(d->hw, a.chunk_px);
+    share_samples(p, d->n, bwd ? std::max(1LL, 8LL * kNumCUs / ((long long)a.segs * a.chunks)) : (1LL << 22) / ((long long)a.segs * a.chunks) + 1);
+    p.part_bytes = align_up((size_t)std::max(1, d->n) * a.chunks * a.parts * d->groups * sizeof(float2));
+    if (bwd) p.chan_bytes = align_up((size_t)a.slots * a.chunks * d->c * sizeof(float2));
+    return p;
+}
+
+// Whether the forward's launches can write the checkpoint on the way.
+bool emits(const NormPlan &p) { return p.a.parts == 1 && (p.a.segs == 1 || p.a.gps * p.a.cpg % kKeep == 0) && p.a.svl >= 2; }
+
+template <typename T, int U> ql_status launch_fwd(const NormPlan &p, const NormArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)a.blocks), wg((unsigned)p.th);
+    if (p.fused) {
+        if (p.th == 256 && p.r == 2) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 2, U, true, 256>), grid, wg, 0, st, a);
+        else if (p.th == 256) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, true, 256>), grid, wg, 0, st, a);
+        else if (p.r <= 8) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, true, 512>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 16, U, true, 512>), grid, wg, 0, st, a);
+    } else {
+        hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, false, kThreads>), grid, wg, 0, st, a);
+        hipLaunchKernelGGL((qblock_norm_apply_kernel<T, U>), grid, wg, 0, st, a);
+    }
+    return hip_status();
+}
+
+template <typename T, int U, bool KEPT> ql_status launch_bwd(const NormPlan &p, const NormArgs &a, float *dgamma, float *dbeta, hipStream_t st) {
+    const dim3 grid((unsigned)a.blocks), wg((unsigned)p.th);
+    if (p.fused) {
+        if (p.th == 256 && p.r == 2) hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 2, U, true, KEPT, 256>), grid, wg, 0, st, a);
+        else if (p.th == 256) hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 256>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 512>), grid, wg, 0, st, a);
+    } else {
+        hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 4, U, false, KEPT, kThreads>), grid, wg, 0, st, a);
+        if (a.out) hipLaunchKernelGGL((qblock_norm_dx_kernel<T, U, KEPT>), grid, wg, 0, st, a);
+    }
+    if (a.chan)
+        hipLaunchKernelGGL(qblock_norm_param_kernel<>, dim3(cdiv(a.c, 32)), dim3(1024), 0, st, a.chan, a.slots * a.chunks, a.c, dgamma, dbeta);
+    return hip_status();
+}
+
+template <int = 0> __global__ __launch_bounds__(kThreads) void qblock_zero_kernel(float *p, float *q, int n) {
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) {
+        if (p) p[i] = 0.0f;
+        if (q) q[i] = 0.0f;
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t qblock_norm_fwd_workspace_size(const qblock_norm_desc *d) {
+    if (!norm_ok(d) || !sizes_fit(d) || d->n == 0) return 0;
+    // (with a checkpoint the segments may be others)
+    return std::max(plan_norm(d, false, false).bytes(), plan_norm(d, false, true).bytes());
+}
+
+ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float *gamma, const float *beta, void *y, float *mean,
+                          float *rstd, int8_t *q, uint8_t *e, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!norm_ok(d) || !(d->eps > 0.0f) || !std::isfinite(d->eps)) return QL_EINVAL;
+    if (!sizes_fit(d)) return QL_EUNSUPPORTED;
+    if (d->n == 0) return QL_OK;
+    if (!x || !y || !q != !e) return QL_EINVAL;
+    if (!aligned(x, esize(d->dtype)) || !aligned(y, esize(d->dtype))) return QL_EINVAL;
+    const void *floats[] = {gamma, beta, mean, rstd};
+    for (const void *p : floats)
+        if (!aligned(p, 4)) return QL_EINVAL;
+    const size_t need = qblock_norm_fwd_workspace_size(d);
+    if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
+    if (workspace && !aligned16(workspace)) return QL_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const NormPlan p = plan_norm(d, false, q != nullptr);
+    NormArgs a = p.a;
+    a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.mean = mean, a.rstd = rstd;
+    a.part = static_cast<float2 *>(workspace);
+    if (q && emits(p)) {
+        a.q = q, a.e = e;
+    } else if (q) {  // (first: y may be x)
+        const ql_status s = run_keep(true, d->dtype, const_cast<void *>(x), d->c, q, e, (long long)d->n * d->hw, d->c, st);
+        if (s != QL_OK) return s;
+    }
+    if (d->dtype == QL_BF16) return p.u == 8 ? launch_fwd<uint16_t, 8>(p, a, st) : launch_fwd<uint16_t, 1>(p, a, st);
+    return p.u == 8 ? launch_fwd<float, 8>(p, a, st) : launch_fwd<float, 1>(p, a, st);
+}
+
+size_t qblock_norm_bwd_workspace_size(const qblock_norm_desc *d) {
+    if (!norm_ok(d) || !sizes_fit(d) || d->n == 0) return 0;
+    return plan_norm(d, true, false).bytes();
+}
+
+ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void *x, const int8_t *q, const uint8_t *e, const float *gamma,
+                          const float *beta, const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    if (!norm_ok(d)) return QL_EINVAL;
+    if (!dx && !dgamma && !dbeta) return QL_EINVAL;
+    if (!sizes_fit(d)) return QL_EUNSUPPORTED;
+    const size_t es = esize(d->dtype);
+    if (d->n > 0 && (!dy || (!x && (!q || !e)) || !mean || !rstd)) return QL_EINVAL;
+    if (!aligned(dy, es) || !aligned(x, es) || !aligned(dx, es)) return QL_EINVAL;
+    const void *floats[] = {gamma, beta, mean, rstd, dgamma, dbeta};
+    for (const void *p : floats)
+        if (!aligned(p, 4)) return QL_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (d->n == 0) {
+        if (dgamma || dbeta)
+            hipLaunchKernelGGL(qblock_zero_kernel<>, dim3(grid_1d(d->c)), dim3(kThreads), 0, st, dgamma, dbeta, d->c);
+        return hip_status();
+    }
+    const size_t need = qblock_norm_bwd_workspace_size(d);
+    if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
+    if (workspace && !aligned16(workspace)) return QL_EINVAL;
+    const NormPlan p = plan_norm(d, true, false);
+    NormArgs a = p.a;
+    a.x = x, a.dy = dy, a.out = dx, a.gamma = gamma, a.beta = beta;
+    a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
+    a.part = static_cast<float2 *>(workspace);
+    if (dgamma || dbeta) a.chan = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.part_bytes);
+    const bool kept = x == nullptr;
+    if (kept) a.q = const_cast<int8_t *>(q), a.e = const_cast<uint8_t *>(e);
+#define QL_NORM_BWD(T)                                                                                                            \
+    (p.u == 8 ? (kept ? launch_bwd<T, 8, true>(p, a, dgamma, dbeta, st) : launch_bwd<T, 8, false>(p, a, dgamma, dbeta, st)) \
+              : (kept ? launch_bwd<T, 1, true>(p, a, dgamma, dbeta, st) : launch_bwd<T, 1, false>(p, a, dgamma, dbeta, st)))
+    return d->dtype == QL_BF16 ? QL_NORM_BWD(uint16_t) : QL_NORM_BWD(float);
+#undef QL_NORM_BWD
+}
+
+}  // extern "C"
