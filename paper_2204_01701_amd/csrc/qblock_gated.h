@@ -8,6 +8,7 @@
 //   GATED_DW   C = [dg du]^T x: the rows of both weights' gradients, tiles of either in one launch.
 #pragma once
 
+#include "qblock_act.h"
 #include "qblock_keep.h"
 
 namespace ql {
@@ -62,7 +63,7 @@ __device__ __forceinline__ void gated_put(const GatedOut &o, int I, int J, int i
         keep(u, (size_t)I + i);
     }
     if (n <= 0) return;
-    head_acts<8>(o.act, g);
+    block_acts<8>(o.act, g);
 #pragma unroll
     for (int k = 0; k < 8; ++k) g[k] *= u[k];
     head_store8<T>(static_cast<T *>(o.h) + (size_t)i * o.ldh + j, g, n);
@@ -332,7 +333,7 @@ template <typename T> __global__ __launch_bounds__(512) void qblock_gated_few_ke
         z[0] = from_f32<T>(v[0]);
         z[(size_t)g.I * g.J] = from_f32<T>(v[1]);
     }
-    head_acts<1>(g.o.act, v);
+    block_acts<1>(g.o.act, v);
     static_cast<T *>(g.o.h)[(size_t)i * g.o.ldh + j] = from_f32<T>(v[0] * v[1]);
 }
 
@@ -387,8 +388,8 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(kThreads) void qbl
                     dg[k] = d[x][k] * u[x][k];
                     act[k] = g[x][k];
                 }
-                head_slopes<8>(a.act, g[x], dg);
-                head_acts<8>(a.act, act);
+                block_slopes<8>(a.act, g[x], dg);
+                block_acts<8>(a.act, act);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     act[k] *= d[x][k];

@@ -24,8 +24,8 @@ struct NormPlan {
     bool fused;
     int th, r, u;  // threads, pixels a thread, channels a thread takes as one
     NormArgs a;    // the geometry
-    size_t part_bytes, chan_bytes;
-    size_t bytes() const { return part_bytes + chan_bytes; }
+    size_t part_bytes, joined_bytes, chan_bytes;
+    size_t bytes() const { return part_bytes + joined_bytes + chan_bytes; }
 };
 
 // The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most.
@@ -34,6 +34,9 @@ void share_samples(NormPlan &p, int n, long long most) {
     const long long groups = ((long long)n + (1LL << snl) - 1) >> snl;
     p.a.slots = (int)std::max(1LL, std::min(groups, most));
     p.a.blocks = (int)((long long)p.a.slots * p.a.chunks * p.a.segs);
+    p.a.by_segs = make_fastdiv(p.a.segs);
+    p.a.by_chunks = make_fastdiv(p.a.chunks);
+    p.a.by_wide = make_fastdiv(p.a.cpg);
 }
 
 // bwd: the backward's plan (its registers hold dy as well, its workgroups share few lines of a.chan).
@@ -57,33 +60,53 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
         a.svl = log2_up(((long long)a.gps * cpg + 7) / 8);
         if (emit) a.svl = std::max(a.svl, 2);
     };
-    // Registers: segments of whole lines (128 bytes; 64 where that does not fit).
-    const int most_r = bwd ? 8 : 16;
-    if (cpg <= 8 * 512 && env_override("QBLOCK_NORM_FUSED", 1))
-        for (int line : {128, 64}) {
+    // Registers.  Time of a candidate in us: a launch, then the values of a workgroup at `each` ns (fitted on 12 maps from
+    // 1 x 1024 x 512 to 128 x 1024 x 256 and 8192 rows of 1024; segments of a line of 128, 64 or 32 bytes, of which the XCD's L2
+    // joins neighbours), in rounds over the CUs; that of chunks with their further launches likewise.
+    const double values = (double)std::max(1, d->n) * d->hw * d->c, each = 1e-3 * (bwd ? (p.u == 8 ? 0.45 : 1.2) : (p.u == 8 ? 0.35 : 0.7));
+    double best = (bwd ? 13.0 : 10.0) + 1.3 * each * values / kNumCUs;
+    const int forced = env_override("QBLOCK_NORM_FUSED", -1), forced_line = env_override("QBLOCK_NORM_LINE", 0);
+    if (forced == 1) best = 1e300;
+    const int most_r = !bwd && d->dtype == QL_F32 ? 16 : 8;
+    int line_at = 0, th_at = 0;
+    if (cpg <= 8 * 512 && forced != 0)
+        for (int line : {128, 64, 32}) {
+            if (forced_line && line != forced_line) continue;
             segment(std::max(least, cdiv(line, cpg * es)));
             for (int th : {256, 512}) {
                 const int lth = log2_up(th);
                 if (a.svl > lth) continue;
                 const long long need = (d->hw + (1LL << (lth - a.svl)) - 1) >> (lth - a.svl);
-                const int fits = th == 256 ? 8 : most_r;
-                if (need > fits) continue;
-                p.fused = true;
-                p.th = th;
-                a.pnl = lth - a.svl;
-                p.r = need <= 2 ? 2 : need <= 8 ? 8 : 16;
-                // several samples a workgroup, as long as their lanes have room and all CUs work
-                while (a.pnl > 0 && ((long long)p.r << (a.pnl - 1)) >= d->hw) --a.pnl;
-                a.chunks = 1;
-                a.chunk_px = d->hw;
-                share_samples(p, d->n, bwd ? std::max(1, cdiv(4 * kNumCUs, a.segs)) : (1 << 20) / a.segs + 1);
-                if (bwd) p.chan_bytes = align_up((size_t)a.slots * d->c * sizeof(float2));
-                return p;
+                if (need > (th == 256 ? 8 : most_r) || (need > 8 && line < 64)) continue;
+                const double wgs = std::max(1.0, (double)std::max(1, d->n) * a.segs), rounds = wgs / kNumCUs;
+                // (a float's line of 32 bytes is a single column: 168 us where 128 bytes take 125; two workgroups of 256 threads
+                // on a CU load and compute in turn, where their registers leave one of 512: 76 us, 85)
+                const double form = es == 4 && line == 32 ? 1.5 : bwd && es == 2 && th == 512 && p.u == 8 ? 1.12 : 1.0;
+                const double t = 5.0 + form * each * values / wgs * (rounds < 4 ? std::ceil(rounds) : rounds);
+                if (t < 0.97 * best) best = t, line_at = line, th_at = th;
+                break;
             }
         }
+    if (line_at) {
+        segment(std::max(least, cdiv(line_at, cpg * es)));
+        const int lth = log2_up(th_at);
+        const long long need = (d->hw + (1LL << (lth - a.svl)) - 1) >> (lth - a.svl);
+        a.pnl = lth - a.svl;
+        p.r = need <= 2 ? 2 : need <= 8 ? 8 : 16;
+        // several samples a workgroup, as long as their lanes have room
+        while (a.pnl > 0 && ((long long)p.r << (a.pnl - 1)) >= d->hw) --a.pnl;
+        if ((double)(1 << (lth - a.svl - a.pnl)) * d->hw * d->c * es < 2147483648.0) {  // (a thread's offset)
+            p.fused = true;
+            p.th = th_at;
+            a.chunks = 1;
+            a.chunk_px = d->hw;
+            share_samples(p, d->n, bwd ? std::max(1, cdiv(4 * kNumCUs, a.segs)) : (1 << 20) / a.segs + 1);
+            if (bwd) p.chan_bytes = align_up((size_t)a.slots * d->c * sizeof(float2));
+            return p;
+        }
+    }
     // Chunks: segments of up to 512 channels, or a part of a group of up to 2048.
     p.th = kThreads;
-    p.r = 8;
     if (cpg > 2048) {
         a.gps = 1;
         a.part_c = 2048;
@@ -98,16 +121,24 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
         }
     }
     a.pnl = 8 - a.svl;
-    const int batch = p.r << a.pnl;
-    const long long batches = cdiv(d->hw, batch), want = std::max(1LL, 8LL * kNumCUs / std::max(1LL, (long long)std::max(1, d->n) * a.segs));
-    // (at most 16 batches: a thread's sums stay short)
-    const long long per = std::min(16LL, std::max((batches + 63) / 64, (batches + want - 1) / want));
-    a.chunk_px = (int)std::min<long long>(d->hw, per * batch);
+    // steps of the workgroup's pixel lanes: at most 128 a chunk (a thread's sums stay short), else what gives every CU four workgroups
+    const long long steps = (d->hw + (1LL << a.pnl) - 1) >> a.pnl, all = steps * std::max(1, d->n) * a.segs;
+    // (two where the map is small or the groups' channels are told apart: 24 us for 2 x 50176 x 64 in 32 groups, 31 with four)
+    const int wgs = env_override("QBLOCK_NORM_WGS", p.u == 8 && values >= 8e6 ? 4 * kNumCUs : 2 * kNumCUs);
+    const long long per = std::max(1LL, std::min(128LL, (all + wgs - 1) / wgs));
+    p.r = per <= 2 ? 2 : 8;
+    a.chunk_px = (int)std::min<long long>(d->hw, per << a.pnl);
     a.chunks = cdiv(d->hw, a.chunk_px);
     share_samples(p, d->n, bwd ? std::max(1LL, 8LL * kNumCUs / ((long long)a.segs * a.chunks)) : (1LL << 22) / ((long long)a.segs * a.chunks) + 1);
     p.part_bytes = align_up((size_t)std::max(1, d->n) * a.chunks * a.parts * d->groups * sizeof(float2));
+    p.joined_bytes = align_up((size_t)std::max(1, d->n) * d->groups * sizeof(float2));  // (mean and rstd, or the two averages)
     if (bwd) p.chan_bytes = align_up((size_t)a.slots * a.chunks * d->c * sizeof(float2));
     return p;
+}
+
+template <bool STATS> void launch_join(const NormArgs &a, hipStream_t st) {
+    const int slices = a.chunks * a.parts, lanes = std::min(64, 1 << log2_up(slices));
+    hipLaunchKernelGGL((qblock_norm_join_kernel<STATS>), dim3(grid_1d((long long)a.n * a.groups * lanes)), dim3(kThreads), 0, st, a);
 }
 
 // Whether the forward's launches can write the checkpoint on the way.
@@ -121,7 +152,9 @@ template <typename T, int U> ql_status launch_fwd(const NormPlan &p, const NormA
         else if (p.r <= 8) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, true, 512>), grid, wg, 0, st, a);
         else hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 16, U, true, 512>), grid, wg, 0, st, a);
     } else {
-        hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, false, kThreads>), grid, wg, 0, st, a);
+        if (p.r == 2) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 2, U, false, kThreads>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, false, kThreads>), grid, wg, 0, st, a);
+        launch_join<true>(a, st);
         hipLaunchKernelGGL((qblock_norm_apply_kernel<T, U>), grid, wg, 0, st, a);
     }
     return hip_status();
@@ -134,11 +167,14 @@ template <typename T, int U, bool KEPT> ql_status launch_bwd(const NormPlan &p, 
         else if (p.th == 256) hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 256>), grid, wg, 0, st, a);
         else hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 512>), grid, wg, 0, st, a);
     } else {
-        hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 4, U, false, KEPT, kThreads>), grid, wg, 0, st, a);
-        if (a.out) hipLaunchKernelGGL((qblock_norm_dx_kernel<T, U, KEPT>), grid, wg, 0, st, a);
+        hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 2, U, false, KEPT, kThreads>), grid, wg, 0, st, a);
+        if (a.out) {
+            launch_join<false>(a, st);
+            hipLaunchKernelGGL((qblock_norm_dx_kernel<T, U, KEPT>), grid, wg, 0, st, a);
+        }
     }
     if (a.chan)
-        hipLaunchKernelGGL(qblock_norm_param_kernel<>, dim3(cdiv(a.c, 32)), dim3(1024), 0, st, a.chan, a.slots * a.chunks, a.c, dgamma, dbeta);
+        hipLaunchKernelGGL(qblock_norm_param_kernel<>, dim3(cdiv(a.c, 16)), dim3(1024), 0, st, a.chan, a.slots * a.chunks, a.c, dgamma, dbeta);
     return hip_status();
 }
 
@@ -177,6 +213,9 @@ ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float 
     NormArgs a = p.a;
     a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.mean = mean, a.rstd = rstd;
     a.part = static_cast<float2 *>(workspace);
+    float *stats = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_bytes);
+    if (!p.fused && !a.mean) a.mean = stats;
+    if (!p.fused && !a.rstd) a.rstd = stats + (size_t)d->n * d->groups;
     if (q && emits(p)) {
         a.q = q, a.e = e;
     } else if (q) {  // (first: y may be x)
@@ -218,7 +257,8 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void 
     a.x = x, a.dy = dy, a.out = dx, a.gamma = gamma, a.beta = beta;
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.part = static_cast<float2 *>(workspace);
-    if (dgamma || dbeta) a.chan = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.part_bytes);
+    a.avg = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.part_bytes);
+    if (dgamma || dbeta) a.chan = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.part_bytes + p.joined_bytes);
     const bool kept = x == nullptr;
     if (kept) a.q = const_cast<int8_t *>(q), a.e = const_cast<uint8_t *>(e);
 #define QL_NORM_BWD(T)                                                                                                            \
