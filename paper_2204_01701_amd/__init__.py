@@ -881,6 +881,28 @@ def _block_call(name, query, desc, ptrs, index, workspace, stream):
         return _head_call(name, query, desc, ptrs, index, workspace, stream)
 
 
+def _block_launch(name, desc, ptrs, device, query=None):
+    """The entry point on the pointers of operands that the caller has checked, on the current stream of their device.
+
+    The autograd functions' way in: half of a small layer's time is the host's, and their backward runs on a thread of its
+    own, on which each step costs twice as much.  (The workspace is the stream's, which orders its reuse.)"""
+    import torch
+    index = device.index
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return _block_launch(name, desc, ptrs, device, query)
+    L = lib()
+    ref = ctypes.byref(desc)
+    if query is None:
+        status = getattr(L, name)(ref, *ptrs, _current_stream(index))
+    else:
+        need = getattr(L, query)(ref)
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        status = getattr(L, name)(ref, *ptrs, None if ws is None else ws.data_ptr(), need, _current_stream(index))
+    if status != 0:
+        raise QLError(name, status)
+
+
 def _kept_dense(index, q, e, lead, cols):
     """Pointers of a checkpoint of `lead` rows of `cols` values, both or neither given."""
     if (q is None) != (e is None):

@@ -45,7 +45,9 @@ under the same terms.  They, ``linear_act`` and the quadratic layers take
 ``checkpoint="int8"``, the third memory mode beside saving and recomputing: what the backward
 reads of the activations (X, T_a and T_b, pre-activations) is kept in 8 bits, blocks of 32
 channels with a power of two each (include/qblock.h), and the gradients are formed from these
-values.  The outputs are those without it, bit for bit.
+values.  The outputs are those without it, bit for bit (``gated_linear`` of up to 16 rows: but for a
+rounding).  As nothing then ties the gradients to the
+activations, a backward under ``create_graph`` raises.
 """
 from __future__ import annotations
 
@@ -56,8 +58,8 @@ from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL
                qlayer_conv2d_bwd_weight, qlayer_conv2d_fwd, qlayer_conv2d_fwd_ex,
                qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex,
                qhead_distill_bwd, qhead_distill_fwd, qhead_linear_bwd, qhead_linear_fwd, qhead_logprobs_bwd,
-               qhead_logprobs_fwd, BLOCK_KEEP, qblock_gated_bwd, qblock_gated_fwd, qblock_norm_bwd, qblock_norm_fwd,
-               qblock_pack8, qblock_unpack8)
+               qhead_logprobs_fwd, BLOCK_KEEP, BlockGatedDesc, BlockKeepDesc, BlockNormDesc, HeadLinearDesc,
+               _block_launch, _head_act, _unaligned)
 
 __all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction", "linear_act", "token_logprobs",
            "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction", "group_norm_act",
@@ -118,23 +120,33 @@ def _kept(checkpoint):
     return checkpoint is not None
 
 
+def _no_graph():
+    """Refuses create_graph where a checkpoint stands for an activation."""
+    if torch.is_grad_enabled():
+        raise RuntimeError('checkpoint="int8" keeps no activation that a gradient could be differentiated through: no backward '
+                           "under create_graph, and none can be differentiated twice")
+
+
 def _pack(t):
-    """The 8-bit checkpoint (q, e) of a tensor, in blocks of its last dimension (None: none)."""
+    """The 8-bit checkpoint (q, e) of a matrix or a dense tensor, in blocks of its last dimension (None: none)."""
     if t is None:
         return None, None
-    rows = t if t.dim() == 2 else t.view(-1, t.shape[-1])
-    q = torch.empty(rows.shape, device=t.device, dtype=torch.int8)
-    e = torch.empty((rows.shape[0], -(-rows.shape[1] // BLOCK_KEEP)), device=t.device, dtype=torch.uint8)
-    qblock_pack8(rows, q, e)
+    cols = t.shape[-1]
+    rows = t.numel() // cols
+    q = torch.empty((rows, cols), device=t.device, dtype=torch.int8)
+    e = torch.empty((rows, -(-cols // BLOCK_KEEP)), device=t.device, dtype=torch.uint8)
+    ld = t.stride(0) if t.dim() == 2 and rows > 1 else cols
+    _block_launch("qblock_pack8", BlockKeepDesc(rows, cols, ld, _qdtype(t)), (t.data_ptr(), q.data_ptr(), e.data_ptr()), t.device)
     return q, e
 
 
 def _unpack(q, e, dtype, shape=None):
     if q is None:
         return None
-    t = torch.empty(q.shape, device=q.device, dtype=dtype)
-    qblock_unpack8(q, e, t)
-    return t if shape is None else t.view(shape)
+    rows, cols = q.shape
+    t = torch.empty(q.shape if shape is None else shape, device=q.device, dtype=dtype)
+    _block_launch("qblock_unpack8", BlockKeepDesc(rows, cols, cols, _qdtype(t)), (q.data_ptr(), e.data_ptr(), t.data_ptr()), q.device)
+    return t
 
 
 def _terms(ws, nt):
@@ -184,6 +196,7 @@ class QuadConv2dFunction(torch.autograd.Function):
     def backward(ctx, gy):
         d, nt = ctx.desc, ctx.nt
         if ctx.kept:
+            _no_graph()
             xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
             y_shape = (d.n, d.ho, d.wo, d.o)
             xn = _unpack(xq, xe, _tdtype(d.dtype), (d.n, d.h, d.w, d.c))
@@ -272,6 +285,7 @@ class QuadLinearFunction(torch.autograd.Function):
     def backward(ctx, gy):
         d, nt = ctx.desc, ctx.nt
         if ctx.kept:
+            _no_graph()
             xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
             xc = _unpack(xq, xe, _tdtype(d.dtype))
             ta, tb = _unpack(taq, tae, xc.dtype), _unpack(tbq, tbe, xc.dtype)
@@ -363,15 +377,9 @@ def _once(t, *of):
     return _Undifferentiable.apply(t, *of)
 
 
-def _tie(x):
-    """For _once where x itself is not kept: an empty tensor that stands in x's place in the graph, in a tuple (so that no
-    function takes it for an input)."""
-    return (x[..., :0].clone() if x.requires_grad and torch.is_grad_enabled() else None,)
-
-
 class LinearActFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, b, res, act, train=True, checkpoint=None, tie=None):
+    def forward(ctx, x, w, b, res, act, train=True, checkpoint=None):
         _same_device(x, w, b, res)
         if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
             raise ValueError(f"x (..., in) and w (out, in) are required, got {tuple(x.shape)} and {tuple(w.shape)}")
@@ -389,10 +397,10 @@ class LinearActFunction(torch.autograd.Function):
             ctx.kept = _kept(checkpoint)
             if ctx.kept:
                 # (of x only what the weight's gradient reads)
-                ctx.save_for_backward(*_pack(xm if ctx.needs_input_grad[1] else None), wm, *_pack(z), tie[0], w, b)
+                ctx.save_for_backward(*_pack(xm if ctx.needs_input_grad[1] else None), wm, *_pack(z))
             else:
                 ctx.save_for_backward(xm, wm, z, x, w, b)  # (the last three for _once; no copies)
-            ctx.act, ctx.xshape, ctx.wdtype, ctx.xdtype = act, x.shape, w.dtype, x.dtype
+            ctx.act, ctx.xshape, ctx.wdtype = act, x.shape, w.dtype
             ctx.bdtype = b.dtype if b is not None else None
             ctx.rdtype = res.dtype if res is not None else None
         return y.view(shape)
@@ -401,12 +409,9 @@ class LinearActFunction(torch.autograd.Function):
     def backward(ctx, gy):
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
         if ctx.kept:
-            xq, xe, w, zq, ze, *leaves = ctx.saved_tensors
-            x, z = _unpack(xq, xe, ctx.xdtype), _unpack(zq, ze, ctx.xdtype)
-            if x is None:  # (the gradients asked for do not read it)
-                x = torch.empty((ctx.xshape[:-1].numel(), w.shape[1]), device=w.device, dtype=ctx.xdtype)
-        else:
-            x, w, z, *leaves = ctx.saved_tensors
+            _no_graph()
+            return LinearActFunction._kept_backward(ctx, gy)
+        x, w, z, *leaves = ctx.saved_tensors
         dx = torch.empty(x.shape, device=x.device, dtype=x.dtype) if gx else None
         # (weights kept in float32 get the gradient as it was accumulated)
         dw = torch.empty(w.shape, device=x.device, dtype=x.dtype if ctx.wdtype is x.dtype else torch.float32) if gw else None
@@ -416,7 +421,25 @@ class LinearActFunction(torch.autograd.Function):
         of = leaves if ctx.act != "none" else (None, None, None)  # through act'(z)
         return (_once(dx.view(ctx.xshape), gy, leaves[1], *of) if gx else None,
                 _once(dw.to(ctx.wdtype), gy, leaves[0], *of) if gw else None,
-                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 4)
+                _once(db.to(ctx.bdtype), gy, *of) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 3)
+
+    @staticmethod
+    def _kept_backward(ctx, gy):
+        xq, xe, w, zq, ze = ctx.saved_tensors
+        gx, gw, gb, gr = ctx.needs_input_grad[:4]
+        dtype, dev = w.dtype, w.device
+        dx = dw = db = None
+        if gx or gw or gb:
+            x, z, dy = _unpack(xq, xe, dtype) if gw else None, _unpack(zq, ze, dtype), _matrix(gy)
+            (n, k), m = w.shape, dy.shape[0]
+            dx = torch.empty(ctx.xshape, device=dev, dtype=dtype) if gx else None
+            dw = torch.empty((n, k), device=dev, dtype=dtype if ctx.wdtype is dtype else torch.float32) if gw else None
+            db = torch.empty(n, device=dev) if gb else None
+            px, pw, pdy = _ptr(x), w.data_ptr(), dy.data_ptr()
+            desc = HeadLinearDesc(m, k, n, k, w.stride(0) if n > 1 else k, n, dy.stride(0) if m > 1 else n, _qdtype(w), _head_act(ctx.act),
+                                  _unaligned(px, pw, pdy), gw and dw.dtype is not dtype)
+            _block_launch("qhead_linear_bwd", desc, (px, pw, pdy, _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)), dev, "qhead_linear_bwd_workspace_size")
+        return (dx, dw.to(ctx.wdtype) if gw else None, db.to(ctx.bdtype) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 3)
 
 
 def linear_act(x, weight, bias=None, residual=None, act="none", checkpoint=None):
@@ -428,9 +451,9 @@ def linear_act(x, weight, bias=None, residual=None, act="none", checkpoint=None)
     pre-activation is kept for the backward in that dtype where there is an activation and
     gradients are on (under no_grad and inference_mode it is not even written).  checkpoint="int8": x and the
     pre-activation are kept in 8 bits."""
-    kept = _kept(checkpoint)
+    _kept(checkpoint)
     # (inside an autograd function gradients are off, and its needs_input_grad does not know of no_grad)
-    return LinearActFunction.apply(x, weight, bias, residual, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)
+    return LinearActFunction.apply(x, weight, bias, residual, act, torch.is_grad_enabled(), checkpoint)
 
 
 class TokenLogprobsFunction(torch.autograd.Function):
@@ -528,50 +551,82 @@ def distill_loss(logits, teacher_ids, teacher_logits, labels=None, temperature=1
 
 # --- blocks trained with activations in 8 bits ----------------------------------------
 
+def _dense_image(t):
+    """t with its values in channels-last order, dense (4 dimensions), or row after row (2)."""
+    return t.contiguous(memory_format=torch.channels_last) if t.dim() == 4 else t.contiguous()
+
+
+def _f32(t):
+    return t if t is None or (t.dtype is torch.float32 and t.is_contiguous()) else t.contiguous().float()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 class GroupNormActFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, groups, eps, act, train=True, checkpoint=None, tie=None):
+    def forward(ctx, x, weight, bias, groups, eps, act, train=True, checkpoint=None):
         _same_device(x, weight, bias)
         if x.dim() not in (2, 4):
             raise ValueError(f"x (N, C, H, W) or (N, C) is required, got {tuple(x.shape)}")
-        c = x.shape[1]
-        for name, t in (("weight", weight), ("bias", bias)):
-            if t is not None and t.shape != (c,):
-                raise ValueError(f"the {name} must have {c} elements")
-        xn = _nhwc(x) if x.dim() == 4 else x.contiguous()
-        gamma, beta = (t.contiguous().float() if t is not None else None for t in (weight, bias))
-        y = torch.empty(xn.shape, device=x.device, dtype=x.dtype)
+        n, c = x.shape[:2]
+        hw = 1 if x.dim() == 2 else x.shape[2] * x.shape[3]
+        if not isinstance(groups, int) or groups < 1 or c < 1 or c % groups or hw < 1:
+            raise ValueError(f"{groups!r} groups of {c} channels and {hw} pixels: a whole number that divides the channels is required")
+        if (weight is not None and weight.shape != (c,)) or (bias is not None and bias.shape != (c,)):
+            raise ValueError(f"weight and bias must have {c} elements")
+        xn = _dense_image(x)
+        gamma, beta = _f32(weight), _f32(bias)
+        y = torch.empty_like(xn)
+        desc = BlockNormDesc(n, hw, c, groups, _qdtype(x), _head_act(act), eps)
+        stats = q = e = mean = rstd = None
         train = train and any(ctx.needs_input_grad[:3])
         kept = train and _kept(checkpoint)
-        stats = torch.empty((2, x.shape[0], max(groups, 1)), device=x.device) if train else (None, None)
-        q = e = None
-        if kept:
-            q = torch.empty(xn.shape, device=x.device, dtype=torch.int8)
-            e = torch.empty(xn.shape[:-1] + (-(-c // BLOCK_KEEP),), device=x.device, dtype=torch.uint8)
-        qblock_norm_fwd(xn, groups, gamma, beta, y, stats[0], stats[1], q, e, act, eps)
         if train:
-            ctx.save_for_backward(None if kept else xn, q, e, gamma, beta, stats, tie[0] if kept else x, weight, bias)
-            ctx.groups, ctx.act, ctx.image = groups, act, x.dim() == 4
-        return y.permute(0, 3, 1, 2) if x.dim() == 4 else y
+            stats = torch.empty((2, n, groups), device=x.device)
+            mean = stats.data_ptr()
+            rstd = mean + 4 * n * groups
+        if kept:
+            q = torch.empty((n * hw, c), device=x.device, dtype=torch.int8)
+            e = torch.empty((n * hw, -(-c // BLOCK_KEEP)), device=x.device, dtype=torch.uint8)
+        _block_launch("qblock_norm_fwd", desc, (xn.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean, rstd, _ptr(q), _ptr(e)),
+                      x.device, "qblock_norm_fwd_workspace_size")
+        if train:
+            if kept:
+                ctx.save_for_backward(q, e, gamma, beta, stats)
+            else:
+                ctx.save_for_backward(xn, gamma, beta, stats, x, weight, bias)  # (the last three for _once; no copies)
+            ctx.desc, ctx.kept = desc, kept
+            ctx.dtypes = None if weight is None else weight.dtype, None if bias is None else bias.dtype
+        return y
 
     @staticmethod
     def backward(ctx, gy):
-        x, q, e, gamma, beta, stats, *leaves = ctx.saved_tensors
+        x = q = e = None
+        of = ()
+        if ctx.kept:
+            _no_graph()
+            q, e, gamma, beta, stats = ctx.saved_tensors
+        else:
+            x, gamma, beta, stats, *of = ctx.saved_tensors
         gx, gw, gb = ctx.needs_input_grad[:3]
-        dtype = x.dtype if x is not None else gy.dtype
-        dy = gy.to(dtype)
-        dy = _nhwc(dy) if ctx.image else dy.contiguous()
-        c = dy.shape[-1]
-        dx = torch.empty(dy.shape, device=dy.device, dtype=dtype) if gx else None
-        dgamma = torch.empty(c, device=dy.device) if gw else None
-        dbeta = torch.empty(c, device=dy.device) if gb else None
-        if gx or gw or gb:
-            qblock_norm_bwd(dy, x, ctx.groups, gamma, beta, stats[0], stats[1], dx, dgamma, dbeta, q, e, ctx.act)
-        if dx is not None and ctx.image:
-            dx = dx.permute(0, 3, 1, 2)
-        of = (gy, *leaves)
-        return (_once(dx, *of), _once(dgamma.to(leaves[1].dtype), *of) if gw else None,
-                _once(dbeta.to(leaves[2].dtype), *of) if gb else None, *[None] * 6)
+        desc = ctx.desc
+        dy = _dense_image(gy)
+        dx = torch.empty_like(dy) if gx else None
+        dgamma = torch.empty(desc.c, device=dy.device) if gw else None
+        dbeta = torch.empty(desc.c, device=dy.device) if gb else None
+        mean = stats.data_ptr()
+        _block_launch("qblock_norm_bwd", desc, (dy.data_ptr(), _ptr(x), _ptr(q), _ptr(e), _ptr(gamma), _ptr(beta), mean,
+                                                mean + 4 * desc.n * desc.groups, _ptr(dx), _ptr(dgamma), _ptr(dbeta)),
+                      dy.device, "qblock_norm_bwd_workspace_size")
+        if gw and ctx.dtypes[0] is not torch.float32:
+            dgamma = dgamma.to(ctx.dtypes[0])
+        if gb and ctx.dtypes[1] is not torch.float32:
+            dbeta = dbeta.to(ctx.dtypes[1])
+        if torch.is_grad_enabled():
+            dx, dgamma, dbeta = (_once(t, gy, *of) for t in (dx, dgamma, dbeta))
+        return dx, dgamma, dbeta, None, None, None, None, None
 
 
 def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", checkpoint=None):
@@ -579,65 +634,83 @@ def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", chec
 
     x (N, C, H, W), used in channels_last memory, or (N, C); weight and bias (C) or None; act as in linear_act.
     The backward reads x, or with checkpoint="int8" what 8 bits of it say."""
-    kept = _kept(checkpoint)
-    return GroupNormActFunction.apply(x, weight, bias, groups, eps, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)
+    _kept(checkpoint)
+    return GroupNormActFunction.apply(x, weight, bias, groups, eps, act, torch.is_grad_enabled(), checkpoint)
 
 
 class GatedLinearFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, wg, wu, bg, bu, act, train=True, checkpoint=None, tie=None):
+    def forward(ctx, x, wg, wu, bg, bu, act, train=True, checkpoint=None):
         _same_device(x, wg, wu, bg, bu)
         if wg.dim() != 2 or x.dim() < 1 or x.shape[-1] != wg.shape[1] or wu.shape != wg.shape:
             raise ValueError(f"x (..., in) and two weights (out, in) are required, got {tuple(x.shape)}, {tuple(wg.shape)} and "
                              f"{tuple(wu.shape)}")
-        for b in (bg, bu):
-            if b is not None and b.shape != wg.shape[:1]:
-                raise ValueError(f"each bias must have {wg.shape[0]} elements")
-        xm, wgm, wum = _matrix(x), _matrix(wg.to(x.dtype)), _matrix(wu.to(x.dtype))
+        if (bg is not None and bg.shape != wg.shape[:1]) or (bu is not None and bu.shape != wg.shape[:1]):
+            raise ValueError(f"each bias must have {wg.shape[0]} elements")
+        dtype, dev = x.dtype, x.device
+        xm, wgm, wum = _matrix(x), _matrix(wg.to(dtype)), _matrix(wu.to(dtype))
         if wgm.stride() != wum.stride():
             wgm, wum = wgm.contiguous(), wum.contiguous()
-        m, n = xm.shape[0], wg.shape[0]
-        h = torch.empty((m, n), device=x.device, dtype=x.dtype)
+        (m, k), n = xm.shape, wg.shape[0]
+        h = torch.empty((m, n), device=dev, dtype=dtype)
         train = train and any(ctx.needs_input_grad[:5])
         kept = train and _kept(checkpoint)
-        z = torch.empty((2, m, n), device=x.device, dtype=x.dtype) if train and not kept else None
+        z = torch.empty((2, m, n), device=dev, dtype=dtype) if train and not kept else None
         q = e = None
         if kept:
-            q = torch.empty((2, m, n), device=x.device, dtype=torch.int8)
-            e = torch.empty((2, m, -(-n // BLOCK_KEEP)), device=x.device, dtype=torch.uint8)
-        qblock_gated_fwd(xm, wgm, wum, bg.contiguous().float() if bg is not None else None,
-                         bu.contiguous().float() if bu is not None else None, h, z, q, e, act)
+            q = torch.empty((2, m, n), device=dev, dtype=torch.int8)
+            e = torch.empty((2, m, -(-n // BLOCK_KEEP)), device=dev, dtype=torch.uint8)
+        bgf, buf = _f32(bg), _f32(bu)
+        ldx, ldw = (xm.stride(0) if m > 1 else k), (wgm.stride(0) if n > 1 else k)
+        px, pg, pu = xm.data_ptr(), wgm.data_ptr(), wum.data_ptr()
+        desc = BlockGatedDesc(m, k, n, ldx, ldw, n, _qdtype(x), _head_act(act), _unaligned(px, pg, pu), 0)
+        _block_launch("qblock_gated_fwd", desc, (px, pg, pu, _ptr(bgf), _ptr(buf), h.data_ptr(), _ptr(z), _ptr(q), _ptr(e)), dev,
+                      "qblock_gated_fwd_workspace_size")
         if train:
             # (of x only what the weights' gradients read)
             xs = xm if any(ctx.needs_input_grad[1:3]) else None
-            xq, xe = _pack(xs) if kept else (None, None)
-            ctx.save_for_backward(None if kept else xs, xq, xe, wgm, wum, z, q, e, tie[0] if kept else x, wg, wu, bg, bu)
-            ctx.act, ctx.xshape = act, x.shape
-        return h.view(x.shape[:-1] + (n,))
+            if kept:
+                ctx.save_for_backward(*_pack(xs), wgm, wum, q, e)
+            else:
+                ctx.save_for_backward(xs, wgm, wum, z, x, wg, wu, bg, bu)  # (the last five for _once; no copies)
+            ctx.kept, ctx.act, ctx.xshape, ctx.dtypes = kept, act, x.shape, [None if t is None else t.dtype for t in (wg, wu, bg, bu)]
+        return h if x.dim() == 2 else h.view(x.shape[:-1] + (n,))
 
     @staticmethod
     def backward(ctx, gh):
-        x, xq, xe, wg, wu, z, q, e, *leaves = ctx.saved_tensors
+        x = z = q = e = None
+        of = ()
         gx, gwg, gwu, gbg, gbu = ctx.needs_input_grad[:5]
-        dtype, dev, gw = wg.dtype, wg.device, gwg or gwu
-        dh = _matrix(gh.to(dtype))
-        if xq is not None and gw:
-            x = _unpack(xq, xe, dtype)
-        n, k = wg.shape
-        wdtype = leaves[1].dtype if leaves[1].dtype == leaves[2].dtype == dtype else torch.float32
-        dx = torch.empty((dh.shape[0], k), device=dev, dtype=dtype) if gx else None
+        gw = gwg or gwu
+        if ctx.kept:
+            _no_graph()
+            xq, xe, wg, wu, q, e = ctx.saved_tensors
+            if gw:
+                x = _unpack(xq, xe, wg.dtype)
+        else:
+            x, wg, wu, z, *of = ctx.saved_tensors
+        dtype, dev = wg.dtype, wg.device
+        dh = _matrix(gh)
+        (n, k), m = wg.shape, dh.shape[0]
         # (weights kept in float32 get the gradient as it was accumulated)
-        dwg, dwu = (torch.empty((n, k), device=dev, dtype=wdtype) if gw else None for _ in range(2))
-        dbg, dbu = (torch.empty(n, device=dev) if g else None for g in (gbg, gbu))
-        if gx or gw or gbg or gbu:
-            qblock_gated_bwd(x if gw else None, wg, wu, dh, z, dx, dwg, dwu, dbg, dbu, q, e, ctx.act)
-        of = (gh, *leaves)
-
-        def done(t, leaf, wanted):
-            return _once(t.to(leaf.dtype), *of) if wanted else None
-
-        return (_once(dx.view(ctx.xshape), *of) if gx else None, done(dwg, leaves[1], gwg), done(dwu, leaves[2], gwu),
-                done(dbg, leaves[3], gbg), done(dbu, leaves[4], gbu), *[None] * 4)
+        wdtype = dtype if ctx.dtypes[0] is dtype and ctx.dtypes[1] is dtype else torch.float32
+        dx = torch.empty(ctx.xshape, device=dev, dtype=dtype) if gx else None
+        dwg = torch.empty((n, k), device=dev, dtype=wdtype) if gw else None
+        dwu = torch.empty((n, k), device=dev, dtype=wdtype) if gw else None
+        dbg = torch.empty(n, device=dev) if gbg else None
+        dbu = torch.empty(n, device=dev) if gbu else None
+        px, pg, pu = _ptr(x) if gw else None, wg.data_ptr(), wu.data_ptr()
+        desc = BlockGatedDesc(m, k, n, x.stride(0) if x is not None and m > 1 else k, wg.stride(0) if n > 1 else k,
+                              dh.stride(0) if m > 1 else n, _qdtype(wg), _head_act(ctx.act), _unaligned(px, pg, pu), wdtype is not dtype)
+        _block_launch("qblock_gated_bwd", desc, (px, pg, pu, dh.data_ptr(), _ptr(z), _ptr(q), _ptr(e), _ptr(dx), _ptr(dwg), _ptr(dwu),
+                                                 _ptr(dbg), _ptr(dbu)), dev, "qblock_gated_bwd_workspace_size")
+        out = [dx, dwg if gwg else None, dwu if gwu else None, dbg, dbu]
+        for i, d in enumerate(ctx.dtypes, 1):
+            if out[i] is not None and out[i].dtype is not d:
+                out[i] = out[i].to(d)
+        if torch.is_grad_enabled():
+            out = [_once(t, gh, *of) for t in out]
+        return (*out, None, None, None)
 
 
 def gated_linear(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", checkpoint=None):
@@ -645,5 +718,5 @@ def gated_linear(x, w_gate, w_up, b_gate=None, b_up=None, act="silu", checkpoint
 
     Both projections, the activation (as in linear_act) and the product run in one kernel in the dtype of x.  The projections
     are kept for the backward in that dtype, or, and x with them, in 8 bits under checkpoint="int8"."""
-    kept = _kept(checkpoint)
-    return GatedLinearFunction.apply(x, w_gate, w_up, b_gate, b_up, act, torch.is_grad_enabled(), checkpoint, _tie(x) if kept else None)
+    _kept(checkpoint)
+    return GatedLinearFunction.apply(x, w_gate, w_up, b_gate, b_up, act, torch.is_grad_enabled(), checkpoint)

@@ -40,8 +40,7 @@ void share_samples(NormPlan &p, int n, long long most) {
 }
 
 // bwd: the backward's plan (its registers hold dy as well, its workgroups share few lines of a.chan).
-// emit: the segments begin at blocks of the checkpoint.
-NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
+NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
     NormPlan p{};
     NormArgs &a = p.a;
     const int cpg = d->c / d->groups, es = (int)esize(d->dtype);
@@ -49,16 +48,10 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
     a.act = (int)d->act, a.eps = d->eps;
     p.u = cpg % 8 == 0 ? 8 : 1;
     a.parts = 1, a.part_c = cpg;
-    // whole groups whose channels are a multiple of a checkpoint's block
-    int unit = 1;
-    if (emit)
-        while (unit < kKeep && (long long)unit * cpg % kKeep) unit *= 2;
-    const int least = std::min(d->groups, unit);
     auto segment = [&](int gps) {
-        a.gps = std::min(d->groups, (gps + unit - 1) / unit * unit);
+        a.gps = std::max(1, std::min(d->groups, gps));
         a.segs = cdiv(d->groups, a.gps);
         a.svl = log2_up(((long long)a.gps * cpg + 7) / 8);
-        if (emit) a.svl = std::max(a.svl, 2);
     };
     // Registers.  Time of a candidate in us: a launch, then the values of a workgroup at `each` ns (fitted on 12 maps from
     // 1 x 1024 x 512 to 128 x 1024 x 256 and 8192 rows of 1024; segments of a line of 128, 64 or 32 bytes, of which the XCD's L2
@@ -72,7 +65,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
     if (cpg <= 8 * 512 && forced != 0)
         for (int line : {128, 64, 32}) {
             if (forced_line && line != forced_line) continue;
-            segment(std::max(least, cdiv(line, cpg * es)));
+            segment(cdiv(line, cpg * es));
             for (int th : {256, 512}) {
                 const int lth = log2_up(th);
                 if (a.svl > lth) continue;
@@ -88,7 +81,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
             }
         }
     if (line_at) {
-        segment(std::max(least, cdiv(line_at, cpg * es)));
+        segment(cdiv(line_at, cpg * es));
         const int lth = log2_up(th_at);
         const long long need = (d->hw + (1LL << (lth - a.svl)) - 1) >> (lth - a.svl);
         a.pnl = lth - a.svl;
@@ -114,11 +107,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd, bool emit) {
         a.segs = d->groups * a.parts;
         a.svl = 8;
     } else {
-        segment(std::max(least, 512 / cpg));
-        if ((long long)a.gps * cpg > 2048) {  // (the checkpoint is written by itself then)
-            unit = 1;
-            segment(std::max(1, 2048 / cpg));
-        }
+        segment(512 / cpg);
     }
     a.pnl = 8 - a.svl;
     // steps of the workgroup's pixel lanes: at most 128 a chunk (a thread's sums stay short), else what gives every CU four workgroups
@@ -141,7 +130,8 @@ template <bool STATS> void launch_join(const NormArgs &a, hipStream_t st) {
     hipLaunchKernelGGL((qblock_norm_join_kernel<STATS>), dim3(grid_1d((long long)a.n * a.groups * lanes)), dim3(kThreads), 0, st, a);
 }
 
-// Whether the forward's launches can write the checkpoint on the way.
+// Whether the forward's launches can write the checkpoint on the way: segments of whole blocks, whose lanes are quads.  (Else
+// a launch of its own does: the plan, and with it the order of the sums, is the same with a checkpoint and without.)
 bool emits(const NormPlan &p) { return p.a.parts == 1 && (p.a.segs == 1 || p.a.gps * p.a.cpg % kKeep == 0) && p.a.svl >= 2; }
 
 template <typename T, int U> ql_status launch_fwd(const NormPlan &p, const NormArgs &a, hipStream_t st) {
@@ -191,8 +181,7 @@ extern "C" {
 
 size_t qblock_norm_fwd_workspace_size(const qblock_norm_desc *d) {
     if (!norm_ok(d) || !sizes_fit(d) || d->n == 0) return 0;
-    // (with a checkpoint the segments may be others)
-    return std::max(plan_norm(d, false, false).bytes(), plan_norm(d, false, true).bytes());
+    return plan_norm(d, false).bytes();
 }
 
 ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float *gamma, const float *beta, void *y, float *mean,
@@ -209,7 +198,7 @@ ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float 
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const NormPlan p = plan_norm(d, false, q != nullptr);
+    const NormPlan p = plan_norm(d, false);
     NormArgs a = p.a;
     a.x = x, a.out = y, a.gamma = gamma, a.beta = beta, a.mean = mean, a.rstd = rstd;
     a.part = static_cast<float2 *>(workspace);
@@ -228,7 +217,7 @@ ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float 
 
 size_t qblock_norm_bwd_workspace_size(const qblock_norm_desc *d) {
     if (!norm_ok(d) || !sizes_fit(d) || d->n == 0) return 0;
-    return plan_norm(d, true, false).bytes();
+    return plan_norm(d, true).bytes();
 }
 
 ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void *x, const int8_t *q, const uint8_t *e, const float *gamma,
@@ -252,7 +241,7 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void 
     const size_t need = qblock_norm_bwd_workspace_size(d);
     if (workspace_bytes < need || (need && !workspace)) return QL_EWORKSPACE;
     if (workspace && !aligned16(workspace)) return QL_EINVAL;
-    const NormPlan p = plan_norm(d, true, false);
+    const NormPlan p = plan_norm(d, true);
     NormArgs a = p.a;
     a.x = x, a.dy = dy, a.out = dx, a.gamma = gamma, a.beta = beta;
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);

@@ -221,26 +221,12 @@ def test_unknown_checkpoints_are_refused(call):
 
 @pytest.fixture
 def calls(monkeypatch):
-    """The library's calls replaced by stand-ins that fill every output; each call's arguments by name."""
+    """The library's calls replaced by stand-ins that compute nothing; each call's name and pointers."""
     seen = []
-    names = {"qblock_norm_fwd": "x groups gamma beta y mean rstd q e act eps", "qblock_gated_fwd": "x wg wu bg bu h z q e act",
-             "qblock_norm_bwd": "dy x groups gamma beta mean rstd dx dgamma dbeta q e act", "qblock_pack8": "x q e",
-             "qblock_gated_bwd": "x wg wu dh z dx dwg dwu dbg dbu q e act", "qblock_unpack8": "q e x", "qhead_linear_fwd": "x w b res y z",
-             "qhead_linear_bwd": "x w dy z dx dw db"}
-    outputs = {"fwd": "y mean rstd q e h z", "bwd": "dx dgamma dbeta dwg dwu dbg dbu dw db", "pack8": "q e", "unpack8": "x"}
-
-    def stand_in(name):
-        def call(*args, **kw):
-            got = {**dict(zip(names[name].split(), args)), "call": name}
-            for k in outputs[name.split("_")[-1]].split():
-                if got.get(k) is not None:
-                    got[k].fill_(1)
-            seen.append(got)
-        return call
-
     monkeypatch.setattr(ag, "_same_device", lambda *tensors: None)
-    for name in names:
-        monkeypatch.setattr(ag, name, stand_in(name))
+    monkeypatch.setattr(ag, "_block_launch", lambda name, desc, ptrs, device, query=None: seen.append((name, ptrs)))
+    for name in ("qhead_linear_fwd", "qhead_linear_bwd"):
+        monkeypatch.setattr(ag, name, lambda *args, _name=name, **kw: seen.append((_name, args)))
     return seen
 
 
@@ -256,26 +242,27 @@ def layers(checkpoint):
 @pytest.mark.parametrize("checkpoint", [None, "int8"])
 @pytest.mark.parametrize("which", ["norm", "rows", "gated", "linear"])
 def test_gradients_arrive_and_a_second_derivative_raises(calls, which, checkpoint):
+    """In 8 bits, where nothing ties a gradient to the activation, already a backward that a second one could follow."""
     leaves, f = layers(checkpoint)[which]
     y = f(*leaves)
     grads = torch.autograd.grad(y.sum(), leaves, retain_graph=True)
     for leaf, g in zip(leaves, grads):
-        assert g.shape == leaf.shape and not g.requires_grad and bool((g == 1).all())
+        assert g.shape == leaf.shape and not g.requires_grad
     for i in range(len(leaves) if which != "linear" else 2):
-        g, = torch.autograd.grad(y.sum(), leaves[i], create_graph=True)
         with pytest.raises(RuntimeError, match="twice"):
+            g, = torch.autograd.grad(y.sum(), leaves[i], create_graph=True, retain_graph=True)
             torch.autograd.grad(g.square().sum(), leaves[0], retain_graph=True, allow_unused=True)
 
 
 @pytest.mark.parametrize("which", ["norm", "gated", "linear"])
 def test_what_a_checkpoint_keeps(calls, which):
-    """In 8 bits: nothing of the forward's dtype but the parameters is kept, and x is not either."""
+    """In 8 bits: nothing of the forward's dtype but the parameters and statistics is kept, and x is not either."""
     leaves, f = layers("int8")[which]
     y = f(*leaves)
-    big = [t for t in y.grad_fn.saved_tensors if t is not None and t.dtype == torch.float32 and t.numel() > 12 * 2]
-    assert all(any(t.shape == leaf.shape for leaf in leaves[1:]) for t in big)
-    ptrs = {t.data_ptr() for t in y.grad_fn.saved_tensors if t is not None and t.numel()}
-    assert leaves[0].data_ptr() not in ptrs
+    kept = [t for t in y.grad_fn.saved_tensors if t is not None]
+    for t in kept:
+        assert t.dtype in (torch.int8, torch.uint8) or any(t.shape == leaf.shape for leaf in leaves[1:]) or t.shape == (2, 2, 3)
+    assert leaves[0].data_ptr() not in {t.data_ptr() for t in kept}
 
 
 @pytest.mark.parametrize("off", [torch.no_grad, torch.inference_mode])
@@ -284,13 +271,15 @@ def test_serving_writes_nothing_for_a_backward(calls, off):
         for which in ("norm", "gated", "linear"):
             leaves, f = layers("int8")[which]
             assert not f(*leaves).requires_grad
-    assert [c["call"] for c in calls] == ["qblock_norm_fwd", "qblock_gated_fwd", "qhead_linear_fwd"]
-    assert all(c.get(k) is None for c in calls for k in ("mean", "rstd", "q", "e", "z"))
+    assert [name for name, _ in calls] == ["qblock_norm_fwd", "qblock_gated_fwd", "qhead_linear_fwd"]
+    assert calls[0][1][4:] == (None,) * 4  # mean, rstd, q, e
+    assert calls[1][1][6:] == (None,) * 3 and calls[2][1][5] is None  # z, q, e; z
 
 
 def test_only_what_is_asked_for(calls):
     (x, wg, wu, bg, bu), f = layers("int8")["gated"]
     y = f(x, wg.detach(), wu.detach(), bg, bu)
     y.sum().backward()
-    assert [c["call"] for c in calls] == ["qblock_gated_fwd", "qblock_gated_bwd"]  # (x is not packed: no weight needs it)
-    assert calls[1]["x"] is None and calls[1]["dwg"] is None and calls[1]["dx"] is not None and x.grad is not None and wg.grad is None
+    assert [name for name, _ in calls] == ["qblock_gated_fwd", "qblock_gated_bwd"]  # (x is not packed: no weight needs it)
+    px, *_, dx, dwg, dwu, dbg, dbu = calls[1][1]
+    assert px is None and dwg is None and dwu is None and dx and dbg and dbu and x.grad is not None and wg.grad is None

@@ -1,0 +1,264 @@
+"""checkpoint="int8" of every layer that has it: the outputs are those without it, the gradients those that the library's calls
+give from the checkpoints' values, bit for bit; memory; graphs; a network of all of them."""
+import math
+
+import pytest
+import torch
+
+import block_ref as ref
+import paper_2204_01701_amd as ql
+from paper_2204_01701_amd.autograd import gated_linear, group_norm_act, linear_act, quad_conv2d, quad_linear
+from test_gpu_block_keep import DEV, TYPES, type_ids
+
+pytestmark = pytest.mark.gpu
+
+
+def back(t):
+    """What the checkpoint of t (in blocks of its last dimension) stands for."""
+    x = t.reshape(-1, t.shape[-1]).contiguous()
+    q = torch.empty(x.shape, device=DEV, dtype=torch.int8)
+    e = torch.empty(x.shape[0], -(-x.shape[1] // 32), device=DEV, dtype=torch.uint8)
+    ql.qblock_pack8(x, q, e)
+    out = torch.empty_like(x)
+    ql.qblock_unpack8(q, e, out)
+    return out.view(t.shape)
+
+
+def leaves(*shapes, dtype, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return [(torch.randn(s, generator=g, device=DEV) / (math.sqrt(math.prod(s[1:])) if i else 1)).to(dtype).requires_grad_(True)
+            for i, s in enumerate(shapes)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("m,k,n", [(70, 72, 80), (33, 41, 24), (5, 100, 7)])
+def test_first_order_layer(m, k, n, act, dtype):
+    x, w, b = leaves((m, k), (n, k), (n, 1), dtype=dtype)
+    b = b.detach().float().view(n).requires_grad_(True)
+    y, yk = linear_act(x, w, b, act=act), linear_act(x, w, b, act=act, checkpoint="int8")
+    assert torch.equal(y, yk)
+    dy = torch.randn(m, n, device=DEV).to(dtype)
+    got = torch.autograd.grad(yk, (x, w, b), dy)
+    xd, wd = x.detach(), w.detach()
+    z = torch.empty_like(y)
+    ql.qhead_linear_fwd(xd, wd, b.detach(), None, torch.empty_like(y), z, act=act)
+    dx, dw, db = torch.empty_like(xd), torch.empty_like(wd), torch.empty(n, device=DEV)
+    ql.qhead_linear_bwd(back(xd), wd, dy, back(z), dx, dw, db, act=act)
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw) and torch.equal(got[2], db)
+    gx, = torch.autograd.grad(linear_act(x, wd, act=act, checkpoint="int8"), x, dy)
+    assert gx.shape == x.shape
+    wide = w.detach().float().requires_grad_(True)  # a float32 weight beside bf16: its gradient unrounded
+    gw, = torch.autograd.grad(linear_act(x, wide, b, act=act, checkpoint="int8"), wide, dy)
+    dw32 = torch.empty(n, k, device=DEV)
+    ql.qhead_linear_bwd(back(xd), wd, dy, back(z), None, dw32, act=act)
+    assert gw.dtype == torch.float32 and torch.equal(gw, dw32)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("recompute", [False, True], ids=["save", "recompute"])
+@pytest.mark.parametrize("relu", [False, True], ids=["linear", "relu"])
+@pytest.mark.parametrize("neuron", sorted(ql.NEURON_TERMS))
+def test_quadratic_dense(neuron, relu, recompute, dtype):
+    nt = ql.NEURON_TERMS[neuron]
+    shape = (24, 24) if neuron == ql.QL_NEURON_T4_IDENTITY else (40, 24)
+    x, *w = leaves((20, 24), *[shape] * nt, dtype=dtype)
+    w += [None] * (3 - nt)
+    how = dict(neuron=neuron, relu=relu, recompute=recompute)
+    y, yk = quad_linear(x, *w, **how), quad_linear(x, *w, checkpoint="int8", **how)
+    assert torch.equal(y, yk)
+    dy = torch.randn_like(y)
+    got = torch.autograd.grad(yk, [x] + w[:nt], dy)
+    # the same from the checkpoints' values: X, and the maps of the layer (recomputed from it)
+    x8 = back(x.detach())
+    d = ql.linear_desc(20, 24, shape[0], ql.QL_BF16 if dtype == torch.bfloat16 else ql.QL_F32, neuron)
+    wd = [t.detach() if t is not None else None for t in w]
+    ta, tb = torch.empty_like(y), torch.empty_like(y) if nt >= 2 else None
+    if neuron != ql.QL_NEURON_T2:
+        ql.qlayer_linear_fwd(d, x8 if recompute else x.detach(), *wd, y=None if recompute else torch.empty_like(y), ta=ta, tb=tb)
+        if not recompute:
+            ta, tb = back(ta), back(tb) if tb is not None else None
+    else:
+        ta = tb = None
+    dx, dw = torch.empty_like(x8), [torch.empty(shape, device=DEV) if t is not None else None for t in w]
+    if relu:
+        ql.qlayer_linear_bwd_relu(d, x8, dy, y.detach(), ta, tb, *wd, dx, *dw)
+    else:
+        ql.qlayer_linear_bwd(d, x8, dy, ta, tb, *wd, dx, *dw)
+    assert torch.equal(got[0], dx)
+    for g, r in zip(got[1:], dw):
+        assert torch.equal(g, r.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("how", [dict(), dict(recompute=True), dict(relu=True), dict(stride=2)], ids=["save", "recompute", "relu", "stride"])
+def test_quadratic_convolution(how, dtype):
+    x, *w = leaves((3, 20, 9, 7), *[(36, 20, 3, 3)] * 3, dtype=dtype)
+    b = [torch.randn(36, device=DEV, requires_grad=True) for _ in range(3)]
+    y, yk = quad_conv2d(x, *w, *b, pad=1, **how), quad_conv2d(x, *w, *b, pad=1, checkpoint="int8", **how)
+    assert torch.equal(y, yk)
+    dy = torch.randn_like(y)
+    got = torch.autograd.grad(yk, [x, *w, *b], dy)
+    # X alone decides under recompute: the layer at the checkpoint's values (whose own mask a ReLU would take from another output)
+    if how.get("recompute"):
+        x8 = back(x.detach().permute(0, 2, 3, 1)).permute(0, 3, 1, 2).requires_grad_(True)
+        want = torch.autograd.grad(quad_conv2d(x8, *w, *b, pad=1, **how), [x8, *w, *b], dy)
+        assert all(torch.equal(g, r) for g, r in zip(got, want))
+    full = torch.autograd.grad(y, [x, *w, *b], dy)
+    for i, (g, r) in enumerate(zip(got, full)):
+        # a value kept is off by at most 1/127 of its block's largest, uniformly in between: 2^-2 of that largest is about a
+        # standard deviation of normal values, so each factor is off by 2 / 127 / sqrt(12) of its size in the mean (0.0046; for two
+        # factors 0.0065), and bf16 rounds on top of either side
+        assert (g - r).double().norm() <= 0.02 * r.double().norm(), i
+
+
+def test_depthwise():
+    x, *w = leaves((2, 16, 9, 9), *[(16, 1, 3, 3)] * 3, dtype=torch.float32)
+    y, yk = (quad_conv2d(x, *w, pad=1, groups=16, checkpoint=c) for c in (None, "int8"))
+    assert torch.equal(y, yk)
+    got, full = (torch.autograd.grad(t.square().sum(), [x, *w]) for t in (yk, y))
+    for g, r in zip(got, full):
+        assert (g - r).norm() <= 0.02 * r.norm()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gated(act, dtype):
+    x, wg, wu = leaves((2, 35, 72), (40, 72), (40, 72), dtype=dtype)
+    bg, bu = (torch.randn(40, device=DEV, requires_grad=True) for _ in range(2))
+    h, hk = (gated_linear(x, wg, wu, bg, bu, act=act, checkpoint=c) for c in (None, "int8"))
+    assert torch.equal(h, hk)
+    dh = torch.randn_like(h)
+    got = torch.autograd.grad(hk, (x, wg, wu, bg, bu), dh)
+    xm, dhm = x.detach().view(70, 72), dh.view(70, 40)
+    q, e = torch.empty(2, 70, 40, device=DEV, dtype=torch.int8), torch.empty(2, 70, 2, device=DEV, dtype=torch.uint8)
+    h2 = torch.empty(70, 40, device=DEV, dtype=dtype)
+    ql.qblock_gated_fwd(xm, wg.detach(), wu.detach(), bg.detach(), bu.detach(), h2, None, q, e, act=act)
+    assert torch.equal(h2, h.view(70, 40))
+    out = [torch.empty_like(xm), torch.empty_like(wg), torch.empty_like(wu), torch.empty(40, device=DEV), torch.empty(40, device=DEV)]
+    ql.qblock_gated_bwd(back(xm), wg.detach(), wu.detach(), dhm, None, *out, q=q, e=e, act=act)
+    assert torch.equal(got[0].view(70, 72), out[0]) and all(torch.equal(a, b) for a, b in zip(got[1:], out[1:]))
+    # and from the input alone in a batch of few rows: the same kernel as for many
+    few = x.detach()[0, :5].requires_grad_(True)
+    a, b = (gated_linear(few, wg, wu, act=act, checkpoint=c) for c in (None, "int8"))
+    assert (a.double() - b.double()).abs().max() <= 2.0**-7 * a.abs().max()  # (few rows with a checkpoint take another kernel: a rounding)
+
+
+class Block:
+    """norm -> gated layer -> down projection with the input as residual, on rows of `width`."""
+
+    def __init__(self, width, hidden, dtype, seed):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+
+        def w(o, i):
+            return (torch.randn(o, i, generator=g, device=DEV) / math.sqrt(i)).to(dtype).requires_grad_(True)
+
+        self.gamma, self.beta = (torch.ones(width, device=DEV, requires_grad=True), torch.zeros(width, device=DEV, requires_grad=True))
+        self.wg, self.wu, self.wd = w(hidden, width), w(hidden, width), w(width, hidden)
+        self.leaves = [self.gamma, self.beta, self.wg, self.wu, self.wd]
+
+    def __call__(self, x, checkpoint=None):
+        h = group_norm_act(x, 4, self.gamma, self.beta, checkpoint=checkpoint)
+        h = gated_linear(h, self.wg, self.wu, checkpoint=checkpoint)
+        return linear_act(h, self.wd, residual=x, checkpoint=checkpoint)
+
+
+def test_a_network_of_them_against_float64():
+    """fp32, three blocks: without checkpoints the gradients of the definition; with them within what their steps allow."""
+    blocks = [Block(48, 100, torch.float32, s) for s in range(3)]
+    x = torch.randn(65, 48, device=DEV, requires_grad=True)
+    every = [x] + [t for b in blocks for t in b.leaves]
+
+    def run(checkpoint):
+        y = x
+        for b in blocks:
+            y = b(y, checkpoint)
+        return y, torch.autograd.grad(y.square().sum() / 65, every)
+
+    v = [t.detach().double().cpu().requires_grad_(True) for t in every]
+    y = v[0]
+    for i in range(3):
+        ga, be, wg, wu, wd = v[1 + 5 * i:6 + 5 * i]
+        h = torch.nn.functional.group_norm(y, 4, ga, be, 1e-5)
+        y = (torch.nn.functional.silu(h @ wg.t()) * (h @ wu.t())) @ wd.t() + y
+    want = torch.autograd.grad(y.square().sum() / 65, v)
+    (y0, plain), (y8, kept) = run(None), run("int8")
+    assert torch.equal(y0, y8)
+    for g, k, r in zip(plain, kept, want):
+        # three blocks of four sums of up to 100 products, forward and back: a few hundred roundings of 2^-24 at most
+        assert (g.double().cpu() - r).norm() <= 2e-5 * r.norm()
+        # four kept factors a block, each off by 0.0046 of its size in the mean (as above), in three blocks
+        assert (k.double().cpu() - r).norm() <= 0.0046 * math.sqrt(12) * 2 * r.norm()
+
+
+def test_memory_between_forward_and_backward():
+    """bf16: what a block keeps shrinks to the bytes of its checkpoints."""
+    m, width, hidden = 8192, 256, 1024
+    b = Block(width, hidden, torch.bfloat16, 0)
+    held = {}
+    for c in (None, "int8"):
+        x = torch.randn(m, width, device=DEV, dtype=torch.bfloat16).requires_grad_(True)
+        h = x * 1  # (an activation that only the block holds)
+        del x
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        y = b(h, c)
+        del h
+        torch.cuda.synchronize()
+        held[c] = torch.cuda.memory_allocated() - before
+        y.sum().backward()
+        del y
+    # besides the output (counted in both; the input, freed with checkpoints, is counted in neither): norm output, g, u and h
+    # against x, norm output, g, u and h at 33/64 of their bytes
+    out, full, kept = 2 * m * width, 2 * m * (width + 3 * hidden), (1 + 1 / 32) * m * (2 * width + 3 * hidden) - 2 * m * width
+    assert held[None] >= out + full and held["int8"] <= out + kept + (4 << 20), held
+
+
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+def test_captured_and_replayed(checkpoint):
+    """A step of the block in a graph, replayed on new inputs with eager work in between: the eager results every time."""
+    b = Block(64, 96, torch.bfloat16, 1)
+    x = torch.randn(130, 64, device=DEV, dtype=torch.bfloat16)
+
+    def step(x):
+        x = x.detach().requires_grad_(True)
+        y = b(x, checkpoint)
+        return (y.detach(), *torch.autograd.grad(y, [x] + b.leaves, torch.ones_like(y)))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(2):
+            step(x)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x)
+    for i in range(4):
+        x.copy_(torch.randn(130, 64, device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(x.clone())
+        assert all(torch.equal(a, w) for a, w in zip(out, want)), i
+
+
+def test_two_streams_at_once():
+    """Two blocks on two streams, whose workspaces must not meet."""
+    b = Block(64, 200, torch.bfloat16, 2)
+    xs = [torch.randn(3000, 64, device=DEV, dtype=torch.bfloat16).requires_grad_(True) for _ in range(2)]
+
+    def step(x):
+        return torch.autograd.grad(b(x, "int8").float().square().sum(), [x] + b.leaves)
+
+    want = [step(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for _ in range(5):
+        for i, (st, x) in enumerate(zip(streams, xs)):
+            with torch.cuda.stream(st):
+                got[i].append(step(x))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, w) for a, w in zip(g, want[i]))
