@@ -61,4 +61,18 @@ template <int N> __device__ __forceinline__ void block_slopes(int act, const flo
 #undef BLOCK_SWITCH
 #undef BLOCK_ALL
 
+// Eight neighbours stored as what is not read again (`stream`, uniform): they do not drive out of the L2 what the workgroups
+// beside share, and a launch's stores do not queue behind its loads' lines.  For whole lines only: parts of them, written
+// past the L2, reach memory one by one.
+template <typename T> __device__ __forceinline__ void block_store8(T *p, const float *v, int n, bool stream) {
+    if (stream && n >= 8) {
+        // (without something of its own on either side the branch is merged with the other, and the hint is lost)
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 8; h += Elem<T>::VEC) __builtin_nontemporal_store(vpack<T>(v + h), reinterpret_cast<v4u_row *>(p + h));
+        asm volatile("" ::: "memory");
+    } else {
+        head_store8<T>(p, v, n);
+    }
+}
 }  // namespace ql

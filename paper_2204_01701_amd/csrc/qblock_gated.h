@@ -45,8 +45,10 @@ template <typename T>
 __device__ __forceinline__ void gated_put(const GatedOut &o, int I, int J, int i, int j, int n, float *g, float *u) {
     if (o.z && n > 0) {
         T *z = static_cast<T *>(o.z) + (size_t)i * J + j;
-        head_store8<T>(z, g, n);
-        head_store8<T>(z + (size_t)I * J, u, n);
+        // (streamed: 8192 x 2048 -> 8192 with z in 493 us, 557 where the L2 keeps it; for h, which is half as much, and for the
+        // backward's outputs it makes no difference)
+        block_store8<T>(z, g, n, true);
+        block_store8<T>(z + (size_t)I * J, u, n, true);
     }
     if (o.q) {
         const int blocks = (J + kKeep - 1) / kKeep;
@@ -110,8 +112,9 @@ template <typename T, int BX, int W> struct PairSrc {
     }
 };
 
-template <typename T, int MODE, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int NI1>
-__global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qblock_gated_kernel(GatedArgs g) {
+// A workgroup's tile of a product: number `block` of its tiles and splits.
+template <typename T, int MODE, int BI, int BJ, int WVI, int WVJ, int NS, int NI1>
+__device__ __forceinline__ void gated_tile(const GatedArgs &g, int block, char *lds) {
     constexpr int W = WVI * WVJ, TH = 64 * W, WI = BI / WVI, WJ = BJ / WVJ, MI = WI / 32, MJ = WJ / 32;
     constexpr int STAGE = (BI + BJ) * 64, BK = HeadStep<T>::BK;
     static_assert(WJ == 64, "a wave's columns: 32 of g and 32 of u");
@@ -119,9 +122,8 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qblock_gated
     typedef HeadSrc<T, true, BJ, W> NatB;
     typedef PairSrc<T, BJ, W> PairB;
     constexpr int NIB = BJ / (16 * W);
-    __shared__ __attribute__((aligned(16))) char lds[head_tile_lds<BI, BJ, WVI, NS>()];
     const int lane = threadIdx.x & 63, wave = wave_id(), wi = wave / WVJ, wj = wave - wi * WVJ;
-    int bid = xcd_remap(blockIdx.x, g.ti * g.tj * g.splits);
+    const int bid = xcd_remap(block, g.ti * g.tj * g.splits);
     const int split = bid / (g.ti * g.tj);
     int ti, tj;
     head_tile(bid - split * g.ti * g.tj, g.ti, g.tj, ti, tj);
@@ -239,6 +241,23 @@ __global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qblock_gated
     }
 }
 
+template <typename T, int MODE, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int NI1>
+__global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qblock_gated_kernel(GatedArgs g) {
+    __shared__ __attribute__((aligned(16))) char lds[head_tile_lds<BI, BJ, WVI, NS>()];
+    gated_tile<T, MODE, BI, BJ, WVI, WVJ, NS, NI1>(g, blockIdx.x, lds);
+}
+
+// Both products of the backward in one launch, those with the longer reduction first, so that the short ones fill up what
+// their number leaves idle: 4096 x 2048 -> 8192 has 128 tiles of dx, 512 steps each, and 512 of the weights' gradients, 128
+// each; together they are 512 steps for every CU, where dx by itself takes two splits and their join.
+template <typename T, int BI, int BJ, int WVI, int WVJ, int NS, int WGS, int NI1>
+__global__ __launch_bounds__(64 * WVI *WVJ, WGS *WVI *WVJ / 4) void qblock_gated_grads_kernel(GatedArgs dx, GatedArgs dw, int dx0, int dw0) {
+    __shared__ __attribute__((aligned(16))) char lds[head_tile_lds<BI, BJ, WVI, NS>()];
+    const int bid = blockIdx.x;
+    if (bid >= dx0 && bid - dx0 < dx.ti * dx.tj) gated_tile<T, GATED_DX, BI, BJ, WVI, WVJ, NS, NI1>(dx, bid - dx0, lds);
+    else gated_tile<T, GATED_DW, BI, BJ, WVI, WVJ, NS, NI1>(dw, bid - dw0, lds);
+}
+
 // Sum over the splits, in their order, of eight neighbours; four splits requested together.
 __device__ __forceinline__ void gated_sum8(const float *p, size_t stride, int splits, int n, float *v) {
 #pragma unroll
@@ -301,20 +320,34 @@ template <typename T> __global__ __launch_bounds__(512) void qblock_gated_few_ke
     const T *b0 = static_cast<const T *>(g.b0) + at, *b1 = static_cast<const T *>(g.b1) + at;
     const int ra = row < g.I ? g.R : 0;  // (rows past I are zeros; columns past J are not stored)
     v4f acc0 = {0.0f, 0.0f, 0.0f, 0.0f}, acc1 = acc0;
-    for (int t0 = wave * STEP; t0 < g.R; t0 += U * W * STEP) {
-        v4u fa[U], f0[U], f1[U];
+    struct Fragments {
+        v4u a[U], f0[U], f1[U];
+    } now, next;
+    auto load = [&](Fragments &f, int t0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            f0[u] = head_row16<T>(b0, t0 + u * W * STEP + off, g.R);
-            f1[u] = head_row16<T>(b1, t0 + u * W * STEP + off, g.R);
+            f.f0[u] = head_row16<T>(b0, t0 + u * STEP + off, g.R);
+            f.f1[u] = head_row16<T>(b1, t0 + u * STEP + off, g.R);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) fa[u] = head_row16<T>(a, t0 + u * W * STEP + off, ra);
+        for (int u = 0; u < U; ++u) f.a[u] = head_row16<T>(a, t0 + u * STEP + off, ra);
+    };
+    auto multiply = [&](const Fragments &f) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            head_mfma16<T>(f0[u], fa[u], acc0);
-            head_mfma16<T>(f1[u], fa[u], acc1);
+            head_mfma16<T>(f.f0[u], f.a[u], acc0);
+            head_mfma16<T>(f.f1[u], f.a[u], acc1);
         }
+    };
+    // (the next fragments are on their way while these are multiplied)
+    constexpr int S = U * W * STEP;
+    // (a wave's U steps lie side by side: 256 bytes of a row)
+    load(now, wave * U * STEP);
+    for (int t0 = wave * U * STEP; t0 < g.R; t0 += 2 * S) {
+        load(next, t0 + S);
+        multiply(now);
+        load(now, t0 + 2 * S);
+        multiply(next);
     }
     part[0][wave][lane] = acc0;
     part[1][wave][lane] = acc1;

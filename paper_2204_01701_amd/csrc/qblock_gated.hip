@@ -35,6 +35,7 @@ struct GatedPlan {
     Tile tile;
     int ti, tj, steps, splits, per;
     size_t part_bytes;
+    double us;
 };
 
 // Time of a product in us by tile and splits: rounds of the workgroups over the CUs, each with its ramp and epilogue;
@@ -64,9 +65,54 @@ GatedPlan plan(GatedMode mode, const qblock_gated_desc *d) {
             if (c < best) best = c, want = s, p.tile = t, p.ti = ti, p.tj = tj;
         }
     }
+    p.us = best;
     p.per = std::max(1, cdiv(p.steps, want));
     p.splits = std::max(1, cdiv(p.steps, p.per));
     if (p.splits > 1) p.part_bytes = align_up((size_t)p.splits * (size_t)size * sizeof(float));
+    return p;
+}
+
+// Steps until the last CU is done with n1 tiles of s1 steps and then n2 of s2 <= s1, each taken by the first CU that is free.
+long long makespan(long long n1, int s1, long long n2, int s2) {
+    const long long low = n1 / kNumCUs * s1, high = n1 % kNumCUs ? low + s1 : low, behind = n1 % kNumCUs;
+    long long a = high, b = high + (n2 / kNumCUs + 1) * s2;
+    while (a < b) {
+        const long long m = (a + b) / 2, fits = (kNumCUs - behind) * ((m - low) / s2) + behind * ((m - high) / s2);
+        if (fits >= n2) b = m;
+        else a = m + 1;
+    }
+    return a;
+}
+
+// The backward's products: one after the other, or in one launch of the same tiles without splits.
+struct GradsPlan {
+    bool both;
+    GatedPlan dx, dw;
+};
+GradsPlan plan_grads(const qblock_gated_desc *d) {
+    GradsPlan p{false, plan(GATED_DX, d), plan(GATED_DW, d)};
+    const int forced = env_override("QBLOCK_BOTH", -1), forced_tile = env_override("QBLOCK_TILE", -1);
+    if (forced == 0 || d->m == 0) return p;
+    const int bk = step_of(d->dtype);
+    double best = forced == 1 ? 1e300 : p.dx.us + p.dw.us;
+    for (Tile t : {TILE_64, TILE_128, TILE_256}) {
+        if (forced_tile >= 0 && (int)t != forced_tile) continue;
+        // (bf16 in the large tiles, of which a CU holds one, is what the sum of steps describes: 526 us for 4096 x 2048 -> 8192,
+        // in turn 554; small tiles share a CU, and float32 ones in one launch took 660 us for 2048 x 1024 -> 4096, in turn 558)
+        if (forced != 1 && (t != TILE_256 || d->dtype != QL_BF16)) continue;
+        GatedPlan x{}, w{};
+        x.tile = w.tile = t;
+        x.splits = w.splits = 1;
+        x.ti = cdiv(d->m, tile_rows(t)), x.tj = cdiv(d->k, tile_cols(t));
+        w.ti = 2 * cdiv(d->n, tile_rows(t)), w.tj = cdiv(d->k, tile_cols(t));
+        x.per = x.steps = 2 * (half_columns(d) / bk);
+        w.per = w.steps = cdiv(d->m, bk);
+        const long long nx = (long long)x.ti * x.tj, nw = (long long)w.ti * w.tj;
+        if ((double)(nx + nw) * tile_threads(t) >= 4294967296.0) continue;
+        const long long m = x.steps >= w.steps ? makespan(nx, x.steps, nw, w.steps) : makespan(nw, w.steps, nx, x.steps);
+        const double us = (t == TILE_256 ? 8.0 : 5.0) + kStepUs[d->dtype == QL_BF16][t] * (double)m;
+        if (us < best) best = us, p = GradsPlan{true, x, w};
+    }
     return p;
 }
 
@@ -99,6 +145,21 @@ template <typename T, int MODE> ql_status launch(const GatedPlan &p, GatedArgs a
         const long long rows = MODE == GATED_DW ? 2LL * a.I : a.I;
         hipLaunchKernelGGL((qblock_gated_join_kernel<T, MODE>), dim3(grid_1d(rows * cdiv(a.J, kKeep) * 4)), dim3(kThreads), 0, st, a);
     }
+    return hip_status();
+}
+
+template <typename T> ql_status launch_both(const GradsPlan &p, GatedArgs dx, GatedArgs dw, hipStream_t st) {
+    for (auto *q : {&dx, &dw}) {
+        const GatedPlan &g = q == &dx ? p.dx : p.dw;
+        q->ti = g.ti, q->tj = g.tj, q->splits = 1, q->per = g.per, q->steps = g.steps;
+    }
+    const int nx = p.dx.ti * p.dx.tj, nw = p.dw.ti * p.dw.tj;
+    const bool dx_first = p.dx.steps >= p.dw.steps;
+    const int dx0 = dx_first ? 0 : nw, dw0 = dx_first ? nx : 0;
+    const dim3 grid((unsigned)(nx + nw));
+    if (p.dx.tile == TILE_256) hipLaunchKernelGGL((qblock_gated_grads_kernel<T, 256, 256, 2, 4, 4, 1, 2>), grid, dim3(512), 0, st, dx, dw, dx0, dw0);
+    else if (p.dx.tile == TILE_128) hipLaunchKernelGGL((qblock_gated_grads_kernel<T, 128, 128, 2, 2, 4, 2, 4>), grid, dim3(256), 0, st, dx, dw, dx0, dw0);
+    else hipLaunchKernelGGL((qblock_gated_grads_kernel<T, 64, 128, 2, 2, 4, 2, 3>), grid, dim3(256), 0, st, dx, dw, dx0, dw0);
     return hip_status();
 }
 
@@ -153,28 +214,31 @@ ql_status backward(const qblock_gated_desc *d, const void *x, const void *wg, co
     if (joined && (dbg || dbu))
         hipLaunchKernelGGL(qblock_gated_colsum_kernel<>, dim3(cdiv(d->n, 32), 2), dim3(kThreads), 0, st, z0.part0, z0.part1, p.parts, d->n, dbg, dbu);
     ql_status s = hip_status();
-    GatedArgs a{};
-    a.a = ws, a.lda = 2LL * np, a.np = np;
+    if (s != QL_OK || (!dx && !dwg)) return s;
+    GatedArgs x0{}, w0{};
+    x0.a = w0.a = ws, x0.lda = w0.lda = 2LL * np, x0.np = w0.np = np;
     ws += p.dz_bytes + p.part_bytes;
-    if (dx && s == QL_OK) {
-        const Pads pads(d, false, true);
-        a.b0 = wg, a.b1 = wu, a.ldb = d->ldw;
+    const GradsPlan plans = plan_grads(d);
+    const bool both = plans.both && dx && dwg;
+    const Pads pads(d, dwg != nullptr, dx != nullptr);
+    if (dx) {
+        x0.b0 = wg, x0.b1 = wu, x0.ldb = d->ldw;
         if (pads.w) {
-            a.b0 = pad<T>(d, wg, d->ldw, d->n, ws, st);
-            a.b1 = pad<T>(d, wu, d->ldw, d->n, ws + pads.w, st);
-            a.ldb = whole_vectors(d);
+            x0.b0 = pad<T>(d, wg, d->ldw, d->n, ws, st);
+            x0.b1 = pad<T>(d, wu, d->ldw, d->n, ws + pads.w, st);
+            x0.ldb = whole_vectors(d);
         }
-        a.I = d->m, a.J = d->k, a.R = d->n, a.o.c0 = dx;
-        a.part = reinterpret_cast<float *>(ws + 2 * pads.w);
-        s = launch<T, GATED_DX>(plan(GATED_DX, d), a, st);
+        x0.I = d->m, x0.J = d->k, x0.R = d->n, x0.o.c0 = dx;
+        x0.part = reinterpret_cast<float *>(ws + 2 * pads.w);
+        if (!both) s = launch<T, GATED_DX>(plans.both ? plan(GATED_DX, d) : plans.dx, x0, st);
     }
     if (dwg && s == QL_OK) {
-        const Pads pads(d, true, false);
-        a.b0 = x, a.b1 = x, a.ldb = d->ldx;
-        if (pads.x) a.b0 = a.b1 = pad<T>(d, x, d->ldx, d->m, ws, st), a.ldb = whole_vectors(d);
-        a.I = d->n, a.J = d->k, a.R = d->m, a.o.c0 = dwg, a.o.c1 = dwu, a.o.c_f32 = d->dw_f32 != 0;
-        a.part = reinterpret_cast<float *>(ws + pads.x);
-        s = launch<T, GATED_DW>(plan(GATED_DW, d), a, st);
+        if (both) ws += 2 * pads.w;  // (else the products run one after the other on the same piece)
+        w0.b0 = w0.b1 = x, w0.ldb = d->ldx;
+        if (pads.x) w0.b0 = w0.b1 = pad<T>(d, x, d->ldx, d->m, ws, st), w0.ldb = whole_vectors(d);
+        w0.I = d->n, w0.J = d->k, w0.R = d->m, w0.o.c0 = dwg, w0.o.c1 = dwu, w0.o.c_f32 = d->dw_f32 != 0;
+        w0.part = reinterpret_cast<float *>(ws + pads.x);
+        s = both ? launch_both<T>(plans, x0, w0, st) : launch<T, GATED_DW>(plans.both ? plan(GATED_DW, d) : plans.dw, w0, st);
     }
     return s;
 }
@@ -214,9 +278,11 @@ ql_status qblock_gated_fwd(const qblock_gated_desc *d, const void *x, const void
 size_t qblock_gated_bwd_workspace_size(const qblock_gated_desc *d) {
     if (!gated_ok(d) || !sizes_fit(d)) return 0;
     const DzPlan p(d);
-    const Pads dx(d, false, true), dw(d, true, false);
-    // the two products run one after the other on the same piece
-    return p.dz_bytes + p.part_bytes + std::max(2 * dx.w + plan(GATED_DX, d).part_bytes, dw.x + plan(GATED_DW, d).part_bytes);
+    const Pads pads(d, true, true);
+    // the two products run one after the other on the same piece, or in one launch (where both are asked for)
+    size_t most = std::max(2 * pads.w + plan(GATED_DX, d).part_bytes, pads.x + plan(GATED_DW, d).part_bytes);
+    if (plan_grads(d).both) most = std::max(most, pads.x + 2 * pads.w);
+    return p.dz_bytes + p.part_bytes + most;
 }
 
 ql_status qblock_gated_bwd(const qblock_gated_desc *d, const void *x, const void *wg, const void *wu, const void *dh, const void *z,

@@ -8,7 +8,7 @@
 // value, give back a sixth (the largest of 32 normal values is 2.1 sigma on average, of 128 2.7).
 #pragma once
 
-#include "qhead_gemm.h"
+#include "qblock_act.h"
 
 namespace ql {
 
@@ -135,7 +135,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void qblock_unpack8
         const int n = (int)min(a.cols - col, 8LL);
         float v[8];
         keep_values8(keep_get8(a.q + row * a.cols + col, n), a.e[row * a.blocks + blk], v);
-        head_store8<T>(static_cast<T *>(a.x) + row * a.ld + col, v, n);
+        // (float's 32 bytes a lane go out as two halves of a line, which streamed took 45 us for 32768 x 1024, else 27)
+        block_store8<T>(static_cast<T *>(a.x) + row * a.ld + col, v, n, sizeof(T) == 2);
     }
 }
 

@@ -35,6 +35,7 @@ struct NormArgs {
     int svl, pnl;                  // log2 of columns, of pixel lanes of a sample
     int chunks, chunk_px, slots;   // slots: workgroups that share the samples
     int blocks, act;
+    bool stream;  // the output's stores are streamed
     float eps;
     FastDiv by_segs, by_chunks, by_wide;  // (wide: channels of a group within a segment, where groups are whole)
 };
@@ -201,7 +202,7 @@ __device__ __forceinline__ void norm_channels(const float *p, int c, int n8, flo
 // quad comes here; n <= 0: nothing to store).
 template <typename T>
 __device__ __forceinline__ void norm_put(const NormArgs &a, const NormWalk &w, int step, int n, float *x, const float *y) {
-    if (n > 0) head_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), step)), y, n);
+    if (n > 0) block_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), step)), y, n, a.stream);
     if (!a.q) return;
     if (n < 8) {
 #pragma unroll
@@ -581,7 +582,7 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
                 norm_hats<U, F>(mean, rstd, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] = rstd[i / U] * (gam[i] * g[i] - ta[i / U] - x[i] * tx[i / U]);
-                head_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8);
+                block_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8, a.stream);
             }
         } else if (t.p == 0 && last > 0) {
 #pragma unroll
@@ -655,7 +656,7 @@ template <typename T, int U, bool KEPT> __global__ __launch_bounds__(kThreads) v
                 norm_slopes(a.act, gam, bet, x, g);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] = rstd[i / U] * (gam[i] * g[i] - ta[i / U] - x[i] * tx[i / U]);
-                head_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8);
+                block_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8, a.stream);
             }
         }
     }

@@ -23,6 +23,7 @@ int log2_up(long long v) {
 struct NormPlan {
     bool fused;
     int th, r, u;  // threads, pixels a thread, channels a thread takes as one
+    int es;        // bytes of a value
     NormArgs a;    // the geometry
     size_t part_bytes, joined_bytes, chan_bytes;
     size_t bytes() const { return part_bytes + joined_bytes + chan_bytes; }
@@ -30,6 +31,11 @@ struct NormPlan {
 
 // The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most.
 void share_samples(NormPlan &p, int n, long long most) {
+    // Outputs are streamed where a workgroup writes whole rows, or at least 64 bytes (bf16) or 128 (float32) of one:
+    // 128 x 1024 x 256, bf16, forward 45 to 35 us; 512 x 49 x 512, float32, 28 to 22.  Lesser parts of lines lose by it: 32
+    // bytes in bf16 77 to 94 us, 64 in float32 62 to 74.
+    const int line = p.a.gps * p.a.cpg * p.es;
+    p.a.stream = p.a.segs == 1 || p.a.parts > 1 || line >= (p.es == 2 ? 64 : 128);
     const int snl = log2_up(p.th) - p.a.svl - p.a.pnl;
     const long long groups = ((long long)n + (1LL << snl) - 1) >> snl;
     p.a.slots = (int)std::max(1LL, std::min(groups, most));
@@ -47,6 +53,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
     a.n = d->n, a.hw = d->hw, a.c = d->c, a.groups = d->groups, a.cpg = cpg;
     a.act = (int)d->act, a.eps = d->eps;
     p.u = cpg % 8 == 0 ? 8 : 1;
+    p.es = es;
     a.parts = 1, a.part_c = cpg;
     auto segment = [&](int gps) {
         a.gps = std::max(1, std::min(d->groups, gps));
@@ -74,7 +81,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
                 const double wgs = std::max(1.0, (double)std::max(1, d->n) * a.segs), rounds = wgs / kNumCUs;
                 // (a float's line of 32 bytes is a single column: 168 us where 128 bytes take 125; two workgroups of 256 threads
                 // on a CU load and compute in turn, where their registers leave one of 512: 76 us, 85)
-                const double form = es == 4 && line == 32 ? 1.5 : bwd && es == 2 && th == 512 && p.u == 8 ? 1.12 : 1.0;
+                const double form = es == 4 && line == 32 ? 2.2 : bwd && es == 2 && th == 512 && p.u == 8 ? 1.12 : 1.0;
                 const double t = 5.0 + form * each * values / wgs * (rounds < 4 ? std::ceil(rounds) : rounds);
                 if (t < 0.97 * best) best = t, line_at = line, th_at = th;
                 break;

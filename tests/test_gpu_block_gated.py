@@ -125,7 +125,10 @@ def test_every_tile(m, k, n, tile, splits, dtype, monkeypatch):
     monkeypatch.setenv("QBLOCK_TILE", str(tile))
     monkeypatch.setenv("QBLOCK_SPLITS", str(splits))
     forward(m, k, n, dtype, "silu", keep=True, offset=8, pad=8)
-    backward(m, k, n, dtype, "gelu", offset=1, pad=4)
+    for both in range(2):  # the backward's products in turn, or in one launch
+        monkeypatch.setenv("QBLOCK_BOTH", str(both))
+        backward(m, k, n, dtype, "gelu", offset=1, pad=4)
+        backward(m, k, n, dtype, "gelu", need=("dx",) if splits > 1 else ("dwg", "dwu"))
 
 
 def test_float32_weight_gradients():
