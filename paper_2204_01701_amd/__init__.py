@@ -881,6 +881,11 @@ def _block_call(name, query, desc, ptrs, index, workspace, stream):
         return _head_call(name, query, desc, ptrs, index, workspace, stream)
 
 
+def _int(v):
+    """A size as the descriptors hold it: what an int does not hold as one that the library refuses."""
+    return v if v < 2**31 else 2**31 - 1
+
+
 def _block_launch(name, desc, ptrs, device, query=None):
     """The entry point on the pointers of operands that the caller has checked, on the current stream of their device.
 
@@ -918,7 +923,7 @@ def qblock_pack8(x, q, e, stream=None):
     i, dt, code = _head_first(x, "x")
     rows, cols = x.shape
     p, ld = _head_rows("x", x, (rows, cols), dt, i)
-    _block_call("qblock_pack8", None, BlockKeepDesc(rows, cols, ld, code), (p, *_kept_dense(i, q, e, (rows,), cols)), i, None, stream)
+    _block_call("qblock_pack8", None, BlockKeepDesc(rows, _int(cols), ld, code), (p, *_kept_dense(i, q, e, (rows,), cols)), i, None, stream)
 
 
 def qblock_unpack8(q, e, x, stream=None):
@@ -926,7 +931,7 @@ def qblock_unpack8(q, e, x, stream=None):
     i, dt, code = _head_first(x, "x")
     rows, cols = x.shape
     p, ld = _head_rows("x", x, (rows, cols), dt, i)
-    _block_call("qblock_unpack8", None, BlockKeepDesc(rows, cols, ld, code), (*_kept_dense(i, q, e, (rows,), cols), p), i, None, stream)
+    _block_call("qblock_unpack8", None, BlockKeepDesc(rows, _int(cols), ld, code), (*_kept_dense(i, q, e, (rows,), cols), p), i, None, stream)
 
 
 def _block_norm(t, what, groups):
@@ -956,7 +961,7 @@ def qblock_norm_fwd(x, groups, gamma, beta, y, mean=None, rstd=None, q=None, e=N
     f32 = _float32()
     ptrs = _head_dense(i, ("x", x, x.shape, dt), ("gamma", gamma, (c,), f32), ("beta", beta, (c,), f32), ("y", y, x.shape, dt),
                        ("mean", mean, (n, groups), f32), ("rstd", rstd, (n, groups), f32))
-    _block_call("qblock_norm_fwd", "qblock_norm_fwd_workspace_size", BlockNormDesc(n, hw, c, groups, code, _head_act(act), eps),
+    _block_call("qblock_norm_fwd", "qblock_norm_fwd_workspace_size", BlockNormDesc(_int(n), _int(hw), _int(c), groups, code, _head_act(act), eps),
                 (*ptrs, *_kept_rows(i, q, e, x.shape)), i, workspace, stream)
 
 
@@ -982,7 +987,7 @@ def qblock_norm_bwd(dy, x, groups, gamma, beta, mean, rstd, dx=None, dgamma=None
     ptrs = _head_dense(i, ("dy", dy, dy.shape, dt), ("x", x, dy.shape, dt))
     rest = _head_dense(i, ("gamma", gamma, (c,), f32), ("beta", beta, (c,), f32), ("mean", mean, (n, groups), f32),
                        ("rstd", rstd, (n, groups), f32), ("dx", dx, dy.shape, dt), ("dgamma", dgamma, (c,), f32), ("dbeta", dbeta, (c,), f32))
-    _block_call("qblock_norm_bwd", "qblock_norm_bwd_workspace_size", BlockNormDesc(n, hw, c, groups, code, _head_act(act), 1.0),
+    _block_call("qblock_norm_bwd", "qblock_norm_bwd_workspace_size", BlockNormDesc(_int(n), _int(hw), _int(c), groups, code, _head_act(act), 1.0),
                 (*ptrs, *_kept_rows(i, q, e, dy.shape), *rest), i, workspace, stream)
 
 
@@ -1009,7 +1014,7 @@ def qblock_gated_fwd(x, wg, wu, bg, bu, h, z=None, q=None, e=None, act="silu", w
     f32 = _float32()
     pbg, pbu, pz = _head_dense(i, ("bg", bg, (n,), f32), ("bu", bu, (n,), f32), ("z", z, (2, m, n), dt))
     _block_call("qblock_gated_fwd", "qblock_gated_fwd_workspace_size",
-                BlockGatedDesc(m, k, n, ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), 0),
+                BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), 0),
                 (px, pg, pu, pbg, pbu, ph, pz, *_kept_dense(i, q, e, (2, m), n)), i, workspace, stream)
 
 
@@ -1037,5 +1042,5 @@ def qblock_gated_bwd(x, wg, wu, dh, z=None, dx=None, dwg=None, dwu=None, dbg=Non
     pz, = _head_dense(i, ("z", z, (2, m, n), dt))
     rest = _head_dense(i, ("dx", dx, (m, k), dt), ("dwg", dwg, (n, k), dw), ("dwu", dwu, (n, k), dw), ("dbg", dbg, (n,), f32), ("dbu", dbu, (n,), f32))
     _block_call("qblock_gated_bwd", "qblock_gated_bwd_workspace_size",
-                BlockGatedDesc(m, k, n, ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), dw_f32),
+                BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), dw_f32),
                 (px, pg, pu, pdh, pz, *_kept_dense(i, q, e, (2, m), n), *rest), i, workspace, stream)

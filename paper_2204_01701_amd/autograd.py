@@ -59,7 +59,7 @@ from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL
                qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex,
                qhead_distill_bwd, qhead_distill_fwd, qhead_linear_bwd, qhead_linear_fwd, qhead_logprobs_bwd,
                qhead_logprobs_fwd, BLOCK_KEEP, BlockGatedDesc, BlockKeepDesc, BlockNormDesc, HeadLinearDesc,
-               _block_launch, _head_act, _unaligned)
+               _block_launch, _head_act, _int, _unaligned)
 
 __all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction", "linear_act", "token_logprobs",
            "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction", "group_norm_act",
@@ -136,7 +136,7 @@ def _pack(t):
     q = torch.empty((rows, cols), device=t.device, dtype=torch.int8)
     e = torch.empty((rows, -(-cols // BLOCK_KEEP)), device=t.device, dtype=torch.uint8)
     ld = t.stride(0) if t.dim() == 2 and rows > 1 else cols
-    _block_launch("qblock_pack8", BlockKeepDesc(rows, cols, ld, _qdtype(t)), (t.data_ptr(), q.data_ptr(), e.data_ptr()), t.device)
+    _block_launch("qblock_pack8", BlockKeepDesc(rows, _int(cols), ld, _qdtype(t)), (t.data_ptr(), q.data_ptr(), e.data_ptr()), t.device)
     return q, e
 
 
@@ -579,7 +579,7 @@ class GroupNormActFunction(torch.autograd.Function):
         xn = _dense_image(x)
         gamma, beta = _f32(weight), _f32(bias)
         y = torch.empty_like(xn)
-        desc = BlockNormDesc(n, hw, c, groups, _qdtype(x), _head_act(act), eps)
+        desc = BlockNormDesc(_int(n), _int(hw), _int(c), groups, _qdtype(x), _head_act(act), eps)
         stats = q = e = mean = rstd = None
         train = train and any(ctx.needs_input_grad[:3])
         kept = train and _kept(checkpoint)
@@ -663,7 +663,7 @@ class GatedLinearFunction(torch.autograd.Function):
         bgf, buf = _f32(bg), _f32(bu)
         ldx, ldw = (xm.stride(0) if m > 1 else k), (wgm.stride(0) if n > 1 else k)
         px, pg, pu = xm.data_ptr(), wgm.data_ptr(), wum.data_ptr()
-        desc = BlockGatedDesc(m, k, n, ldx, ldw, n, _qdtype(x), _head_act(act), _unaligned(px, pg, pu), 0)
+        desc = BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, n, _qdtype(x), _head_act(act), _unaligned(px, pg, pu), 0)
         _block_launch("qblock_gated_fwd", desc, (px, pg, pu, _ptr(bgf), _ptr(buf), h.data_ptr(), _ptr(z), _ptr(q), _ptr(e)), dev,
                       "qblock_gated_fwd_workspace_size")
         if train:

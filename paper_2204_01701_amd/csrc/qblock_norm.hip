@@ -12,7 +12,9 @@ namespace {
 bool norm_ok(const qblock_norm_desc *d) {
     return d && d->n >= 0 && d->hw > 0 && d->c > 0 && d->groups > 0 && d->c % d->groups == 0 && float_type(d->dtype) && known_act(d->act);
 }
-bool sizes_fit(const qblock_norm_desc *d) { return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20; }
+bool sizes_fit(const qblock_norm_desc *d) {
+    return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20 && (double)d->n * d->hw * d->c < 140737488355328.0;
+}
 
 int log2_up(long long v) {
     int b = 0;

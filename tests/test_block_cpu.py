@@ -99,7 +99,8 @@ def norm_calls(L, d, eps_matters=True):
 @pytest.mark.parametrize("bad,want", [(dict(n=-1), EINVAL), (dict(hw=0), EINVAL), (dict(c=0), EINVAL), (dict(groups=0), EINVAL),
                                       (dict(groups=5), EINVAL), (dict(dtype=7), EINVAL), (dict(act=5), EINVAL), (dict(act=-1), EINVAL),
                                       (dict(n=2**31 - 2), EUNSUPPORTED), (dict(hw=2**31 - 2), EUNSUPPORTED),
-                                      (dict(c=(1 << 20) + 2), EUNSUPPORTED)])
+                                      (dict(c=(1 << 20) + 2), EUNSUPPORTED),
+                                      (dict(n=2**30, hw=2**20), EUNSUPPORTED)])
 def test_norm_refuses_descriptors(L, bad, want):
     for status in norm_calls(L, norm(**bad), False):
         assert status == want
