@@ -27,8 +27,8 @@ struct NormArgs {
     float *mean, *rstd;  // forward: written; backward: read
     int8_t *q;           // forward: written; backward: read in x's place
     uint8_t *e;
-    float2 *part;  // [sample][slice][group]: (mean, sum of squares about it), or the sums of t and t xh
-    float2 *avg;   // [sample][group]: averages of t and t xh
+    float2 *part;  // [sample][slice][group]: (mean, sum of squares about it), or sigma_1 and sigma_2
+    float2 *avg;   // [sample][group]: sigma_1 / N and sigma_2 / N
     float2 *chan;  // [slot * chunks + chunk][c]: sums of dz and dz xh
     int n, hw, c, groups, cpg;
     int gps, parts, part_c, segs;  // groups of a segment; parts of a group, their channels; segments
@@ -125,7 +125,7 @@ struct NormWalk {
     }
 };
 
-// Thread's place.  U: channels that surely share a group (8 where cpg is a multiple of 8, else 1).
+// Thread's place.  U: channels that surely share a group, the largest of 8, 4, 2 and 1 that divides cpg.
 template <int U, int TH> struct NormThread {
     static constexpr int F = 8 / U;  // groups' shares a thread tells apart
     int v, p, sn, col, n8, snl;
@@ -217,7 +217,7 @@ __device__ __forceinline__ void norm_put(const NormArgs &a, const NormWalk &w, i
 
 // Waves a SIMD that the registers are to leave room for: two workgroups of 512 on a CU where the values held allow it, so that
 // one loads while another computes.
-template <typename T, int R, int U> constexpr int norm_waves() { return R * (int)sizeof(T) <= 32 && U == 8 ? 4 : 2; }
+template <typename T, int R, int U> constexpr int norm_waves() { return R * (int)sizeof(T) <= 32 && U >= 4 ? 4 : 2; }
 
 // Forward.  FUSED: a sample's segment in registers (R pixels a thread), read once.  Else the statistics of a
 // chunk: those of its first R pixels a thread in two passes; the rest adds sums of differences, and of their
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(TH, (norm_waves<T, R, U>())) void qblock_norm_fwd_k
 }
 
 // Between the two launches over the pixels: the slices of a group of a sample joined, a lane a slice (64 lanes at most), to
-// its mean and rstd (STATS), or to the averages of t and t xh.  By itself: in every workgroup of the second launch it
+// its mean and rstd (STATS), or to the backward's averages.  By itself: in every workgroup of the second launch it
 // took up to half of the launch.
 template <bool STATS> __global__ __launch_bounds__(kThreads) void qblock_norm_join_kernel(NormArgs a) {
     const int slices = a.chunks * a.parts, lanes = slices > 1 ? 1 << min(6, 32 - __clz(slices - 1)) : 1;
@@ -486,35 +486,37 @@ template <typename T, int U> struct NormPair<T, U, true> {
     }
 };
 
-// x -> xh of eight neighbours; dy -> dz.
-template <int U, int F> __device__ __forceinline__ void norm_hats(const float (&mean)[F], const float (&rstd)[F], float *x) {
+// With d = x - mean and A = gamma rstd: z = A d + beta, and in the sums over a group sigma_1 = sum A dz, sigma_2 = sum A dz d,
+//     dx = A dz - sigma_1 / N - d rstd^2 sigma_2 / N,
+// which takes three instructions a value less than xh and t do.
+
+// x -> d of eight neighbours; dy -> dz.
+template <int U, int F> __device__ __forceinline__ void norm_differences(const float (&mean)[F], float *x) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (x[i] - mean[i / U]) * rstd[i / U];
+    for (int i = 0; i < 8; ++i) x[i] -= mean[i / U];
 }
-__device__ __forceinline__ void norm_slopes(int act, const float *gam, const float *bet, const float *x, float *g) {
+__device__ __forceinline__ void norm_slopes(int act, const float *scale, const float *bet, const float *d, float *g) {
     if (act != HEAD_NONE) {
         float z[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = x[i] * gam[i] + bet[i];
+        for (int i = 0; i < 8; ++i) z[i] = d[i] * scale[i] + bet[i];
         block_slopes<4>(act, z, g);  // (by fours: fewer registers at a time)
         block_slopes<4>(act, z + 4, g + 4);
     }
 }
-
 // Backward.  FUSED: a sample's segment of dy and x in registers, read once, and dx.  Else the sums of a chunk.
 // Either way the channels' sums over the workgroup's samples and pixels go to a.chan.
 template <typename T, int R, int U, bool FUSED, bool KEPT, int TH>
-__global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(TH, FUSED || U < 4 ? 2 : 4) void qblock_norm_bwd_kernel(NormArgs a) {
     constexpr int F = 8 / U;
     __shared__ float red[2 * TH * F], sum[2 * TH * F];
     __shared__ v4f chan[4][TH];  // (each thread's own: its channels' sums over the samples, kept out of its registers)
     const NormSeg s(a);
     const NormThread<U, TH> t(a, s);
     const int c = s.c0 + t.col;
-    float gam[8], bet[8];
+    float bet[8];
 #pragma unroll
     for (int h = 0; h < 4; ++h) chan[h][threadIdx.x] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    norm_channels(a.gamma, c, t.n8, 1.0f, gam);
     norm_channels(a.beta, c, t.n8, 0.0f, bet);
     for (long long ng = s.slot; (ng << t.snl) < a.n; ng += a.slots) {
         const long long sample = (ng << t.snl) + t.sn;
@@ -528,6 +530,13 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
             mean[f] = last ? a.mean[at] : 0.0f;
             rstd[f] = last ? a.rstd[at] : 0.0f;
         }
+        float scale[8];
+        norm_channels(a.gamma, c, t.n8, 1.0f, scale);
+        auto times_rstd = [&] {  // (behind the loads, which it would wait in front of)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) scale[i] *= rstd[i / U];
+        };
+        if (!FUSED) times_rstd();
         NormPair<T, U, KEPT> raw[R];
         float dz[FUSED ? R : 1][8];  // (the slopes cost as much as all else: once, where the values stay)
         float s1[8] = {}, s2[8] = {};
@@ -535,6 +544,7 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 if (px + (r << a.pnl) < last) raw[r].load(a, w, r, U == 8 ? 8 : t.n8, room);
+            if (FUSED) times_rstd();
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if (px + (r << a.pnl) >= last) continue;
@@ -542,8 +552,8 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
                 float *g = dz[FUSED ? r : 0], x[8];
                 raw[r].gradient(g);
                 raw[r].input(w, x);
-                norm_hats<U, F>(mean, rstd, x);
-                norm_slopes(a.act, gam, bet, x, g);
+                norm_differences<U, F>(mean, x);
+                norm_slopes(a.act, scale, bet, x, g);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s1[i] += g[i], s2[i] += g[i] * x[i];
                 if constexpr (FUSED) raw[r].forget();
@@ -553,8 +563,9 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
         float two[2][F] = {};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            two[0][i / U] += gam[i] * s1[i];
-            two[1][i / U] += gam[i] * s2[i];
+            two[0][i / U] += scale[i] * s1[i];
+            two[1][i / U] += scale[i] * s2[i];
+            s2[i] *= rstd[i / U];
         }
         if (a.chan) {
 #pragma unroll
@@ -571,7 +582,7 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 ta[f] = sum[t.sn * s.ng + t.gi[f]] * inv;
-                tx[f] = sum[TH * F + t.sn * s.ng + t.gi[f]] * inv;
+                tx[f] = rstd[f] * (rstd[f] * (sum[TH * F + t.sn * s.ng + t.gi[f]] * inv));
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -579,9 +590,9 @@ __global__ __launch_bounds__(TH, FUSED || U == 1 ? 2 : 4) void qblock_norm_bwd_k
                 if (at >= last) continue;
                 float *g = dz[r], x[8];
                 raw[r].input(w, x);
-                norm_hats<U, F>(mean, rstd, x);
+                norm_differences<U, F>(mean, x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = rstd[i / U] * (gam[i] * g[i] - ta[i / U] - x[i] * tx[i / U]);
+                for (int i = 0; i < 8; ++i) g[i] = scale[i] * g[i] - (ta[i / U] + x[i] * tx[i / U]);
                 block_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8, a.stream);
             }
         } else if (t.p == 0 && last > 0) {
@@ -623,11 +634,11 @@ template <typename T, int U, bool KEPT> __global__ __launch_bounds__(kThreads) v
     const NormSeg s(a);
     const NormThread<U, kThreads> t(a, s);
     const int c = s.c0 + t.col;
-    float gam[8], bet[8];
-    norm_channels(a.gamma, c, t.n8, 1.0f, gam);
+    float bet[8];
     norm_channels(a.beta, c, t.n8, 0.0f, bet);
     for (long long sample = s.slot; sample < a.n; sample += a.slots) {
-        float mean[F], rstd[F], ta[F], tx[F];
+        float mean[F], rstd[F], ta[F], tx[F], scale[8];
+        norm_channels(a.gamma, c, t.n8, 1.0f, scale);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
             const long long at = sample * a.groups + s.g0 + t.gi[f];
@@ -635,8 +646,10 @@ template <typename T, int U, bool KEPT> __global__ __launch_bounds__(kThreads) v
             rstd[f] = a.rstd[at];
             const float2 x = a.avg[at];
             ta[f] = x.x;
-            tx[f] = x.y;
+            tx[f] = rstd[f] * (rstd[f] * x.y);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) scale[i] *= rstd[i / U];
         if (t.n8 <= 0) continue;
         const bool room = NormSeg::room(a, sample * a.hw + s.p1);
         NormWalk w(a, s.c0, sample * a.hw + s.p0, (uint32_t)t.p, t.col);
@@ -652,10 +665,10 @@ template <typename T, int U, bool KEPT> __global__ __launch_bounds__(kThreads) v
                 float g[8], x[8];
                 raw[r].gradient(g);
                 raw[r].input(w, x);
-                norm_hats<U, F>(mean, rstd, x);
-                norm_slopes(a.act, gam, bet, x, g);
+                norm_differences<U, F>(mean, x);
+                norm_slopes(a.act, scale, bet, x, g);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = rstd[i / U] * (gam[i] * g[i] - ta[i / U] - x[i] * tx[i / U]);
+                for (int i = 0; i < 8; ++i) g[i] = scale[i] * g[i] - (ta[i / U] + x[i] * tx[i / U]);
                 block_store8<T>(reinterpret_cast<T *>(w.ptr<T>(static_cast<char *>(a.out), r)), g, U == 8 ? 8 : t.n8, a.stream);
             }
         }

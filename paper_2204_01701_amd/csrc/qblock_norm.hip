@@ -1,8 +1,7 @@
 // qblock_norm.hip -- host side of the group normalization of include/qblock.h.
 #include <cmath>
 
-#include "qblock_host.h"
-#include "qblock_norm.h"
+#include "qblock_norm_host.h"
 
 using namespace ql;
 using namespace ql::host;
@@ -15,21 +14,6 @@ bool norm_ok(const qblock_norm_desc *d) {
 bool sizes_fit(const qblock_norm_desc *d) {
     return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20 && (double)d->n * d->hw * d->c < 140737488355328.0;
 }
-
-int log2_up(long long v) {
-    int b = 0;
-    while ((1LL << b) < v) ++b;
-    return b;
-}
-
-struct NormPlan {
-    bool fused;
-    int th, r, u;  // threads, pixels a thread, channels a thread takes as one
-    int es;        // bytes of a value
-    NormArgs a;    // the geometry
-    size_t part_bytes, joined_bytes, chan_bytes;
-    size_t bytes() const { return part_bytes + joined_bytes + chan_bytes; }
-};
 
 // The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most.
 void share_samples(NormPlan &p, int n, long long most) {
@@ -54,7 +38,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
     const int cpg = d->c / d->groups, es = (int)esize(d->dtype);
     a.n = d->n, a.hw = d->hw, a.c = d->c, a.groups = d->groups, a.cpg = cpg;
     a.act = (int)d->act, a.eps = d->eps;
-    p.u = cpg % 8 == 0 ? 8 : 1;
+    p.u = cpg % 8 == 0 ? 8 : cpg % 4 == 0 ? 4 : cpg % 2 == 0 ? 2 : 1;
     p.es = es;
     a.parts = 1, a.part_c = cpg;
     auto segment = [&](int gps) {
@@ -81,9 +65,8 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
                 const long long need = (d->hw + (1LL << (lth - a.svl)) - 1) >> (lth - a.svl);
                 if (need > (th == 256 ? 8 : most_r) || (need > 8 && line < 64)) continue;
                 const double wgs = std::max(1.0, (double)std::max(1, d->n) * a.segs), rounds = wgs / kNumCUs;
-                // (a float's line of 32 bytes is a single column: 168 us where 128 bytes take 125; two workgroups of 256 threads
-                // on a CU load and compute in turn, where their registers leave one of 512: 76 us, 85)
-                const double form = es == 4 && line == 32 ? 2.2 : bwd && es == 2 && th == 512 && p.u == 8 ? 1.12 : 1.0;
+                // (a float's line of 32 bytes is a single column: 134 us where 128 bytes take 125)
+                const double form = es == 4 && line == 32 ? 2.2 : 1.0;
                 const double t = 5.0 + form * each * values / wgs * (rounds < 4 ? std::ceil(rounds) : rounds);
                 if (t < 0.97 * best) best = t, line_at = line, th_at = th;
                 break;
@@ -134,48 +117,9 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
     return p;
 }
 
-template <bool STATS> void launch_join(const NormArgs &a, hipStream_t st) {
-    const int slices = a.chunks * a.parts, lanes = std::min(64, 1 << log2_up(slices));
-    hipLaunchKernelGGL((qblock_norm_join_kernel<STATS>), dim3(grid_1d((long long)a.n * a.groups * lanes)), dim3(kThreads), 0, st, a);
-}
-
 // Whether the forward's launches can write the checkpoint on the way: segments of whole blocks, whose lanes are quads.  (Else
 // a launch of its own does: the plan, and with it the order of the sums, is the same with a checkpoint and without.)
 bool emits(const NormPlan &p) { return p.a.parts == 1 && (p.a.segs == 1 || p.a.gps * p.a.cpg % kKeep == 0) && p.a.svl >= 2; }
-
-template <typename T, int U> ql_status launch_fwd(const NormPlan &p, const NormArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)a.blocks), wg((unsigned)p.th);
-    if (p.fused) {
-        if (p.th == 256 && p.r == 2) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 2, U, true, 256>), grid, wg, 0, st, a);
-        else if (p.th == 256) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, true, 256>), grid, wg, 0, st, a);
-        else if (p.r <= 8) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, true, 512>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 16, U, true, 512>), grid, wg, 0, st, a);
-    } else {
-        if (p.r == 2) hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 2, U, false, kThreads>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((qblock_norm_fwd_kernel<T, 8, U, false, kThreads>), grid, wg, 0, st, a);
-        launch_join<true>(a, st);
-        hipLaunchKernelGGL((qblock_norm_apply_kernel<T, U>), grid, wg, 0, st, a);
-    }
-    return hip_status();
-}
-
-template <typename T, int U, bool KEPT> ql_status launch_bwd(const NormPlan &p, const NormArgs &a, float *dgamma, float *dbeta, hipStream_t st) {
-    const dim3 grid((unsigned)a.blocks), wg((unsigned)p.th);
-    if (p.fused) {
-        if (p.th == 256 && p.r == 2) hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 2, U, true, KEPT, 256>), grid, wg, 0, st, a);
-        else if (p.th == 256) hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 256>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 8, U, true, KEPT, 512>), grid, wg, 0, st, a);
-    } else {
-        hipLaunchKernelGGL((qblock_norm_bwd_kernel<T, 2, U, false, KEPT, kThreads>), grid, wg, 0, st, a);
-        if (a.out) {
-            launch_join<false>(a, st);
-            hipLaunchKernelGGL((qblock_norm_dx_kernel<T, U, KEPT>), grid, wg, 0, st, a);
-        }
-    }
-    if (a.chan)
-        hipLaunchKernelGGL(qblock_norm_param_kernel<>, dim3(cdiv(a.c, 16)), dim3(1024), 0, st, a.chan, a.slots * a.chunks, a.c, dgamma, dbeta);
-    return hip_status();
-}
 
 template <int = 0> __global__ __launch_bounds__(kThreads) void qblock_zero_kernel(float *p, float *q, int n) {
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) {
@@ -220,8 +164,7 @@ ql_status qblock_norm_fwd(const qblock_norm_desc *d, const void *x, const float 
         const ql_status s = run_keep(true, d->dtype, const_cast<void *>(x), d->c, q, e, (long long)d->n * d->hw, d->c, st);
         if (s != QL_OK) return s;
     }
-    if (d->dtype == QL_BF16) return p.u == 8 ? launch_fwd<uint16_t, 8>(p, a, st) : launch_fwd<uint16_t, 1>(p, a, st);
-    return p.u == 8 ? launch_fwd<float, 8>(p, a, st) : launch_fwd<float, 1>(p, a, st);
+    return launch_norm_fwd(d->dtype, p, a, st);
 }
 
 size_t qblock_norm_bwd_workspace_size(const qblock_norm_desc *d) {
@@ -259,11 +202,11 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void 
     if (dgamma || dbeta) a.chan = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.part_bytes + p.joined_bytes);
     const bool kept = x == nullptr;
     if (kept) a.q = const_cast<int8_t *>(q), a.e = const_cast<uint8_t *>(e);
-#define QL_NORM_BWD(T)                                                                                                            \
-    (p.u == 8 ? (kept ? launch_bwd<T, 8, true>(p, a, dgamma, dbeta, st) : launch_bwd<T, 8, false>(p, a, dgamma, dbeta, st)) \
-              : (kept ? launch_bwd<T, 1, true>(p, a, dgamma, dbeta, st) : launch_bwd<T, 1, false>(p, a, dgamma, dbeta, st)))
-    return d->dtype == QL_BF16 ? QL_NORM_BWD(uint16_t) : QL_NORM_BWD(float);
-#undef QL_NORM_BWD
+    if (d->dtype == QL_BF16) launch_norm_bwd_of<uint16_t>(p, a, kept, st);
+    else launch_norm_bwd_of<float>(p, a, kept, st);
+    if (a.chan)
+        hipLaunchKernelGGL(qblock_norm_param_kernel<>, dim3(cdiv(a.c, 16)), dim3(1024), 0, st, a.chan, a.slots * a.chunks, a.c, dgamma, dbeta);
+    return hip_status();
 }
 
 }  // extern "C"
