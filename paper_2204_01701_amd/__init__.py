@@ -874,11 +874,21 @@ BLOCK_KEEP = 32  # QBLOCK_KEEP of qblock.h: neighbours that share a power of two
 
 def _block_call(name, query, desc, ptrs, index, workspace, stream):
     """_head_call with the tensors' device as the current one."""
-    import torch
+    torch = _torch()
     if torch.cuda.current_device() == index:
+        if stream is None and workspace is None:
+            return _block_launch(name, desc, ptrs, index, query)
         return _head_call(name, query, desc, ptrs, index, workspace, stream)
     with torch.cuda.device(index):
         return _head_call(name, query, desc, ptrs, index, workspace, stream)
+
+
+def _torch(found=[]):
+    """torch, which importing this module does not import (an import statement a call costs more than this)."""
+    if not found:
+        import torch
+        found.append(torch)
+    return found[0]
 
 
 def _int(v):
@@ -886,33 +896,37 @@ def _int(v):
     return v if v < 2**31 else 2**31 - 1
 
 
-def _block_launch(name, desc, ptrs, device, query=None):
-    """The entry point on the pointers of operands that the caller has checked, on the current stream of their device.
+def _block_launch(name, desc, ptrs, index, query=None):
+    """The entry point on the pointers of operands that the caller has checked, on the current stream of their device (its index).
 
     The autograd functions' way in: half of a small layer's time is the host's, and their backward runs on a thread of its
     own, on which each step costs twice as much.  (The workspace is the stream's, which orders its reuse.)"""
-    import torch
-    index = device.index
+    torch = _torch()
     if torch.cuda.current_device() != index:
         with torch.cuda.device(index):
-            return _block_launch(name, desc, ptrs, device, query)
-    L = lib()
+            return _block_launch(name, desc, ptrs, index, query)
+    L = _lib or lib()
     ref = ctypes.byref(desc)
     if query is None:
         status = getattr(L, name)(ref, *ptrs, _current_stream(index))
     else:
         need = getattr(L, query)(ref)
-        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        status = getattr(L, name)(ref, *ptrs, None if ws is None else ws.data_ptr(), need, _current_stream(index))
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
+            status = getattr(L, name)(ref, *ptrs, ws.data_ptr(), need, _current_stream(index))
+        else:
+            status = getattr(L, name)(ref, *ptrs, None, 0, _current_stream(index))
     if status != 0:
         raise QLError(name, status)
 
 
 def _kept_dense(index, q, e, lead, cols):
     """Pointers of a checkpoint of `lead` rows of `cols` values, both or neither given."""
-    if (q is None) != (e is None):
+    if q is None and e is None:
+        return None, None
+    if q is None or e is None:
         raise ValueError("q and e: both or neither")
-    import torch
+    torch = _torch()
     return _head_dense(index, ("q", q, (*lead, cols), torch.int8), ("e", e, (*lead, -(-cols // BLOCK_KEEP)), torch.uint8))
 
 
@@ -923,6 +937,8 @@ def qblock_pack8(x, q, e, stream=None):
     i, dt, code = _head_first(x, "x")
     rows, cols = x.shape
     p, ld = _head_rows("x", x, (rows, cols), dt, i)
+    if q is None or e is None:
+        raise ValueError("q and e are required")
     _block_call("qblock_pack8", None, BlockKeepDesc(rows, _int(cols), ld, code), (p, *_kept_dense(i, q, e, (rows,), cols)), i, None, stream)
 
 
@@ -931,6 +947,8 @@ def qblock_unpack8(q, e, x, stream=None):
     i, dt, code = _head_first(x, "x")
     rows, cols = x.shape
     p, ld = _head_rows("x", x, (rows, cols), dt, i)
+    if q is None or e is None:
+        raise ValueError("q and e are required")
     _block_call("qblock_unpack8", None, BlockKeepDesc(rows, _int(cols), ld, code), (*_kept_dense(i, q, e, (rows,), cols), p), i, None, stream)
 
 
@@ -940,16 +958,21 @@ def _block_norm(t, what, groups):
         raise ValueError(f"{what}: {t.dim()} dimensions, (n, ..., c) is required")
     if not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
-    n, c = t.shape[0], t.shape[-1]
-    i, dt, code = _head_first(t if t.dim() == 2 else t.view(n, -1) if t.numel() else t.new_empty((n, 0)), what)
+    n, *pixels, c = t.shape
+    index, dt = t.get_device(), t.dtype
+    if index < 0:
+        raise ValueError(f"{what}: a CUDA device tensor is required, got one on {t.device}")
+    torch = _torch()
+    if dt is not torch.bfloat16 and dt is not torch.float32:
+        raise ValueError(f"{what}: dtype {dt}, bfloat16 or float32 is required")
     if not isinstance(groups, int) or groups < 1 or c < 1 or c % groups:
         raise ValueError(f"groups {groups!r}: a whole number that divides the {c} channels is required")
     hw = 1
-    for size in t.shape[1:-1]:
+    for size in pixels:
         hw *= size
     if hw < 1:
         raise ValueError(f"{what}: shape {tuple(t.shape)} has no pixels")
-    return i, dt, code, n, hw, c
+    return index, dt, QL_BF16 if dt is torch.bfloat16 else QL_F32, n, hw, c
 
 
 def qblock_norm_fwd(x, groups, gamma, beta, y, mean=None, rstd=None, q=None, e=None, act="none", eps=1e-5, workspace=None, stream=None):
@@ -967,6 +990,8 @@ def qblock_norm_fwd(x, groups, gamma, beta, y, mean=None, rstd=None, q=None, e=N
 
 def _kept_rows(index, q, e, shape):
     """A checkpoint of a map, given in the map's shape or as (pixels, c)."""
+    if q is None and e is None:
+        return None, None
     if q is not None and q.dim() == 2 and len(shape) != 2:
         pixels = 1
         for size in shape[:-1]:

@@ -136,7 +136,7 @@ def _pack(t):
     q = torch.empty((rows, cols), device=t.device, dtype=torch.int8)
     e = torch.empty((rows, -(-cols // BLOCK_KEEP)), device=t.device, dtype=torch.uint8)
     ld = t.stride(0) if t.dim() == 2 and rows > 1 else cols
-    _block_launch("qblock_pack8", BlockKeepDesc(rows, _int(cols), ld, _qdtype(t)), (t.data_ptr(), q.data_ptr(), e.data_ptr()), t.device)
+    _block_launch("qblock_pack8", BlockKeepDesc(rows, _int(cols), ld, _qdtype(t)), (t.data_ptr(), q.data_ptr(), e.data_ptr()), t.get_device())
     return q, e
 
 
@@ -145,7 +145,7 @@ def _unpack(q, e, dtype, shape=None):
         return None
     rows, cols = q.shape
     t = torch.empty(q.shape if shape is None else shape, device=q.device, dtype=dtype)
-    _block_launch("qblock_unpack8", BlockKeepDesc(rows, cols, cols, _qdtype(t)), (q.data_ptr(), e.data_ptr(), t.data_ptr()), q.device)
+    _block_launch("qblock_unpack8", BlockKeepDesc(rows, cols, cols, _qdtype(t)), (q.data_ptr(), e.data_ptr(), t.data_ptr()), q.get_device())
     return t
 
 
@@ -438,7 +438,7 @@ class LinearActFunction(torch.autograd.Function):
             px, pw, pdy = _ptr(x), w.data_ptr(), dy.data_ptr()
             desc = HeadLinearDesc(m, k, n, k, w.stride(0) if n > 1 else k, n, dy.stride(0) if m > 1 else n, _qdtype(w), _head_act(ctx.act),
                                   _unaligned(px, pw, pdy), gw and dw.dtype is not dtype)
-            _block_launch("qhead_linear_bwd", desc, (px, pw, pdy, _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)), dev, "qhead_linear_bwd_workspace_size")
+            _block_launch("qhead_linear_bwd", desc, (px, pw, pdy, _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)), w.get_device(), "qhead_linear_bwd_workspace_size")
         return (dx, dw.to(ctx.wdtype) if gw else None, db.to(ctx.bdtype) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 3)
 
 
@@ -591,7 +591,7 @@ class GroupNormActFunction(torch.autograd.Function):
             q = torch.empty((n * hw, c), device=x.device, dtype=torch.int8)
             e = torch.empty((n * hw, -(-c // BLOCK_KEEP)), device=x.device, dtype=torch.uint8)
         _block_launch("qblock_norm_fwd", desc, (xn.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean, rstd, _ptr(q), _ptr(e)),
-                      x.device, "qblock_norm_fwd_workspace_size")
+                      x.get_device(), "qblock_norm_fwd_workspace_size")
         if train:
             if kept:
                 ctx.save_for_backward(q, e, gamma, beta, stats)
@@ -619,7 +619,7 @@ class GroupNormActFunction(torch.autograd.Function):
         mean = stats.data_ptr()
         _block_launch("qblock_norm_bwd", desc, (dy.data_ptr(), _ptr(x), _ptr(q), _ptr(e), _ptr(gamma), _ptr(beta), mean,
                                                 mean + 4 * desc.n * desc.groups, _ptr(dx), _ptr(dgamma), _ptr(dbeta)),
-                      dy.device, "qblock_norm_bwd_workspace_size")
+                      dy.get_device(), "qblock_norm_bwd_workspace_size")
         if gw and ctx.dtypes[0] is not torch.float32:
             dgamma = dgamma.to(ctx.dtypes[0])
         if gb and ctx.dtypes[1] is not torch.float32:
@@ -664,7 +664,7 @@ class GatedLinearFunction(torch.autograd.Function):
         ldx, ldw = (xm.stride(0) if m > 1 else k), (wgm.stride(0) if n > 1 else k)
         px, pg, pu = xm.data_ptr(), wgm.data_ptr(), wum.data_ptr()
         desc = BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, n, _qdtype(x), _head_act(act), _unaligned(px, pg, pu), 0)
-        _block_launch("qblock_gated_fwd", desc, (px, pg, pu, _ptr(bgf), _ptr(buf), h.data_ptr(), _ptr(z), _ptr(q), _ptr(e)), dev,
+        _block_launch("qblock_gated_fwd", desc, (px, pg, pu, _ptr(bgf), _ptr(buf), h.data_ptr(), _ptr(z), _ptr(q), _ptr(e)), x.get_device(),
                       "qblock_gated_fwd_workspace_size")
         if train:
             # (of x only what the weights' gradients read)
@@ -703,7 +703,7 @@ class GatedLinearFunction(torch.autograd.Function):
         desc = BlockGatedDesc(m, k, n, x.stride(0) if x is not None and m > 1 else k, wg.stride(0) if n > 1 else k,
                               dh.stride(0) if m > 1 else n, _qdtype(wg), _head_act(ctx.act), _unaligned(px, pg, pu), wdtype is not dtype)
         _block_launch("qblock_gated_bwd", desc, (px, pg, pu, dh.data_ptr(), _ptr(z), _ptr(q), _ptr(e), _ptr(dx), _ptr(dwg), _ptr(dwu),
-                                                 _ptr(dbg), _ptr(dbu)), dev, "qblock_gated_bwd_workspace_size")
+                                                 _ptr(dbg), _ptr(dbu)), wg.get_device(), "qblock_gated_bwd_workspace_size")
         out = [dx, dwg if gwg else None, dwu if gwu else None, dbg, dbu]
         for i, d in enumerate(ctx.dtypes, 1):
             if out[i] is not None and out[i].dtype is not d:

@@ -225,7 +225,7 @@ def calls(monkeypatch):
     """The library's calls replaced by stand-ins that compute nothing; each call's name and pointers."""
     seen = []
     monkeypatch.setattr(ag, "_same_device", lambda *tensors: None)
-    monkeypatch.setattr(ag, "_block_launch", lambda name, desc, ptrs, device, query=None: seen.append((name, ptrs)))
+    monkeypatch.setattr(ag, "_block_launch", lambda name, desc, ptrs, index, query=None: seen.append((name, ptrs)))
     for name in ("qhead_linear_fwd", "qhead_linear_bwd"):
         monkeypatch.setattr(ag, name, lambda *args, _name=name, **kw: seen.append((_name, args)))
     return seen
