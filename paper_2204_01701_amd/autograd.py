@@ -610,6 +610,7 @@ class GroupNormActFunction(torch.autograd.Function):
             q, e, gamma, beta, stats = ctx.saved_tensors
         else:
             x, gamma, beta, stats, *of = ctx.saved_tensors
+            x = _dense_image(x)  # (a hook of the saved tensors may have changed the order in memory)
         gx, gw, gb = ctx.needs_input_grad[:3]
         desc = ctx.desc
         dy = _dense_image(gy)

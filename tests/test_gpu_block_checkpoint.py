@@ -262,3 +262,37 @@ def test_two_streams_at_once():
     for i in range(2):
         for g in got[i]:
             assert all(torch.equal(a, w) for a, w in zip(g, want[i]))
+
+
+def test_saved_tensors_that_come_back_row_after_row():
+    # a hook of the saved tensors may return the same values in another order of memory (as one that keeps them in pinned memory
+    # of their size does): the gradients are those without it
+    x = torch.randn(3, 24, 5, 7, device=DEV).contiguous(memory_format=torch.channels_last).requires_grad_(True)
+    g, b = (torch.randn(24, device=DEV).requires_grad_(True) for _ in range(2))
+    dy = torch.randn_like(x)
+    want = torch.autograd.grad(group_norm_act(x, 4, g, b, act="silu"), (x, g, b), dy)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.contiguous().clone(memory_format=torch.contiguous_format), lambda t: t):
+        y = group_norm_act(x, 4, g, b, act="silu")
+    assert all(torch.equal(a, c) for a, c in zip(want, torch.autograd.grad(y, (x, g, b), dy)))
+    xl, wg, wu = leaves((9, 40), (33, 40), (33, 40), dtype=torch.float32, seed=1)
+    wide = torch.cat([t.detach() for t in (wg, wu)], 1)  # (weights that are halves of one matrix's rows)
+    wg, wu = (wide[:, s].requires_grad_(True) for s in (slice(0, 40), slice(40, 80)))
+    dh = torch.randn(9, 33, device=DEV)
+    want = torch.autograd.grad(gated_linear(xl, wg, wu), (xl, wg, wu), dh)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.clone(memory_format=torch.contiguous_format), lambda t: t):
+        h = gated_linear(xl, wg, wu)
+    assert all(torch.equal(a, c) for a, c in zip(want, torch.autograd.grad(h, (xl, wg, wu), dh)))
+
+
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+def test_an_empty_batch(checkpoint):
+    x = torch.randn(0, 16, 3, 3, device=DEV, requires_grad=True)
+    g, b = (torch.randn(16, device=DEV).requires_grad_(True) for _ in range(2))
+    y = group_norm_act(x, 4, g, b, act="gelu", checkpoint=checkpoint)
+    dx, dg, db = torch.autograd.grad(y, (x, g, b), torch.empty_like(y))
+    assert dx.shape == x.shape and not dg.any() and not db.any()
+    x = torch.randn(0, 40, device=DEV, requires_grad=True)
+    w, u = (torch.randn(33, 40, device=DEV).requires_grad_(True) for _ in range(2))
+    h = gated_linear(x, w, u, checkpoint=checkpoint)
+    dx, dw, du = torch.autograd.grad(h, (x, w, u), torch.empty_like(h))
+    assert h.shape == (0, 33) and dx.shape == x.shape and not dw.any() and not du.any()
