@@ -564,6 +564,23 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# What a backward reads of its saved tensors it reads by their pointers.  A hook of the saved tensors may bring one back in
+# another order of memory, or, by mistake, as something else than what was saved.
+
+def _saved(t, what, dtype, shape, index):
+    """A saved tensor whose dtype, shape and device are those that were saved."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"the saved {what} came back as {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {tuple(shape)} on the "
+                         "gradient's device was saved")
+    return t
+
+
+def _saved_dense(t, what, dtype, shape, index):
+    """... and dense, row after row."""
+    t = _saved(t, what, dtype, shape, index)
+    return t if t.is_contiguous() else t.contiguous()
+
+
 class GroupNormActFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, eps, act, train=True, checkpoint=None):
@@ -683,16 +700,23 @@ class GatedLinearFunction(torch.autograd.Function):
         of = ()
         gx, gwg, gwu, gbg, gbu = ctx.needs_input_grad[:5]
         gw = gwg or gwu
+        dtype, dev, index = gh.dtype, gh.device, gh.get_device()
+        dh = _matrix(gh)
+        (m, n), k = dh.shape, ctx.xshape[-1]
         if ctx.kept:
             _no_graph()
             xq, xe, wg, wu, q, e = ctx.saved_tensors
+            q = _saved_dense(q, "checkpoint", torch.int8, (2, m, n), index)
+            e = _saved_dense(e, "checkpoint's exponents", torch.uint8, (2, m, -(-n // BLOCK_KEEP)), index)
             if gw:
-                x = _unpack(xq, xe, wg.dtype)
+                x = _unpack(xq, xe, dtype)
         else:
             x, wg, wu, z, *of = ctx.saved_tensors
-        dtype, dev = wg.dtype, wg.device
-        dh = _matrix(gh)
-        (n, k), m = wg.shape, dh.shape[0]
+            z = _saved_dense(z, "projections", dtype, (2, m, n), index)
+            x = _matrix(_saved(x, "input", dtype, (m, k), index)) if gw else None
+        wg, wu = (_matrix(_saved(w, "weight", dtype, (n, k), index)) for w in (wg, wu))
+        if wg.stride() != wu.stride():
+            wg, wu = wg.contiguous(), wu.contiguous()
         # (weights kept in float32 get the gradient as it was accumulated)
         wdtype = dtype if ctx.dtypes[0] is dtype and ctx.dtypes[1] is dtype else torch.float32
         dx = torch.empty(ctx.xshape, device=dev, dtype=dtype) if gx else None
@@ -700,11 +724,11 @@ class GatedLinearFunction(torch.autograd.Function):
         dwu = torch.empty((n, k), device=dev, dtype=wdtype) if gw else None
         dbg = torch.empty(n, device=dev) if gbg else None
         dbu = torch.empty(n, device=dev) if gbu else None
-        px, pg, pu = _ptr(x) if gw else None, wg.data_ptr(), wu.data_ptr()
+        px, pg, pu = _ptr(x), wg.data_ptr(), wu.data_ptr()
         desc = BlockGatedDesc(m, k, n, x.stride(0) if x is not None and m > 1 else k, wg.stride(0) if n > 1 else k,
                               dh.stride(0) if m > 1 else n, _qdtype(wg), _head_act(ctx.act), _unaligned(px, pg, pu), wdtype is not dtype)
         _block_launch("qblock_gated_bwd", desc, (px, pg, pu, dh.data_ptr(), _ptr(z), _ptr(q), _ptr(e), _ptr(dx), _ptr(dwg), _ptr(dwu),
-                                                 _ptr(dbg), _ptr(dbu)), wg.get_device(), "qblock_gated_bwd_workspace_size")
+                                                 _ptr(dbg), _ptr(dbu)), index, "qblock_gated_bwd_workspace_size")
         out = [dx, dwg if gwg else None, dwu if gwu else None, dbg, dbu]
         for i, d in enumerate(ctx.dtypes, 1):
             if out[i] is not None and out[i].dtype is not d:

@@ -1,0 +1,139 @@
+"""Saved tensors that a hook brings back in another order of memory, of another dtype or of another shape: what the backward's
+calls are given holds the values that were saved, at the strides that the call states, or the backward refuses.  No GPU: the
+library's calls are replaced by a reader of the memory behind their pointers."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2204_01701_amd import autograd as ag
+
+SIZES = {torch.float32: 4, torch.int8: 1, torch.uint8: 1}
+
+
+def read(ptr, shape, strides=None, dtype=torch.float32):
+    """The values at a pointer as a kernel that knows only shape and strides takes them."""
+    if strides is None:
+        strides = [math.prod(shape[i + 1:]) for i in range(len(shape))]
+    n = sum((s - 1) * d for s, d in zip(shape, strides)) + 1
+    raw = bytearray(ctypes.string_at(ptr, n * SIZES[dtype]))
+    return torch.frombuffer(raw, dtype=dtype).as_strided(shape, strides).clone()
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """What the library's calls are given: (name, descriptor, pointers), or, by name, what a reader makes of them at the call."""
+    seen, readers = [], {}
+
+    def launch(name, desc, ptrs, index, query=None):
+        seen.append((name, readers[name](desc, ptrs) if name in readers else None))
+
+    monkeypatch.setattr(ag, "_same_device", lambda *tensors: None)
+    monkeypatch.setattr(ag, "_block_launch", launch)
+    launch.seen, launch.readers = seen, readers
+    return launch
+
+
+def turned(t):
+    """The same values, the last dimension outermost in memory."""
+    dims = list(range(t.dim()))[::-1]
+    return t.permute(dims).contiguous().permute(dims)
+
+
+def spread(t):
+    """The same values, every other element of memory."""
+    wide = torch.empty(*t.shape, 2, dtype=t.dtype)
+    wide[..., 0] = t
+    return wide[..., 0]
+
+
+ORDERS = [turned, spread]
+
+
+def only(i, f):
+    """A hook that changes the i-th saved tensor alone."""
+    count = [0]
+
+    def unpack(t):
+        count[0] += 1
+        return f(t) if count[0] == i + 1 else t
+    return unpack
+
+
+def leaf(*shape):
+    return torch.randn(*shape, requires_grad=True)
+
+
+# --- the gated layer -------------------------------------------------------------------
+
+M, K, N = 6, 40, 36
+
+
+def read_gated(desc, ptrs):
+    assert (desc.m, desc.k, desc.n) == (M, K, N)
+    x, wg, wu, dh, z, q, e = ptrs[:7]
+    out = {"wg": read(wg, (N, K), (desc.ldw, 1)), "wu": read(wu, (N, K), (desc.ldw, 1)), "dh": read(dh, (M, N), (desc.ldh, 1))}
+    if x is not None:
+        out["x"] = read(x, (M, K), (desc.ldx, 1))
+    if z is not None:
+        out["z"] = read(z, (2, M, N))
+    if q is not None:
+        out["q"], out["e"] = read(q, (2, M, N), dtype=torch.int8), read(e, (2, M, 2), dtype=torch.uint8)
+    return out
+
+
+def gated(calls, unpack, checkpoint=None):
+    """(what the backward read without the hook, with it)."""
+    calls.readers["qblock_gated_bwd"] = read_gated
+    torch.manual_seed(3)
+    leaves, dh = [leaf(M, K), leaf(N, K), leaf(N, K)], torch.randn(M, N)
+    filled = torch.randn(2, M, N), torch.randint(-9, 9, (2, M, N), dtype=torch.int8), torch.randint(1, 9, (2, M, 2), dtype=torch.uint8)
+
+    def write(desc, ptrs):  # what the forward leaves for the backward
+        for p, t in zip(ptrs[6:9], filled):
+            if p is not None:
+                ctypes.memmove(p, t.data_ptr(), t.numel() * t.element_size())
+    calls.readers["qblock_gated_fwd"] = write
+    for hook in (lambda t: t, unpack):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, hook):
+            h = ag.gated_linear(*leaves, checkpoint=checkpoint)
+        torch.autograd.grad(h, leaves, dh)
+    plain, hooked = [got for name, got in calls.seen if name == "qblock_gated_bwd"]
+    return plain, hooked
+
+
+@pytest.mark.parametrize("f", ORDERS)
+@pytest.mark.parametrize("i", range(4), ids=["x", "wg", "wu", "z"])
+def test_gated_layer(calls, i, f):
+    plain, hooked = gated(calls, only(i, f))
+    assert sorted(plain) == ["dh", "wg", "wu", "x", "z"]
+    for name, t in plain.items():
+        assert torch.equal(hooked[name], t), name
+
+
+@pytest.mark.parametrize("f", ORDERS)
+@pytest.mark.parametrize("i", range(2, 6), ids=["wg", "wu", "q", "e"])
+def test_gated_layer_from_its_checkpoint(calls, i, f):
+    plain, hooked = gated(calls, only(i, f), "int8")
+    assert sorted(plain) == ["dh", "e", "q", "wg", "wu", "x"]
+    for name, t in plain.items():
+        if name != "x":  # (unpacked by a call that is not made here)
+            assert torch.equal(hooked[name], t), name
+
+
+WRONG = [lambda t: t.double(), lambda t: t[..., :-1], lambda t: t.unsqueeze(0)]
+
+
+@pytest.mark.parametrize("f", WRONG, ids=["dtype", "shape", "dimensions"])
+@pytest.mark.parametrize("i", range(4), ids=["x", "wg", "wu", "z"])
+def test_gated_layer_refuses(calls, i, f):
+    with pytest.raises(ValueError, match="saved"):
+        gated(calls, only(i, f))
+
+
+@pytest.mark.parametrize("f", WRONG, ids=["dtype", "shape", "dimensions"])
+@pytest.mark.parametrize("i", range(2, 6), ids=["wg", "wu", "q", "e"])
+def test_gated_layer_refuses_checkpoints(calls, i, f):
+    with pytest.raises(ValueError, match="saved"):
+        gated(calls, only(i, f), "int8")

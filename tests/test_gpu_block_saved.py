@@ -1,0 +1,61 @@
+"""Hooks of the saved tensors that bring them back in another order of memory: the gradients are those without the hook, bit for
+bit; tensors that come back on another device or of another dtype are refused before a kernel reads them."""
+import pytest
+import torch
+
+from paper_2204_01701_amd.autograd import gated_linear
+from test_block_saved_cpu import ORDERS
+from test_gpu_block_keep import DEV, TYPES, type_ids
+
+pytestmark = pytest.mark.gpu
+
+
+def check(leaves, f, order):
+    """Gradients of f(*leaves) with every saved tensor brought back as `order` leaves it, against those without."""
+    y = f(*leaves)
+    dy = torch.randn_like(y)
+    want = torch.autograd.grad(y, leaves, dy)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, order):
+        y = f(*leaves)
+    for got, w in zip(torch.autograd.grad(y, leaves, dy), want):
+        assert torch.equal(got, w)
+
+
+def refused(leaves, f):
+    for wrong in (lambda t: t.cpu(), lambda t: t.half()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, wrong):
+            y = f(*leaves)
+        with pytest.raises(ValueError):
+            torch.autograd.grad(y, leaves, torch.randn_like(y))
+
+
+def leaf(*shape, dtype):
+    return torch.randn(*shape, device=DEV).to(dtype).requires_grad_(True)
+
+
+def _gpu_order(order):
+    """The orders of the CPU's tests on tensors of this device."""
+    if order.__name__ == "spread":
+        def spread(t):
+            wide = torch.zeros(*t.shape, 2, dtype=t.dtype, device=t.device)
+            wide[..., 0] = t
+            return wide[..., 0]
+        return spread
+    return order
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+@pytest.mark.parametrize("m,k,n", [(33, 40, 72), (9, 17, 5)])
+def test_gated_layer(m, k, n, checkpoint, order, dtype):
+    leaves = [leaf(m, k, dtype=dtype), leaf(n, k, dtype=dtype), leaf(n, k, dtype=dtype)]
+
+    def f(*leaves):
+        return gated_linear(*leaves, checkpoint=checkpoint)
+    if checkpoint is None:
+        check(leaves, f, _gpu_order(order))
+    else:  # (the weights and the projections' checkpoint; x's own is read by unpack8, the input's gradient alone does not need it)
+        x, wg, wu = leaves
+        check([x], lambda x: gated_linear(x, wg.detach(), wu.detach(), checkpoint=checkpoint), _gpu_order(order))
+    refused(leaves, f)
