@@ -622,22 +622,27 @@ class GroupNormActFunction(torch.autograd.Function):
     def backward(ctx, gy):
         x = q = e = None
         of = ()
+        gx, gw, gb = ctx.needs_input_grad[:3]
+        desc = ctx.desc
+        n, c, index = desc.n, desc.c, gy.get_device()
         if ctx.kept:
             _no_graph()
             q, e, gamma, beta, stats = ctx.saved_tensors
+            q = _saved_dense(q, "checkpoint", torch.int8, (n * desc.hw, c), index)
+            e = _saved_dense(e, "checkpoint's exponents", torch.uint8, (n * desc.hw, -(-c // BLOCK_KEEP)), index)
         else:
             x, gamma, beta, stats, *of = ctx.saved_tensors
-            x = _dense_image(x)  # (a hook of the saved tensors may have changed the order in memory)
-        gx, gw, gb = ctx.needs_input_grad[:3]
-        desc = ctx.desc
+            x = _dense_image(_saved(x, "input", gy.dtype, gy.shape, index))
+        gamma, beta = (None if t is None else _saved_dense(t, "weight or bias", torch.float32, (c,), index) for t in (gamma, beta))
+        stats = _saved_dense(stats, "statistics", torch.float32, (2, n, desc.groups), index)
         dy = _dense_image(gy)
         dx = torch.empty_like(dy) if gx else None
-        dgamma = torch.empty(desc.c, device=dy.device) if gw else None
-        dbeta = torch.empty(desc.c, device=dy.device) if gb else None
+        dgamma = torch.empty(c, device=dy.device) if gw else None
+        dbeta = torch.empty(c, device=dy.device) if gb else None
         mean = stats.data_ptr()
         _block_launch("qblock_norm_bwd", desc, (dy.data_ptr(), _ptr(x), _ptr(q), _ptr(e), _ptr(gamma), _ptr(beta), mean,
-                                                mean + 4 * desc.n * desc.groups, _ptr(dx), _ptr(dgamma), _ptr(dbeta)),
-                      dy.get_device(), "qblock_norm_bwd_workspace_size")
+                                                mean + 4 * n * desc.groups, _ptr(dx), _ptr(dgamma), _ptr(dbeta)),
+                      index, "qblock_norm_bwd_workspace_size")
         if gw and ctx.dtypes[0] is not torch.float32:
             dgamma = dgamma.to(ctx.dtypes[0])
         if gb and ctx.dtypes[1] is not torch.float32:

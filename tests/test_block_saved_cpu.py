@@ -137,3 +137,62 @@ def test_gated_layer_refuses(calls, i, f):
 def test_gated_layer_refuses_checkpoints(calls, i, f):
     with pytest.raises(ValueError, match="saved"):
         gated(calls, only(i, f), "int8")
+
+
+# --- group norm ------------------------------------------------------------------------
+
+MAP, GROUPS = (2, 36, 3, 5), 4
+
+
+def read_norm(desc, ptrs):
+    n, c, h, w = MAP
+    assert (desc.n, desc.hw, desc.c, desc.groups) == (n, h * w, c, GROUPS)
+    dy, x, q, e, gamma, beta, mean, rstd = ptrs[:8]
+    out = {"dy": read(dy, (n, h, w, c)), "gamma": read(gamma, (c,)), "beta": read(beta, (c,)), "mean": read(mean, (n, GROUPS)),
+           "rstd": read(rstd, (n, GROUPS))}
+    if x is not None:
+        out["x"] = read(x, (n, h, w, c))
+    if q is not None:
+        out["q"], out["e"] = read(q, (n * h * w, c), dtype=torch.int8), read(e, (n * h * w, 2), dtype=torch.uint8)
+    return out
+
+
+def norm(calls, unpack, checkpoint=None):
+    calls.readers["qblock_norm_bwd"] = read_norm
+    n, c, h, w = MAP
+    torch.manual_seed(4)
+    leaves, dy = [leaf(*MAP), leaf(c), leaf(c)], torch.randn(MAP)
+    stats = torch.randn(2, n, GROUPS)
+    filled = (stats[0], stats[1], torch.randint(-9, 9, (n * h * w, c), dtype=torch.int8), torch.randint(1, 9, (n * h * w, 2), dtype=torch.uint8))
+
+    def write(desc, ptrs):
+        for p, t in zip(ptrs[4:8], filled):
+            if p is not None:
+                ctypes.memmove(p, t.data_ptr(), t.numel() * t.element_size())
+    calls.readers["qblock_norm_fwd"] = write
+    for hook in (lambda t: t, unpack):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, hook):
+            y = ag.group_norm_act(leaves[0], GROUPS, leaves[1], leaves[2], checkpoint=checkpoint)
+        torch.autograd.grad(y, leaves, dy)
+    plain, hooked = [got for name, got in calls.seen if name == "qblock_norm_bwd"]
+    return plain, hooked
+
+
+KEPT = [(None, i) for i in range(4)] + [("int8", i) for i in range(5)]
+KEPT_IDS = ["x", "gamma", "beta", "stats", "kept q", "kept e", "kept gamma", "kept beta", "kept stats"]
+
+
+@pytest.mark.parametrize("f", ORDERS)
+@pytest.mark.parametrize("checkpoint,i", KEPT, ids=KEPT_IDS)
+def test_group_norm(calls, checkpoint, i, f):
+    plain, hooked = norm(calls, only(i, f), checkpoint)
+    assert sorted(plain) == sorted(["dy", "gamma", "beta", "mean", "rstd"] + (["q", "e"] if checkpoint else ["x"]))
+    for name, t in plain.items():
+        assert torch.equal(hooked[name], t), name
+
+
+@pytest.mark.parametrize("f", WRONG, ids=["dtype", "shape", "dimensions"])
+@pytest.mark.parametrize("checkpoint,i", KEPT, ids=KEPT_IDS)
+def test_group_norm_refuses(calls, checkpoint, i, f):
+    with pytest.raises(ValueError, match="saved"):
+        norm(calls, only(i, f), checkpoint)

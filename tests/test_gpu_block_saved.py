@@ -3,7 +3,7 @@ bit; tensors that come back on another device or of another dtype are refused be
 import pytest
 import torch
 
-from paper_2204_01701_amd.autograd import gated_linear
+from paper_2204_01701_amd.autograd import gated_linear, group_norm_act
 from test_block_saved_cpu import ORDERS
 from test_gpu_block_keep import DEV, TYPES, type_ids
 
@@ -58,4 +58,17 @@ def test_gated_layer(m, k, n, checkpoint, order, dtype):
     else:  # (the weights and the projections' checkpoint; x's own is read by unpack8, the input's gradient alone does not need it)
         x, wg, wu = leaves
         check([x], lambda x: gated_linear(x, wg.detach(), wu.detach(), checkpoint=checkpoint), _gpu_order(order))
+    refused(leaves, f)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+@pytest.mark.parametrize("shape", [(3, 36, 5, 7), (9, 36)])
+def test_group_norm(shape, checkpoint, order, dtype):
+    leaves = [leaf(*shape, dtype=dtype), leaf(36, dtype=torch.float32), leaf(36, dtype=dtype)]
+
+    def f(x, g, b):
+        return group_norm_act(x, 4, g, b, act="silu", checkpoint=checkpoint)
+    check(leaves, f, _gpu_order(order))
     refused(leaves, f)
