@@ -51,6 +51,8 @@ activations, a backward under ``create_graph`` raises.
 """
 from __future__ import annotations
 
+import math
+
 import torch
 
 from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL_NEURON_T24, conv_desc, epilogue,
@@ -140,12 +142,32 @@ def _pack(t):
     return q, e
 
 
-def _unpack(q, e, dtype, shape=None):
+# What a backward reads of its saved tensors it reads by their pointers.  A hook of the saved tensors may bring one back in
+# another order of memory, or, by mistake, as something else than what was saved.
+
+def _saved(t, what, dtype, shape, index):
+    """A saved tensor whose dtype, shape and device are those that were saved."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"the saved {what} came back as {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {tuple(shape)} on the "
+                         "gradient's device was saved")
+    return t
+
+
+def _saved_dense(t, what, dtype, shape, index):
+    """... and dense, row after row."""
+    t = _saved(t, what, dtype, shape, index)
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _unpack(q, e, dtype, shape, index):
+    """The values (`shape`, in blocks of its last dimension) of a saved checkpoint (None: none)."""
     if q is None:
         return None
-    rows, cols = q.shape
-    t = torch.empty(q.shape if shape is None else shape, device=q.device, dtype=dtype)
-    _block_launch("qblock_unpack8", BlockKeepDesc(rows, cols, cols, _qdtype(t)), (q.data_ptr(), e.data_ptr(), t.data_ptr()), q.get_device())
+    rows, cols = math.prod(shape[:-1]), shape[-1]
+    q = _saved_dense(q, "checkpoint", torch.int8, (rows, cols), index)
+    e = _saved_dense(e, "checkpoint's exponents", torch.uint8, (rows, -(-cols // BLOCK_KEEP)), index)
+    t = torch.empty(shape, device=q.device, dtype=dtype)
+    _block_launch("qblock_unpack8", BlockKeepDesc(rows, cols, cols, _qdtype(t)), (q.data_ptr(), e.data_ptr(), t.data_ptr()), index)
     return t
 
 
@@ -199,8 +221,9 @@ class QuadConv2dFunction(torch.autograd.Function):
             _no_graph()
             xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
             y_shape = (d.n, d.ho, d.wo, d.o)
-            xn = _unpack(xq, xe, _tdtype(d.dtype), (d.n, d.h, d.w, d.c))
-            ta, tb = _unpack(taq, tae, xn.dtype, y_shape), _unpack(tbq, tbe, xn.dtype, y_shape)
+            index = gy.get_device()
+            xn = _unpack(xq, xe, _tdtype(d.dtype), (d.n, d.h, d.w, d.c), index)
+            ta, tb = (_unpack(q, e, xn.dtype, y_shape, index) for q, e in ((taq, tae), (tbq, tbe)))
         else:
             xn, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
         wn, bl = [wa, wb, wc], [ba, bb, bc]
@@ -287,8 +310,9 @@ class QuadLinearFunction(torch.autograd.Function):
         if ctx.kept:
             _no_graph()
             xq, xe, wa, wb, wc, ba, bb, bc, taq, tae, tbq, tbe, relu_y = ctx.saved_tensors
-            xc = _unpack(xq, xe, _tdtype(d.dtype))
-            ta, tb = _unpack(taq, tae, xc.dtype), _unpack(tbq, tbe, xc.dtype)
+            index = gy.get_device()
+            xc = _unpack(xq, xe, _tdtype(d.dtype), (d.batch, d.in_), index)
+            ta, tb = (_unpack(q, e, xc.dtype, (d.batch, d.out), index) for q, e in ((taq, tae), (tbq, tbe)))
         else:
             xc, wa, wb, wc, ba, bb, bc, ta, tb, relu_y = ctx.saved_tensors
         wl, bl = [wa, wb, wc], [ba, bb, bc]
@@ -427,11 +451,12 @@ class LinearActFunction(torch.autograd.Function):
     def _kept_backward(ctx, gy):
         xq, xe, w, zq, ze = ctx.saved_tensors
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
-        dtype, dev = w.dtype, w.device
+        dtype, dev, index = w.dtype, w.device, gy.get_device()
         dx = dw = db = None
         if gx or gw or gb:
-            x, z, dy = _unpack(xq, xe, dtype) if gw else None, _unpack(zq, ze, dtype), _matrix(gy)
+            dy = _matrix(gy)
             (n, k), m = w.shape, dy.shape[0]
+            x, z = _unpack(xq, xe, dtype, (m, k), index) if gw else None, _unpack(zq, ze, dtype, (m, n), index)
             dx = torch.empty(ctx.xshape, device=dev, dtype=dtype) if gx else None
             dw = torch.empty((n, k), device=dev, dtype=dtype if ctx.wdtype is dtype else torch.float32) if gw else None
             db = torch.empty(n, device=dev) if gb else None
@@ -562,23 +587,6 @@ def _f32(t):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-# What a backward reads of its saved tensors it reads by their pointers.  A hook of the saved tensors may bring one back in
-# another order of memory, or, by mistake, as something else than what was saved.
-
-def _saved(t, what, dtype, shape, index):
-    """A saved tensor whose dtype, shape and device are those that were saved."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
-        raise ValueError(f"the saved {what} came back as {t.dtype} {tuple(t.shape)} on {t.device}, {dtype} {tuple(shape)} on the "
-                         "gradient's device was saved")
-    return t
-
-
-def _saved_dense(t, what, dtype, shape, index):
-    """... and dense, row after row."""
-    t = _saved(t, what, dtype, shape, index)
-    return t if t.is_contiguous() else t.contiguous()
 
 
 class GroupNormActFunction(torch.autograd.Function):
@@ -714,7 +722,7 @@ class GatedLinearFunction(torch.autograd.Function):
             q = _saved_dense(q, "checkpoint", torch.int8, (2, m, n), index)
             e = _saved_dense(e, "checkpoint's exponents", torch.uint8, (2, m, -(-n // BLOCK_KEEP)), index)
             if gw:
-                x = _unpack(xq, xe, dtype)
+                x = _unpack(xq, xe, dtype, (m, k), index)
         else:
             x, wg, wu, z, *of = ctx.saved_tensors
             z = _saved_dense(z, "projections", dtype, (2, m, n), index)

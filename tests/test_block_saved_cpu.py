@@ -196,3 +196,79 @@ def test_group_norm(calls, checkpoint, i, f):
 def test_group_norm_refuses(calls, checkpoint, i, f):
     with pytest.raises(ValueError, match="saved"):
         norm(calls, only(i, f), checkpoint)
+
+
+# --- what the layers keep of their inputs and maps in 8 bits ---------------------------------
+
+@pytest.fixture
+def layer(calls, monkeypatch):
+    """The layers' own calls replaced as well; what the reads of the checkpoints are given: (q, e) by the shape of q."""
+    for name in ("qhead_linear_fwd", "qhead_linear_bwd", "qlayer_linear_fwd", "qlayer_linear_bwd", "qlayer_conv2d_fwd", "qlayer_conv2d_bwd_data",
+                 "qlayer_conv2d_bwd_weight"):
+        monkeypatch.setattr(ag, name, lambda *args, **kw: None)
+
+    def pack(desc, ptrs):
+        g = torch.Generator().manual_seed(desc.rows * 1000 + desc.cols)
+        for p, shape, dtype, lo in ((ptrs[1], (desc.rows, desc.cols), torch.int8, -9), (ptrs[2], (desc.rows, -(-desc.cols // 32)), torch.uint8, 1)):
+            t = torch.randint(lo, 9, shape, dtype=dtype, generator=g)
+            ctypes.memmove(p, t.data_ptr(), t.numel())
+
+    def unpack(desc, ptrs):
+        return read(ptrs[0], (desc.rows, desc.cols), dtype=torch.int8), read(ptrs[1], (desc.rows, -(-desc.cols // 32)), dtype=torch.uint8)
+    calls.readers.update(qblock_pack8=pack, qblock_unpack8=unpack)
+    return calls
+
+
+def layers():
+    """name: leaves, layer, the places of the checkpoints among what is saved."""
+    ws = [leaf(36, 40) for _ in range(3)]
+    cs = [leaf(36, 40, 3, 3) for _ in range(3)]
+    return {"linear": ([leaf(6, 40), leaf(36, 40)], lambda x, w: ag.linear_act(x, w, act="silu", checkpoint="int8"), (0, 1, 3, 4)),
+            "gated": ([leaf(6, 40), leaf(36, 40), leaf(36, 40)], lambda *a: ag.gated_linear(*a, checkpoint="int8"), (0, 1)),
+            "quadratic": ([leaf(6, 40), *ws], lambda *a: ag.quad_linear(*a, checkpoint="int8"), (0, 1, 5, 6, 7, 8)),
+            "convolution": ([leaf(2, 40, 4, 5), *cs], lambda *a: ag.quad_conv2d(*a, pad=1, checkpoint="int8"), (0, 1, 5, 6, 7, 8))}
+
+
+def read_back(layer, which, unpack):
+    """What the reads of the checkpoints were given without the hook, with it."""
+    leaves, f, _ = layers()[which]
+    every = []
+    for hook in (lambda t: t, unpack):
+        layer.seen.clear()
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, hook):
+            y = f(*leaves)
+        torch.autograd.grad(y, leaves, torch.randn(y.shape))
+        every.append([got for name, got in layer.seen if name == "qblock_unpack8"])
+    return every
+
+
+KEEPS = [(which, i) for which, (_, _, kept) in layers().items() for i in range(len(kept))]
+
+
+@pytest.mark.parametrize("f", ORDERS)
+@pytest.mark.parametrize("which,i", KEEPS)
+def test_checkpoints(layer, which, i, f):
+    # (saved tensors that are None do not come by a hook: those of the layers above are all there but the biases)
+    plain, hooked = read_back(layer, which, at_kept(i, f))
+    assert len(plain) == len(hooked) == len([k for w, k in KEEPS if w == which]) // 2
+    for (q, e), (hq, he) in zip(plain, hooked):
+        assert torch.equal(q, hq) and torch.equal(e, he)
+
+
+def at_kept(i, f):
+    """A hook that changes the i-th of the checkpoints' tensors alone (int8 and uint8 ones, in the order in which they were saved)."""
+    count = [0]
+
+    def unpack(t):
+        if t.dtype not in (torch.int8, torch.uint8):
+            return t
+        count[0] += 1
+        return f(t) if count[0] == i + 1 else t
+    return unpack
+
+
+@pytest.mark.parametrize("f", WRONG, ids=["dtype", "shape", "dimensions"])
+@pytest.mark.parametrize("which,i", KEEPS)
+def test_checkpoints_refuse(layer, which, i, f):
+    with pytest.raises(ValueError, match="saved"):
+        read_back(layer, which, at_kept(i, f))

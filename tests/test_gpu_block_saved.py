@@ -3,7 +3,7 @@ bit; tensors that come back on another device or of another dtype are refused be
 import pytest
 import torch
 
-from paper_2204_01701_amd.autograd import gated_linear, group_norm_act
+from paper_2204_01701_amd.autograd import gated_linear, group_norm_act, linear_act, quad_conv2d, quad_linear
 from test_block_saved_cpu import ORDERS
 from test_gpu_block_keep import DEV, TYPES, type_ids
 
@@ -72,3 +72,30 @@ def test_group_norm(shape, checkpoint, order, dtype):
         return group_norm_act(x, 4, g, b, act="silu", checkpoint=checkpoint)
     check(leaves, f, _gpu_order(order))
     refused(leaves, f)
+
+
+def of_checkpoints(order):
+    """The hook for the checkpoints' tensors alone."""
+    return lambda t: order(t) if t.dtype in (torch.int8, torch.uint8) else t
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("layer", ["linear", "gated", "quadratic", "convolution"])
+def test_checkpoints(layer, order, dtype):
+    def leaves(*shapes):
+        return [leaf(*s, dtype=dtype) for s in shapes]
+    if layer == "convolution":
+        of, f = leaves((2, 40, 5, 6), *[(36, 40, 3, 3)] * 3), lambda *a: quad_conv2d(*a, pad=1, checkpoint="int8")
+    elif layer == "quadratic":
+        of, f = leaves((20, 40), *[(36, 40)] * 3), lambda *a: quad_linear(*a, checkpoint="int8")
+    elif layer == "gated":
+        of, f = leaves((20, 40), (36, 40), (36, 40)), lambda *a: gated_linear(*a, checkpoint="int8")
+    else:
+        of, f = leaves((20, 40), (36, 40)), lambda *a: linear_act(*a, act="gelu", checkpoint="int8")
+    check(of, f, of_checkpoints(_gpu_order(order)))
+    for wrong in (lambda t: t.cpu(), lambda t: t.short()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, of_checkpoints(wrong)):
+            y = f(*of)
+        with pytest.raises(ValueError):
+            torch.autograd.grad(y, of, torch.randn_like(y))
