@@ -451,11 +451,12 @@ class LinearActFunction(torch.autograd.Function):
     def _kept_backward(ctx, gy):
         xq, xe, w, zq, ze = ctx.saved_tensors
         gx, gw, gb, gr = ctx.needs_input_grad[:4]
-        dtype, dev, index = w.dtype, w.device, gy.get_device()
+        dtype, dev, index = gy.dtype, gy.device, gy.get_device()
         dx = dw = db = None
         if gx or gw or gb:
             dy = _matrix(gy)
-            (n, k), m = w.shape, dy.shape[0]
+            (m, n), k = dy.shape, ctx.xshape[-1]
+            w = _matrix(_saved(w, "weight", dtype, (n, k), index))
             x, z = _unpack(xq, xe, dtype, (m, k), index) if gw else None, _unpack(zq, ze, dtype, (m, n), index)
             dx = torch.empty(ctx.xshape, device=dev, dtype=dtype) if gx else None
             dw = torch.empty((n, k), device=dev, dtype=dtype if ctx.wdtype is dtype else torch.float32) if gw else None
@@ -463,7 +464,7 @@ class LinearActFunction(torch.autograd.Function):
             px, pw, pdy = _ptr(x), w.data_ptr(), dy.data_ptr()
             desc = HeadLinearDesc(m, k, n, k, w.stride(0) if n > 1 else k, n, dy.stride(0) if m > 1 else n, _qdtype(w), _head_act(ctx.act),
                                   _unaligned(px, pw, pdy), gw and dw.dtype is not dtype)
-            _block_launch("qhead_linear_bwd", desc, (px, pw, pdy, _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)), w.get_device(), "qhead_linear_bwd_workspace_size")
+            _block_launch("qhead_linear_bwd", desc, (px, pw, pdy, _ptr(z), _ptr(dx), _ptr(dw), _ptr(db)), index, "qhead_linear_bwd_workspace_size")
         return (dx, dw.to(ctx.wdtype) if gw else None, db.to(ctx.bdtype) if gb else None, gy.to(ctx.rdtype) if gr else None, *[None] * 3)
 
 

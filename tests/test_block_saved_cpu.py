@@ -272,3 +272,31 @@ def at_kept(i, f):
 def test_checkpoints_refuse(layer, which, i, f):
     with pytest.raises(ValueError, match="saved"):
         read_back(layer, which, at_kept(i, f))
+
+
+# --- the first-order layer's weight beside its checkpoints -----------------------------------
+
+def linear(layer, unpack, act="none"):
+    """(weight as the backward read it without the hook, with it)."""
+    def read_linear(desc, ptrs):
+        assert (desc.m, desc.k, desc.n) == (M, K, N)
+        return read(ptrs[1], (N, K), (desc.ldw, 1))
+    layer.readers["qhead_linear_bwd"] = read_linear
+    leaves = [leaf(M, K), leaf(N, K)]
+    for hook in (lambda t: t, unpack):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, hook):
+            y = ag.linear_act(*leaves, act=act, checkpoint="int8")
+        torch.autograd.grad(y, leaves, torch.randn(M, N))
+    return [got for name, got in layer.seen if name == "qhead_linear_bwd"]
+
+
+@pytest.mark.parametrize("f", ORDERS)
+def test_first_order_layers_weight(layer, f):
+    plain, hooked = linear(layer, only(2, f))
+    assert torch.equal(plain, hooked)
+
+
+@pytest.mark.parametrize("f", WRONG, ids=["dtype", "shape", "dimensions"])
+def test_first_order_layers_weight_refuses(layer, f):
+    with pytest.raises(ValueError, match="saved"):
+        linear(layer, only(2, f))

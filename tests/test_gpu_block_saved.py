@@ -99,3 +99,18 @@ def test_checkpoints(layer, order, dtype):
             y = f(*of)
         with pytest.raises(ValueError):
             torch.autograd.grad(y, of, torch.randn_like(y))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("m,k,n", [(33, 40, 72), (9, 17, 5)])
+def test_first_order_layer(m, k, n, order, dtype):
+    leaves = [leaf(m, k, dtype=dtype), leaf(n, k, dtype=dtype)]
+
+    def f(*leaves):
+        return linear_act(*leaves, act="silu", checkpoint="int8")
+    check(leaves, f, _gpu_order(order))
+    refused(leaves, f)
+    x, w = leaves  # (the weight alone: the input's gradient without an activation reads nothing else)
+    check([x], lambda x: linear_act(x, w.detach(), checkpoint="int8"), _gpu_order(order))
+    refused([x], lambda x: linear_act(x, w.detach(), checkpoint="int8"))
