@@ -74,8 +74,8 @@ ql_status qblock_unpack8(const qblock_keep_desc *desc, const int8_t *q, const ui
  *     t = gamma dz,   dx = rstd (t - avg(t) - xh avg(t xh))     (averages over the group)
  * x is given as it was, or (x NULL) as its checkpoint q, e: xh and z are then formed
  * from x8 with the mean and rstd of the forward.  dx : of `dtype`, may be dy or x;
- * dgamma, dbeta : c float32; each of the three may be NULL (not all).  relu'(0) = 0.
- * n >= 0 (with n = 0 dgamma and dbeta are 0); hw, c >= 1; groups divides c;
+ * dgamma, dbeta : c float32; each of the three may be NULL (not all, but for n = 0).
+ * relu'(0) = 0.  n >= 0 (with n = 0 dgamma and dbeta are 0); hw, c >= 1; groups divides c;
  * eps > 0 and finite.  QL_EUNSUPPORTED: n or hw above 2^31 - 65536, c above 2^20,
  * 2^47 values or more.
  * ------------------------------------------------------------------------- */

@@ -176,7 +176,7 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void 
                           const float *beta, const float *mean, const float *rstd, void *dx, float *dgamma, float *dbeta, void *workspace,
                           size_t workspace_bytes, void *stream) {
     if (!norm_ok(d)) return QL_EINVAL;
-    if (!dx && !dgamma && !dbeta) return QL_EINVAL;
+    if (d->n > 0 && !dx && !dgamma && !dbeta) return QL_EINVAL;  // (of an empty map dx is no pointer)
     if (!sizes_fit(d)) return QL_EUNSUPPORTED;
     const size_t es = esize(d->dtype);
     if (d->n > 0 && (!dy || (!x && (!q || !e)) || !mean || !rstd)) return QL_EINVAL;
@@ -186,8 +186,8 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *d, const void *dy, const void 
         if (!aligned(p, 4)) return QL_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (d->n == 0) {
-        if (dgamma || dbeta)
-            hipLaunchKernelGGL(qblock_zero_kernel<>, dim3(grid_1d(d->c)), dim3(kThreads), 0, st, dgamma, dbeta, d->c);
+        if (!dgamma && !dbeta) return QL_OK;
+        hipLaunchKernelGGL(qblock_zero_kernel<>, dim3(grid_1d(d->c)), dim3(kThreads), 0, st, dgamma, dbeta, d->c);
         return hip_status();
     }
     const size_t need = qblock_norm_bwd_workspace_size(d);

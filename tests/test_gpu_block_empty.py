@@ -1,0 +1,20 @@
+"""Batches of no rows where only some gradients are wanted."""
+import pytest
+import torch
+
+from paper_2204_01701_amd.autograd import group_norm_act
+from test_gpu_block_keep import DEV, TYPES, type_ids
+
+pytestmark = pytest.mark.gpu
+checkpoints = pytest.mark.parametrize("checkpoint", [None, "int8"])
+types = pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+
+
+@types
+@checkpoints
+@pytest.mark.parametrize("shape", [(0, 16, 3, 3), (0, 16)])
+def test_group_norm_without_parameters(shape, checkpoint, dtype):
+    x = torch.empty(shape, device=DEV, dtype=dtype, requires_grad=True)
+    y = group_norm_act(x, 4, act="gelu", checkpoint=checkpoint)
+    dx, = torch.autograd.grad(y, x, torch.empty_like(y))
+    assert y.shape == dx.shape == x.shape
