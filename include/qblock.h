@@ -110,7 +110,7 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *desc, const void *dy, const vo
  *     dx = dg wg + du wu,   dwg = dg^T x,   dwu = du^T x,   dbg, dbu = column sums
  *   dx : m x k dense of `dtype`; dwg, dwu : n x k dense of `dtype`, or float32
  *   (dw_f32), both or neither; dbg, dbu : n float32, each may be NULL.  Not all of
- *   them NULL.  x is needed for the weights' gradients, wg and wu for dx.  In bf16, dg
+ *   them NULL (but for m = 0).  x is needed for the weights' gradients, wg and wu for dx.  In bf16, dg
  *   and du are rounded once to bf16 as operands of the products; the column sums take
  *   them unrounded.  relu'(0) = 0.
  * Operands whose rows are not whole, aligned 16-byte vectors are copied into the

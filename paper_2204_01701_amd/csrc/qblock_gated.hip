@@ -289,8 +289,9 @@ ql_status qblock_gated_bwd(const qblock_gated_desc *d, const void *x, const void
                            const int8_t *q, const uint8_t *e, void *dx, void *dwg, void *dwu, float *dbg, float *dbu, void *workspace,
                            size_t workspace_bytes, void *stream) {
     if (!gated_ok(d) || d->ldh < d->n) return QL_EINVAL;
-    if ((!dx && !dwg && !dbg && !dbu) || !dwg != !dwu) return QL_EINVAL;
+    if ((d->m > 0 && !dx && !dwg && !dbg && !dbu) || !dwg != !dwu) return QL_EINVAL;  // (of no rows dx is no pointer)
     if (!sizes_fit(d)) return QL_EUNSUPPORTED;
+    if (d->m == 0 && !dwg && !dbg && !dbu) return QL_OK;
     if (d->m > 0 && (!dh || (!z && (!q || !e)) || (dx && (!wg || !wu)) || (dwg && !x))) return QL_EINVAL;
     const void *ptrs[] = {x, wg, wu, dh, z, dx};
     for (const void *p : ptrs)
