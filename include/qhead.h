@@ -49,7 +49,7 @@ extern "C" {
  * Backward, with dy = dl/dy (m x n, ldy), from the stored z:
  *     dz = dy o act'(z),  dx = dz w,  dw = dz^T x,  db = column sums of dz
  *   (dr = dy).  dx : m x k dense of `dtype`; dw : n x k dense of `dtype`, or float32 (dw_f32); db : n float32.
- *   Each of dx, dw, db may be NULL (not all).  z may be NULL for QL_ACT_NONE;
+ *   Each of dx, dw, db may be NULL (not all, but for m = 0).  z may be NULL for QL_ACT_NONE;
  *   x is needed for dw, w for dx.  In bf16, dz is rounded once to bf16 as the
  *   operand of both products; db sums it unrounded.  relu'(0) = 0.
  * Operands whose rows are not whole, aligned 16-byte vectors are copied into the

@@ -283,8 +283,9 @@ size_t qhead_linear_bwd_workspace_size(const qhead_linear_desc *d) {
 ql_status qhead_linear_bwd(const qhead_linear_desc *d, const void *x, const void *w, const void *dy, const void *z,
                            void *dx, void *dw, float *db, void *workspace, size_t workspace_bytes, void *stream) {
     if (!linear_ok(d) || d->ldy < d->n) return QL_EINVAL;
-    if (!dx && !dw && !db) return QL_EINVAL;
+    if (d->m > 0 && !dx && !dw && !db) return QL_EINVAL;  // (of no rows dx is no pointer)
     if (!sizes_fit(d)) return QL_EUNSUPPORTED;
+    if (d->m == 0 && !dw && !db) return QL_OK;
     if (d->m > 0 && (!dy || (d->act != QL_ACT_NONE && !z) || (dx && !w) || (dw && !x))) return QL_EINVAL;
     const void *ptrs[] = {x, w, dy, z, dx};
     for (const void *p : ptrs)

@@ -33,3 +33,12 @@ def test_gated_gradient_of_the_input_alone(L, dtype):
     assert L.qblock_gated_bwd(desc(0), *[None] * 12, None, 0, None) == OK
     assert L.qblock_gated_bwd(desc(0), P, P, P, P, P, None, None, P, None, None, None, None, None, 0, None) == OK
     assert L.qblock_gated_bwd(desc(1), *[P] * 5, None, None, *[None] * 5, P, 1 << 60, None) == EINVAL
+
+
+@pytest.mark.parametrize("dtype", [ql.QL_BF16, ql.QL_F32], ids=["bf16", "fp32"])
+def test_first_order_gradient_of_the_input_alone(L, dtype):
+    def desc(m):
+        return ctypes.byref(ql.HeadLinearDesc(m, 16, 24, 16, 16, 24, 24, dtype, 4, 0, 0))
+    assert L.qhead_linear_bwd(desc(0), *[None] * 7, None, 0, None) == OK
+    assert L.qhead_linear_bwd(desc(0), P, P, P, P, P, None, None, None, 0, None) == OK
+    assert L.qhead_linear_bwd(desc(1), P, P, P, P, None, None, None, P, 1 << 60, None) == EINVAL

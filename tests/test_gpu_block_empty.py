@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2204_01701_amd.autograd import gated_linear, group_norm_act
+from paper_2204_01701_amd.autograd import gated_linear, group_norm_act, linear_act
 from test_gpu_block_keep import DEV, TYPES, type_ids
 
 pytestmark = pytest.mark.gpu
@@ -29,3 +29,15 @@ def test_gated_layer_with_frozen_weights(shape, checkpoint, dtype):
     h = gated_linear(x, w, u, checkpoint=checkpoint)
     dx, = torch.autograd.grad(h, x, torch.empty_like(h))
     assert h.shape == shape[:-1] + (33,) and dx.shape == x.shape
+
+
+@types
+@checkpoints
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("shape", [(0, 40), (2, 0, 40)])
+def test_first_order_layer_with_a_frozen_weight(shape, act, checkpoint, dtype):
+    x = torch.empty(shape, device=DEV, dtype=dtype, requires_grad=True)
+    w = torch.randn(33, 40, device=DEV, dtype=dtype)
+    y = linear_act(x, w, act=act, checkpoint=checkpoint)
+    dx, = torch.autograd.grad(y, x, torch.empty_like(y))
+    assert y.shape == shape[:-1] + (33,) and dx.shape == x.shape
