@@ -291,7 +291,10 @@ ql_status qblock_gated_bwd(const qblock_gated_desc *d, const void *x, const void
     if (!gated_ok(d) || d->ldh < d->n) return QL_EINVAL;
     if ((d->m > 0 && !dx && !dwg && !dbg && !dbu) || !dwg != !dwu) return QL_EINVAL;  // (of no rows dx is no pointer)
     if (!sizes_fit(d)) return QL_EUNSUPPORTED;
-    if (d->m == 0 && !dwg && !dbg && !dbu) return QL_OK;
+    if (d->m == 0) {
+        if (!dwg && !dbg && !dbu) return QL_OK;
+        dx = nullptr;  // (nothing to write there: a launch without workgroups, which HIP refuses, would end the call)
+    }
     if (d->m > 0 && (!dh || (!z && (!q || !e)) || (dx && (!wg || !wu)) || (dwg && !x))) return QL_EINVAL;
     const void *ptrs[] = {x, wg, wu, dh, z, dx};
     for (const void *p : ptrs)
