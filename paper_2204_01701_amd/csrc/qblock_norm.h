@@ -684,12 +684,17 @@ __global__ __launch_bounds__(1024) void qblock_norm_param_kernel(const float2 *c
     const int col = threadIdx.x & 15, j = blockIdx.x * 16 + col, r0 = threadIdx.x >> 4;
     float u = 0.0f, w = 0.0f;
     if (j < c)
-        for (int r = r0; r < rows; r += 256) {
-            float2 x[4];
+        for (int q = r0; q < rows; q += 4096) {  // (64 of a thread's rows, and sums of these)
+            float2 t = make_float2(0.0f, 0.0f);
+            const int end = min(rows, q + 4096);
+            for (int r = q; r < end; r += 256) {
+                float2 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = r + 64 * k < rows ? chan[(size_t)(r + 64 * k) * c + j] : make_float2(0.0f, 0.0f);
+                for (int k = 0; k < 4; ++k) x[k] = r + 64 * k < rows ? chan[(size_t)(r + 64 * k) * c + j] : make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) u += x[k].x, w += x[k].y;
+                for (int k = 0; k < 4; ++k) t.x += x[k].x, t.y += x[k].y;
+            }
+            u += t.x, w += t.y;
         }
     sum[r0][col] = make_float2(u, w);
     __syncthreads();

@@ -15,8 +15,9 @@ bool sizes_fit(const qblock_norm_desc *d) {
     return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20 && (double)d->n * d->hw * d->c < 140737488355328.0;
 }
 
-// The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most.
-void share_samples(NormPlan &p, int n, long long most) {
+// The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most, but where each would then take
+// more than `run` batches.
+void share_samples(NormPlan &p, int n, long long most, long long run) {
     // Outputs are streamed where a workgroup writes whole rows, or at least 64 bytes (bf16) or 128 (float32) of one:
     // 128 x 1024 x 256, bf16, forward 45 to 35 us; 512 x 49 x 512, float32, 28 to 22.  Lesser parts of lines lose by it: 32
     // bytes in bf16 77 to 94 us, 64 in float32 62 to 74.
@@ -24,12 +25,17 @@ void share_samples(NormPlan &p, int n, long long most) {
     p.a.stream = p.a.segs == 1 || p.a.parts > 1 || line >= (p.es == 2 ? 64 : 128);
     const int snl = log2_up(p.th) - p.a.svl - p.a.pnl;
     const long long groups = ((long long)n + (1LL << snl) - 1) >> snl;
-    p.a.slots = (int)std::max(1LL, std::min(groups, most));
+    p.a.slots = (int)std::max(1LL, std::min(groups, std::max(most, (groups + run - 1) / run)));
     p.a.blocks = (int)((long long)p.a.slots * p.a.chunks * p.a.segs);
     p.a.by_segs = make_fastdiv(p.a.segs);
     p.a.by_chunks = make_fastdiv(p.a.chunks);
     p.a.by_wide = make_fastdiv(p.a.cpg);
 }
+
+// Batches of samples whose channels' sums the backward adds up one by one, in registers' form and in chunks (whose own sums are up to
+// 128 terms long).  2^20 rows of 4096 took 2048 of them, whose roundings cost up to 492 x 2^-24 of a sum; a.chan then has 8 bytes a
+// channel more for each of these runs, at most a fiftieth of x.
+constexpr long long kRunFused = 192, kRunChunks = 64, kNoRun = 1LL << 40;
 
 // bwd: the backward's plan (its registers hold dy as well, its workgroups share few lines of a.chan).
 NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
@@ -85,7 +91,7 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
             p.th = th_at;
             a.chunks = 1;
             a.chunk_px = d->hw;
-            share_samples(p, d->n, bwd ? std::max(1, cdiv(4 * kNumCUs, a.segs)) : (1 << 20) / a.segs + 1);
+            share_samples(p, d->n, bwd ? std::max(1, cdiv(4 * kNumCUs, a.segs)) : (1 << 20) / a.segs + 1, bwd ? kRunFused : kNoRun);
             if (bwd) p.chan_bytes = align_up((size_t)a.slots * d->c * sizeof(float2));
             return p;
         }
@@ -110,7 +116,8 @@ NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
     p.r = per <= 2 ? 2 : 8;
     a.chunk_px = (int)std::min<long long>(d->hw, per << a.pnl);
     a.chunks = cdiv(d->hw, a.chunk_px);
-    share_samples(p, d->n, bwd ? std::max(1LL, 8LL * kNumCUs / ((long long)a.segs * a.chunks)) : (1LL << 22) / ((long long)a.segs * a.chunks) + 1);
+    share_samples(p, d->n, bwd ? std::max(1LL, 8LL * kNumCUs / ((long long)a.segs * a.chunks)) : (1LL << 22) / ((long long)a.segs * a.chunks) + 1,
+                  bwd ? kRunChunks : kNoRun);
     p.part_bytes = align_up((size_t)std::max(1, d->n) * a.chunks * a.parts * d->groups * sizeof(float2));
     p.joined_bytes = align_up((size_t)std::max(1, d->n) * d->groups * sizeof(float2));  // (mean and rstd, or the two averages)
     if (bwd) p.chan_bytes = align_up((size_t)a.slots * a.chunks * d->c * sizeof(float2));
