@@ -390,9 +390,21 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(kThreads) void qbl
     const int cg = threadIdx.x & 31, rg = threadIdx.x >> 5;
     const int j = blockIdx.x * 256 + cg * 8, n8 = a.n - j, blocks = (a.n + kKeep - 1) / kKeep;
     const int begin = blockIdx.y * a.rpp, end = min(a.m, begin + a.rpp);
+    // (a thread's sums over 64 rows, and sums of these: 2^24 rows are 16384 a thread, whose roundings added up to 3900 x 2^-24)
     float s[2][8] = {};
+    auto keep = [&](bool first) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float *to0 = &sum[0][rg][cg * 8 + k], *to1 = &sum[1][rg][cg * 8 + k];
+            *to0 = first ? s[0][k] : *to0 + s[0][k], *to1 = first ? s[1][k] : *to1 + s[1][k];
+            s[0][k] = s[1][k] = 0.0f;
+        }
+    };
+    int left = 32;
+    keep(true);
     if (j < a.np)
         for (int i0 = begin + rg; i0 < end; i0 += 16) {
+            if (--left < 0) keep(false), left = 31;
             float d[2][8], g[2][8], u[2][8];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {  // (two rows requested together)
@@ -437,8 +449,7 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(kThreads) void qbl
             }
         }
     if (!a.part0 && !a.part1) return;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum[0][rg][cg * 8 + k] = s[0][k], sum[1][rg][cg * 8 + k] = s[1][k];
+    keep(false);
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= a.n) return;
@@ -460,7 +471,12 @@ __global__ __launch_bounds__(kThreads) void qblock_gated_colsum_kernel(const flo
     const int c = threadIdx.x & 31, r = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
     float s = 0.0f;
     if (j < n)
-        for (int p = r; p < parts; p += 8) s += part[(size_t)p * n + j];
+        for (int p0 = r; p0 < parts; p0 += 512) {  // (64 parts, and sums of these)
+            const int end = min(parts, p0 + 512);
+            float t = 0.0f;
+            for (int p = p0; p < end; p += 8) t += part[(size_t)p * n + j];
+            s += t;
+        }
     sum[r][c] = s;
     __syncthreads();
     if (r || j >= n) return;

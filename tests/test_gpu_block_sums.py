@@ -28,3 +28,16 @@ def test_norm_parameters():
     ql.qblock_norm_bwd(ones, ones, groups, None, None, mean, rstd, None, dg, db)
     assert bool((db == n).all())
     assert float((dg.double() - n * v).abs().max()) <= ref.DEPTH * ref.U32 * n * v
+
+
+def test_gated_biases():
+    """2^24 rows: dbu sums dh g = 1, dbg sums dh u = 1 + d.  64 rows of a thread, 128 of these sums, eight threads, the parts."""
+    m, k, n = 2**24, 8, 4
+    v = least_kept(14)
+    z = torch.ones(2, m, n, device=DEV)
+    z[1] = v
+    dh, w = torch.ones(m, n, device=DEV), torch.zeros(n, k, device=DEV)
+    dbg, dbu = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ql.qblock_gated_bwd(None, w, w, dh, z, dbg=dbg, dbu=dbu, act="none")
+    assert bool((dbu == m).all())
+    assert float((dbg.double() - m * v).abs().max()) <= (64 + 128 + 8 + 64 + 8) * ref.U32 * m * v
