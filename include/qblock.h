@@ -116,10 +116,14 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *desc, const void *dy, const vo
  * Operands whose rows are not whole, aligned 16-byte vectors are copied into the
  * workspace; the query covers what the descriptor shows, and misaligned pointers if
  * `unaligned` is set.  A misaligned pointer among x, wg, wu without it: QL_EINVAL,
- * but for the forward of up to 16 rows without a checkpoint, which reads any layout.
+ * but for the forward of up to QBLOCK_FEW_ROWS rows without a checkpoint, which reads
+ * any layout and needs no workspace, whatever the query (which does not know of the
+ * checkpoint) returns.
  * Sizes: m >= 0 (m = 0: zeros in the weights' and bias gradients), k, n >= 1;
  * QL_EUNSUPPORTED for m above 2^31 - 65536, or k or n above 2^19.
  * ------------------------------------------------------------------------- */
+#define QBLOCK_FEW_ROWS 16
+
 typedef struct {
     int m, k, n;
     long long ldx, ldw, ldh;

@@ -711,7 +711,7 @@ def _head_dense(index, *operands):
 
 
 def _head_call(name, query, desc, ptrs, index, workspace, stream):
-    """The entry point on checked pointers; query: its workspace query, or None if it takes no workspace."""
+    """The entry point on checked pointers; query: its workspace query, or None if it takes no workspace ("": this call needs none)."""
     L = lib()
     if stream is None:
         st = _current_stream(index)
@@ -724,7 +724,7 @@ def _head_call(name, query, desc, ptrs, index, workspace, stream):
         if workspace is not None:
             wp, wn = _workspace(workspace, 0, None)
         else:
-            wp, wn = None, getattr(L, query)(ref)
+            wp, wn = None, getattr(L, query)(ref) if query else 0
             if wn:
                 import torch
                 wp, wn = _workspace(None, wn, torch.device("cuda", index), stream)
@@ -870,6 +870,7 @@ def qhead_distill_step(logits, t_ids, t_logits, labels, g, loss, dlogits, temper
 # --- blocks trained with activations in 8 bits (include/qblock.h) ----------------
 
 BLOCK_KEEP = 32  # QBLOCK_KEEP of qblock.h: neighbours that share a power of two in a checkpoint
+BLOCK_FEW_ROWS = 16  # QBLOCK_FEW_ROWS of qblock.h: up to these the gated layer's forward without a checkpoint needs no workspace
 
 
 def _block_call(name, query, desc, ptrs, index, workspace, stream):
@@ -910,7 +911,7 @@ def _block_launch(name, desc, ptrs, index, query=None):
     if query is None:
         status = getattr(L, name)(ref, *ptrs, _current_stream(index))
     else:
-        need = getattr(L, query)(ref)
+        need = getattr(L, query)(ref) if query else 0
         if need:
             ws = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
             status = getattr(L, name)(ref, *ptrs, ws.data_ptr(), need, _current_stream(index))
@@ -1024,6 +1025,12 @@ def _gated_weights(index, wg, wu, shape, dt):
     return pg, pu, ldg
 
 
+def _gated_fwd_query(m, q):
+    """The forward's workspace query.  It does not know of the checkpoint, without which a few rows need no workspace: the weights
+    are read in place, whatever their layout (else 134 MB for a bf16 row of 4097 and 8192 outputs, which nothing touches)."""
+    return "" if m <= BLOCK_FEW_ROWS and q is None else "qblock_gated_fwd_workspace_size"
+
+
 def qblock_gated_fwd(x, wg, wu, bg, bu, h, z=None, q=None, e=None, act="silu", workspace=None, stream=None):
     """h = act(x wg^T + bg) * (x wu^T + bu).
 
@@ -1038,7 +1045,7 @@ def qblock_gated_fwd(x, wg, wu, bg, bu, h, z=None, q=None, e=None, act="silu", w
     ph, ldh = _head_rows("h", h, (m, n), dt, i)
     f32 = _float32()
     pbg, pbu, pz = _head_dense(i, ("bg", bg, (n,), f32), ("bu", bu, (n,), f32), ("z", z, (2, m, n), dt))
-    _block_call("qblock_gated_fwd", "qblock_gated_fwd_workspace_size",
+    _block_call("qblock_gated_fwd", _gated_fwd_query(m, q),
                 BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, ldh, code, _head_act(act), _unaligned(px, pg, pu), 0),
                 (px, pg, pu, pbg, pbu, ph, pz, *_kept_dense(i, q, e, (2, m), n)), i, workspace, stream)
 

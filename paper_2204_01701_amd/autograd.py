@@ -61,7 +61,7 @@ from . import (NEURON_TERMS, QL_BF16, QL_F32, QL_NEURON_QUADRA, QL_NEURON_T2, QL
                qlayer_linear_bwd, qlayer_linear_bwd_relu, qlayer_linear_fwd, qlayer_linear_fwd_ex,
                qhead_distill_bwd, qhead_distill_fwd, qhead_linear_bwd, qhead_linear_fwd, qhead_logprobs_bwd,
                qhead_logprobs_fwd, BLOCK_KEEP, BlockGatedDesc, BlockKeepDesc, BlockNormDesc, HeadLinearDesc,
-               _block_launch, _head_act, _int, _unaligned)
+               _block_launch, _gated_fwd_query, _head_act, _int, _unaligned)
 
 __all__ = ["quad_conv2d", "quad_linear", "QuadConv2dFunction", "QuadLinearFunction", "linear_act", "token_logprobs",
            "distill_loss", "LinearActFunction", "TokenLogprobsFunction", "DistillLossFunction", "group_norm_act",
@@ -697,7 +697,7 @@ class GatedLinearFunction(torch.autograd.Function):
         px, pg, pu = xm.data_ptr(), wgm.data_ptr(), wum.data_ptr()
         desc = BlockGatedDesc(_int(m), _int(k), _int(n), ldx, ldw, n, _qdtype(x), _head_act(act), _unaligned(px, pg, pu), 0)
         _block_launch("qblock_gated_fwd", desc, (px, pg, pu, _ptr(bgf), _ptr(buf), h.data_ptr(), _ptr(z), _ptr(q), _ptr(e)), x.get_device(),
-                      "qblock_gated_fwd_workspace_size")
+                      _gated_fwd_query(m, q))
         if train:
             # (of x only what the weights' gradients read)
             xs = xm if any(ctx.needs_input_grad[1:3]) else None

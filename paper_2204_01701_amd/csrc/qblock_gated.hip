@@ -116,7 +116,7 @@ GradsPlan plan_grads(const qblock_gated_desc *d) {
     return p;
 }
 
-bool few_rows(const qblock_gated_desc *d, bool keep) { return d->m <= 16 && !keep && env_override("QBLOCK_TILE", -1) < 0; }
+bool few_rows(const qblock_gated_desc *d, bool keep) { return d->m <= QBLOCK_FEW_ROWS && !keep; }
 
 struct Pads {
     size_t x, w;  // bytes of x's copy, of one weight's
