@@ -390,21 +390,9 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(kThreads) void qbl
     const int cg = threadIdx.x & 31, rg = threadIdx.x >> 5;
     const int j = blockIdx.x * 256 + cg * 8, n8 = a.n - j, blocks = (a.n + kKeep - 1) / kKeep;
     const int begin = blockIdx.y * a.rpp, end = min(a.m, begin + a.rpp);
-    // (a thread's sums over 64 rows, and sums of these: 2^24 rows are 16384 a thread, whose roundings added up to 3900 x 2^-24)
     float s[2][8] = {};
-    auto keep = [&](bool first) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            float *to0 = &sum[0][rg][cg * 8 + k], *to1 = &sum[1][rg][cg * 8 + k];
-            *to0 = first ? s[0][k] : *to0 + s[0][k], *to1 = first ? s[1][k] : *to1 + s[1][k];
-            s[0][k] = s[1][k] = 0.0f;
-        }
-    };
-    int left = 32;
-    keep(true);
     if (j < a.np)
         for (int i0 = begin + rg; i0 < end; i0 += 16) {
-            if (--left < 0) keep(false), left = 31;
             float d[2][8], g[2][8], u[2][8];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {  // (two rows requested together)
@@ -449,7 +437,8 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(kThreads) void qbl
             }
         }
     if (!a.part0 && !a.part1) return;
-    keep(false);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[0][rg][cg * 8 + k] = s[0][k], sum[1][rg][cg * 8 + k] = s[1][k];
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= a.n) return;

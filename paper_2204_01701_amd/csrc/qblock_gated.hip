@@ -191,9 +191,10 @@ struct DzPlan {
     int rpp, parts;
     size_t dz_bytes, part_bytes;
     explicit DzPlan(const qblock_gated_desc *d) {
-        // (up to 64 rows are one part, whose sums are the results themselves; from 2^23 rows on there are more parts than 128, up to
-        // 2^15, so that neither a part's sums nor their joining grow longer)
-        rpp = d->m <= 64 ? std::max(1, d->m) : std::max(32, std::min(1 << 16, cdiv(d->m, 128)));
+        // (up to 64 rows are one part, whose sums are the results themselves.  A part has at most 1024 rows, 128 a thread, as long as
+        // a grid's 65535 rows of workgroups take the parts, up to 2^26 rows: 2^24 rows in 128 parts made sums of 16384 terms, whose
+        // roundings added up to 3900 x 2^-24; a second sum in the kernel, for every 64 rows, gives the same bound and costs 1.5 % of every pass)
+        rpp = d->m <= 64 ? std::max(1, d->m) : std::max({32, std::min(1024, cdiv(d->m, 128)), cdiv(d->m, 65535)});
         parts = std::max(1, cdiv(d->m, rpp));
         dz_bytes = align_up((size_t)d->m * 2 * half_columns(d) * esize(d->dtype));
         part_bytes = parts > 1 ? align_up((size_t)parts * 2 * d->n * sizeof(float)) : 0;
