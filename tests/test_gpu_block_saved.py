@@ -114,3 +114,27 @@ def test_first_order_layer(m, k, n, order, dtype):
     x, w = leaves  # (the weight alone: the input's gradient without an activation reads nothing else)
     check([x], lambda x: linear_act(x, w.detach(), checkpoint="int8"), _gpu_order(order))
     refused([x], lambda x: linear_act(x, w.detach(), checkpoint="int8"))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=type_ids)
+@pytest.mark.parametrize("checkpoint", [None, "int8"])
+@pytest.mark.parametrize("pinned", [False, True])
+def test_kept_in_host_memory(pinned, checkpoint, dtype):
+    """torch's own hook, whose pinned copies are dense whatever was saved."""
+    def of(*shapes):
+        return [leaf(*s, dtype=dtype) for s in shapes]
+    wide = torch.randn(36, 96, device=DEV).to(dtype)
+    halves = [wide[:, i:i + 40].requires_grad_(True) for i in (0, 48)]  # (one row stride, other than their length)
+    image = torch.randn(2, 40, 5, 6, device=DEV).to(dtype).contiguous(memory_format=torch.channels_last).requires_grad_(True)
+    for leaves, f in ((of((20, 40)) + halves, lambda *a: gated_linear(*a, checkpoint=checkpoint)),
+                      (of((20, 40)) + halves[:1], lambda *a: linear_act(*a, act="gelu", checkpoint=checkpoint)),
+                      ([image, *of((40,), (40,))], lambda x, g, b: group_norm_act(x, 4, g, b, act="silu", checkpoint=checkpoint)),
+                      (of((20, 40), *[(36, 40)] * 3), lambda *a: quad_linear(*a, relu=True, checkpoint=checkpoint)),
+                      ([image, *of(*[(36, 40, 3, 3)] * 3)], lambda *a: quad_conv2d(*a, pad=1, relu=True, checkpoint=checkpoint))):
+        y = f(*leaves)
+        dy = torch.randn_like(y)
+        want = torch.autograd.grad(y, leaves, dy)
+        with torch.autograd.graph.save_on_cpu(pin_memory=pinned):
+            y = f(*leaves)
+        for got, w in zip(torch.autograd.grad(y, leaves, dy), want):
+            assert torch.equal(got, w)
