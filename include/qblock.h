@@ -35,9 +35,10 @@ extern "C" {
  * magnitude in a block,
  *     E = the least integer >= -126 with amax <= 127 * 2^E,
  *     q = x / 2^E rounded to the nearest integer (halves to even),   x8 = q 2^E.
- * |x - x8| <= 2^E / 2 <= amax / 127 (while 2^E >= 2^-125).  x8 is exact in bfloat16
- * and float32: reading a checkpoint rounds nothing.  At the very end of the range
- * (E = 122) |q| is at most 63, so that x8 is finite.
+ * |x - x8| <= 2^E / 2 <= amax / 127 (for 2^E from 2^-125 to 2^121).  x8 is exact in
+ * bfloat16 and float32: reading a checkpoint rounds nothing.  At the very end of the
+ * range (E = 122) |q| is at most 63, so that x8 is finite: magnitudes above 63.5 2^122
+ * read back as 63 2^122, up to a whole 2^122 less.
  *   q : rows x cols int8, dense.   e : rows x ceil(cols / 32) uint8, dense: E + 127.
  * A block with a NaN or an infinity has e = 255 and reads back as NaN throughout.
  * An e that no pack writes (0, 250 .. 254) reads as the power of two e - 127, 0 as 0.
@@ -66,8 +67,8 @@ ql_status qblock_unpack8(const qblock_keep_desc *desc, const int8_t *q, const ui
  *   mean, rstd  : n x groups float32, for the backward; either may be NULL.
  *   q, e        : NULL, or the checkpoint of x as (n hw) x c, written on the way.
  * y may be x.  Statistics are float32, from sums of differences to a mean (large
- * offsets of a group cancel before they are squared); they overflow where (x - mean)^2
- * does.  A NaN or infinity reaches its group of its sample and nothing else.
+ * offsets of a group cancel before they are squared); where a sum of (x - mean)^2
+ * overflows, rstd is 0, and where a sum of x does, NaN.  A NaN or infinity reaches its group of its sample and nothing else.
  *
  * Backward, with dy = dl/dy:
  *     dz = dy act'(z),   dbeta = sum dz,   dgamma = sum dz xh   (over samples and pixels)
@@ -116,7 +117,8 @@ ql_status qblock_norm_bwd(const qblock_norm_desc *desc, const void *dy, const vo
  * Operands whose rows are not whole, aligned 16-byte vectors are copied into the
  * workspace; the query covers what the descriptor shows, and misaligned pointers if
  * `unaligned` is set.  A misaligned pointer among x, wg, wu without it: QL_EINVAL,
- * but for the forward of up to QBLOCK_FEW_ROWS rows without a checkpoint, which reads
+ * but where k is not whole 16-byte vectors (which are copied in any case), and for the
+ * forward of up to QBLOCK_FEW_ROWS rows without a checkpoint, which reads
  * any layout and needs no workspace, whatever the query (which does not know of the
  * checkpoint) returns.
  * Sizes: m >= 0 (m = 0: zeros in the weights' and bias gradients), k, n >= 1;

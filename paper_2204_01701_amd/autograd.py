@@ -45,7 +45,8 @@ under the same terms.  They, ``linear_act`` and the quadratic layers take
 ``checkpoint="int8"``, the third memory mode beside saving and recomputing: what the backward
 reads of the activations (X, T_a and T_b, pre-activations) is kept in 8 bits, blocks of 32
 channels with a power of two each (include/qblock.h), and the gradients are formed from these
-values.  The outputs are those without it, bit for bit (``gated_linear`` of up to 16 rows: but for a
+values.  A quadratic layer with relu=True keeps its output beside them, as it is, for the mask; where
+that output is the next layer's X, the checkpoint of X comes on top of it.  The outputs are those without it, bit for bit (``gated_linear`` of up to 16 rows: but for a
 rounding).  As nothing then ties the gradients to the
 activations, a backward under ``create_graph`` raises.
 """
@@ -345,7 +346,7 @@ def quad_conv2d(x, wa, wb=None, wc=None, ba=None, bb=None, bc=None, stride=1, pa
                 neuron=QL_NEURON_QUADRA, relu=False, groups=1, checkpoint=None):
     """Quadratic 2-D convolution layer (NCHW-shaped tensors, channels_last memory).
 
-    checkpoint="int8" keeps X and, unless recompute, T_a and T_b in 8 bits for the backward."""
+    checkpoint="int8" keeps X and, unless recompute, T_a and T_b in 8 bits for the backward (with relu also the output, in full)."""
     _kept(checkpoint)
     return QuadConv2dFunction.apply(x, wa, wb, wc, ba, bb, bc, stride, pad, recompute, neuron, relu, groups,
                                     checkpoint if torch.is_grad_enabled() else None)

@@ -98,7 +98,8 @@ GradsPlan plan_grads(const qblock_gated_desc *d) {
     for (Tile t : {TILE_64, TILE_128, TILE_256}) {
         if (forced_tile >= 0 && (int)t != forced_tile) continue;
         // (bf16 in the large tiles, of which a CU holds one, is what the sum of steps describes: 526 us for 4096 x 2048 -> 8192,
-        // in turn 554; small tiles share a CU, and float32 ones in one launch took 660 us for 2048 x 1024 -> 4096, in turn 558)
+        // in turn 554.  Small tiles share a CU; of float32 one size was measured, 2048 x 1024 -> 4096 of many tiles: 660 us in one
+        // launch, in turn 558.  Sizes with fewer tiles than CUs were not)
         if (forced != 1 && (t != TILE_256 || d->dtype != QL_BF16)) continue;
         GatedPlan x{}, w{};
         x.tile = w.tile = t;
@@ -116,6 +117,8 @@ GradsPlan plan_grads(const qblock_gated_desc *d) {
     return p;
 }
 
+// (1 row of 4096 -> 8192 takes 32 us in bf16 and 62 in float32, 16 rows 37 and 63.  In bf16 the tiles, which take 28 for 64 rows, may be
+// faster from a few rows on; they need a workspace for splits and whole vectors)
 bool few_rows(const qblock_gated_desc *d, bool keep) { return d->m <= QBLOCK_FEW_ROWS && !keep; }
 
 struct Pads {
