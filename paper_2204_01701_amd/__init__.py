@@ -35,7 +35,7 @@ __all__ = [
     "HEAD_ACTS", "HEAD_MAX_TOP", "HeadLinearDesc", "HeadRowsDesc",
     "qhead_linear_fwd", "qhead_linear_bwd", "qhead_logprobs_fwd", "qhead_logprobs_bwd",
     "qhead_distill_fwd", "qhead_distill_bwd", "qhead_distill_step",
-    "BLOCK_KEEP", "BlockKeepDesc", "BlockNormDesc", "BlockGatedDesc",
+    "BLOCK_KEEP", "BLOCK_FEW_ROWS", "BlockKeepDesc", "BlockNormDesc", "BlockGatedDesc",
     "qblock_pack8", "qblock_unpack8", "qblock_norm_fwd", "qblock_norm_bwd", "qblock_gated_fwd", "qblock_gated_bwd",
 ]
 

@@ -1,5 +1,7 @@
 """Batches of no rows at the C ABI, whose tensors may be NULL as those of an empty torch tensor are: nothing to do is no error."""
 import ctypes
+import os
+import re
 
 import pytest
 
@@ -42,3 +44,8 @@ def test_first_order_gradient_of_the_input_alone(L, dtype):
     assert L.qhead_linear_bwd(desc(0), *[None] * 7, None, 0, None) == OK
     assert L.qhead_linear_bwd(desc(0), P, P, P, P, P, None, None, None, 0, None) == OK
     assert L.qhead_linear_bwd(desc(1), P, P, P, P, None, None, None, P, 1 << 60, None) == EINVAL
+
+
+def test_constants_of_the_header():
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qblock.h")).read()
+    assert dict(re.findall(r"#define (QBLOCK_\w+) (\d+)", header)) == {"QBLOCK_KEEP": str(ql.BLOCK_KEEP), "QBLOCK_FEW_ROWS": str(ql.BLOCK_FEW_ROWS)}
