@@ -668,7 +668,8 @@ def group_norm_act(x, groups, weight=None, bias=None, eps=1e-5, act="none", chec
     x (N, C, H, W), used in channels_last memory, or (N, C); weight and bias (C) or None; act as in linear_act.
     The backward reads x, or with checkpoint="int8" what 8 bits of it say."""
     _kept(checkpoint)
-    return GroupNormActFunction.apply(x, weight, bias, groups, eps, act, torch.is_grad_enabled(), checkpoint)
+    # (laid out here, where the copy has a graph of its own: inside, the backward would keep the copy, and x for _once)
+    return GroupNormActFunction.apply(_dense_image(x), weight, bias, groups, eps, act, torch.is_grad_enabled(), checkpoint)
 
 
 class GatedLinearFunction(torch.autograd.Function):
