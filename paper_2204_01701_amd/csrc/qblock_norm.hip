@@ -15,8 +15,8 @@ bool sizes_fit(const qblock_norm_desc *d) {
     return d->n <= kMostInt && d->hw <= kMostInt && d->c <= 1 << 20 && (double)d->n * d->hw * d->c < 140737488355328.0;
 }
 
-// The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most, but where each would then take
-// more than `run` batches.
+// The samples over workgroups: SN of them at once, `most` workgroups a segment and chunk at most, but a multiple of these where each
+// would take more than `run` batches (a multiple, for equal shares on the CUs: 2^18 x 16 x 256 in 1306 us, 1571 with as few as it takes).
 void share_samples(NormPlan &p, int n, long long most, long long run) {
     // Outputs are streamed where a workgroup writes whole rows, or at least 64 bytes (bf16) or 128 (float32) of one:
     // 128 x 1024 x 256, bf16, forward 45 to 35 us; 512 x 49 x 512, float32, 28 to 22.  Lesser parts of lines lose by it: 32
@@ -25,7 +25,8 @@ void share_samples(NormPlan &p, int n, long long most, long long run) {
     p.a.stream = p.a.segs == 1 || p.a.parts > 1 || line >= (p.es == 2 ? 64 : 128);
     const int snl = log2_up(p.th) - p.a.svl - p.a.pnl;
     const long long groups = ((long long)n + (1LL << snl) - 1) >> snl;
-    p.a.slots = (int)std::max(1LL, std::min(groups, std::max(most, (groups + run - 1) / run)));
+    const long long times = std::max(1LL, (groups + run * most - 1) / (run * most));
+    p.a.slots = (int)std::max(1LL, std::min(groups, most * times));
     p.a.blocks = (int)((long long)p.a.slots * p.a.chunks * p.a.segs);
     p.a.by_segs = make_fastdiv(p.a.segs);
     p.a.by_chunks = make_fastdiv(p.a.chunks);
@@ -35,7 +36,7 @@ void share_samples(NormPlan &p, int n, long long most, long long run) {
 // Batches of samples whose channels' sums the backward adds up one by one, in registers' form and in chunks (whose own sums are up to
 // 128 terms long).  2^20 rows of 4096 took 2048 of them, whose roundings cost up to 492 x 2^-24 of a sum; a.chan then has 8 bytes a
 // channel more for each of these runs, at most a fiftieth of x.
-constexpr long long kRunFused = 192, kRunChunks = 64, kNoRun = 1LL << 40;
+constexpr long long kRunFused = 192, kRunChunks = 64, kNoRun = 1LL << 32;
 
 // bwd: the backward's plan (its registers hold dy as well, its workgroups share few lines of a.chan).
 NormPlan plan_norm(const qblock_norm_desc *d, bool bwd) {
